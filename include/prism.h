@@ -15,6 +15,9 @@
  *   prism_sqrt_newton  A^{1/2} and A^{-1/2}        R_k = I - M_k       (DB Newton, App. A.2)
  *   prism_run_grouped  any of them over groups of different shapes in one call
  *
+ * Beside them, operators of the layers whose weights such a step updates: prism_attention,
+ * prism_qk_norm_rope (both with their gradients) and prism_dropout; see their section.
+ *
  * Conventions common to all entry points
  *   - Every matrix pointer is a DEVICE pointer to row-major, contiguous,
  *     batch-strided data: x[batch][m][n].  The caller owns all of it.  Alignment
@@ -305,6 +308,81 @@ int prism_run_grouped_from(prism_fn fn, const prism_group* groups, const void* c
                            int root_p, prism_dtype dt, int degree, int max_iters, int sketch_dim, uint64_t seed,
                            double tol, void* stream, const prism_options* opt);
 
+/* ---- operators of a transformer layer, next to the optimizer step on its weights ----
+ *
+ * The same conventions: device pointers, work enqueued on `stream` and nothing else, errors in the return value.  Arrays of
+ * heads are [batch][token][head][dim] with any strides (in elements, negative ones excepted) between batches, tokens and heads;
+ * the entries of a head are contiguous.  PRISM_F32 or PRISM_BF16; sums, maxima and statistics are fp32 in either.  Pointers and
+ * strides that are multiples of 16 bytes are read as whole vectors, others entry by entry.  Weights, statistics, positions and masks are
+ * contiguous device arrays in 32 bits.  A call repeated gives the same bits.  Empty arrays are valid: nothing is enqueued or read. */
+typedef struct { int64_t batch, token, head; } prism_strides;
+
+/* y = residual + x [u >= limit] / (1 - limit / 65536), limit = p * 65536 rounded (half to even), for `count` contiguous elements; residual may be NULL (0).
+ * u of element e: group g = e / 8; the Philox4x32-10 words of key = seed, counter = (g low, g high, offset, 7) are w0 .. w3; u is the low
+ * (e even) or high half of w[e % 8 / 2].  No mask is stored: the gradient with respect to x is the same call on dy
+ * without the residual.  y may be x or the residual.  0 <= p < 1. */
+int prism_dropout(const void* x, const void* residual, void* y, int64_t count, prism_dtype dt, double p,
+                  uint64_t seed, uint32_t offset, void* stream);
+
+#define PRISM_MAX_NORM_HEAD 256      /* largest head_dim of prism_qk_norm_rope */
+#define PRISM_MAX_ATTENTION_HEAD 128 /* ... of prism_attention */
+
+typedef struct {
+  int32_t batch, len, q_heads, k_heads, head_dim; /* q_heads or k_heads may be 0 */
+  int32_t rot_dim;           /* the first rot_dim (even) entries of a head turn; 0: none */
+  int32_t norm;              /* 0: rotation only */
+  int32_t interleaved;       /* pair i is entries (2i, 2i + 1); 0: (i, i + rot_dim / 2) */
+  int32_t start;             /* position of the first token where positions is NULL */
+  float eps, scale;          /* of the norm; scale: factor of the rotated part (1, or what a stretched context asks for) */
+  const int32_t* positions;  /* [batch][len], or NULL: start, start + 1, ... */
+  const float* inv_freq;     /* [rot_dim / 2]: radians per position */
+  const float* q_weight;     /* [head_dim], or NULL: ones */
+  const float* k_weight;
+  prism_strides q, k;        /* inputs */
+  prism_strides q_out, k_out; /* results; backward: the gradients with respect to them */
+  prism_strides dq, dk;      /* backward: results */
+  void* workspace;           /* backward: device memory aligned to 256 bytes, or NULL for the stream's cached one */
+  size_t workspace_bytes;
+} prism_norm_rope_desc;
+
+/* n = x (mean x^2 + eps)^(-1/2) weight for every head of q and k, then the rotation of its pairs (a, b) by angle = position * inv_freq:
+ * scale (a cos - b sin, b cos + a sin).  The angle is exact to 1e-7 rad at any position.  q_out may be q with the same strides, k_out likewise k. */
+int prism_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, prism_dtype dt,
+                       const prism_norm_rope_desc* desc, void* stream);
+/* Gradients with respect to q, k and the weights (fp32 [head_dim], summed over all tokens and heads in a fixed order; NULL: not
+ * wanted) from those with respect to the results.  q and k (the inputs) are read only where norm is set.  dq may be dq_out with the same strides. */
+int prism_qk_norm_rope_backward(const void* dq_out, const void* dk_out, const void* q, const void* k, void* dq, void* dk,
+                                float* dq_weight, float* dk_weight, prism_dtype dt, const prism_norm_rope_desc* desc, void* stream);
+int prism_norm_rope_workspace_bytes(prism_dtype dt, const prism_norm_rope_desc* desc, size_t* out_bytes);
+
+typedef struct {
+  int32_t batch, q_len, k_len, q_heads, k_heads, head_dim; /* q_heads a multiple of k_heads: head h reads key head h / (q_heads / k_heads) */
+  int32_t causal;          /* query i, whose place is i + keys - q_len, sees keys up to its place */
+  float scale;             /* > 0 */
+  float softcap;           /* scores become softcap * tanh(scale q.k / softcap); 0: as they are */
+  const float* slopes;     /* [q_heads], or NULL: score -= slope |place - key| */
+  const int32_t* prefix;   /* [batch], or NULL; causal only: keys below prefix are seen by every query */
+  const int32_t* k_lens;   /* [batch], or NULL: `keys` of a sequence (clamped to 0 .. k_len); without: k_len */
+  const int32_t* q_doc;    /* [batch][q_len] and [batch][k_len], or both NULL: a query sees keys of its own */
+  const int32_t* k_doc;    /* document only, and a negative document nothing (padding) */
+  prism_strides q, k, v, out;
+  prism_strides dout, dq, dk, dv; /* backward */
+  void* workspace;         /* device memory aligned to 256 bytes, or NULL for the stream's cached one */
+  size_t workspace_bytes;
+} prism_attention_desc;
+
+/* out = softmax of the scores over the keys that a query sees, times v.  lse (fp32 [batch][q_heads][q_len], or NULL) receives the
+ * logarithm of the sum of the exponentials, which the backward pass reads.  A query that sees no key gets out = 0 and
+ * lse = -inf.  Keys and values past a sequence's length or of a negative document, and queries of a negative document, may hold anything.
+ * bf16 rounds the weights to bf16 before their product with v. */
+int prism_attention(const void* q, const void* k, const void* v, void* out, float* lse, prism_dtype dt,
+                    const prism_attention_desc* desc, void* stream);
+/* Gradients with respect to q, k and v; out and lse are those of the forward pass.  Shared key heads receive the sum over their query
+ * heads.  dq, dk and dv may not overlap any input. */
+int prism_attention_backward(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                             void* dq, void* dk, void* dv, prism_dtype dt, const prism_attention_desc* desc, void* stream);
+int prism_attention_workspace_bytes(prism_dtype dt, const prism_attention_desc* desc, int backward, size_t* out_bytes);
+
 /* ---- single steps of the path, exposed for unit tests and profiling ---- */
 
 /* S_k^T (Section 4.2: Gaussian sketch): out[n][sketch_dim] fp32 on the device,
@@ -365,9 +443,9 @@ int prism_gemm_bf16_nt(const uint16_t* A, const uint16_t* B, float* C, int batch
  * bracketed by a HIP event pair on the caller's stream.  prism_profile_enable(on) also discards
  * what was recorded so far.  prism_profile_collect waits for the recorded events and returns the
  * summed milliseconds and the launch counts per kernel kind (host arrays of PRISM_PROFILE_KINDS
- * entries; nkinds >= PRISM_PROFILE_KINDS, or 20: without the kinds that came after those).  Meant for a single benchmarking thread; calls from
+ * entries; nkinds >= PRISM_PROFILE_KINDS, or 20 or 23: without the kinds that came after those).  Meant for a single benchmarking thread; calls from
  * other threads while it is enabled are recorded too (the record list is locked). */
-#define PRISM_PROFILE_KINDS 23
+#define PRISM_PROFILE_KINDS 31
 int prism_profile_enable(int on);
 int prism_profile_collect(double* ms_by_kind, long long* launches_by_kind, int nkinds);
 

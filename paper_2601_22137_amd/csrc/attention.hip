@@ -1,0 +1,220 @@
+// Attention: out = softmax(scores) v over the keys that a query sees, in one pass over the keys with the running maximum and sum of every row.
+//
+//   score(i, j) = cap tanh(scale q_i.k_j / cap) - slope |at_i - j|,  at_i = i + keys - n
+//
+// A workgroup takes 128 rows (32 per wave, on the lanes) of a pair and walks the keys in tiles that all four waves share in LDS, two of them in
+// flight.  Scores come out of the product K Q^T with a row per lane, so a row's maximum and sum are plain arithmetic in its own two lanes, and the
+// weights go from the registers straight into V^T P^T (attention_tile.h).
+#include "attention_tile.h"
+
+namespace prism {
+namespace {
+
+__global__ void __launch_bounds__(256) doc_range_kernel(const int* doc, int4* range, int len, int blocks, int batch) {
+  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (w >= (long long)blocks * batch) return;
+  const int b = (int)(w / blocks), i = (int)(w % blocks) * 64 + (threadIdx.x & 63);
+  const int d = i < len ? doc[(long long)b * len + i] : -1;
+  int lo = d < 0 ? 0x7FFFFFFF : d, hi = d, none = d < 0;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    lo = min(lo, __shfl_xor(lo, m));
+    hi = max(hi, __shfl_xor(hi, m));
+    none |= __shfl_xor(none, m);
+  }
+  if ((threadIdx.x & 63) == 0) range[w] = make_int4(lo, hi, none, 0);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn p) {
+  using L = Lds<T, DP>;
+  constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
+  __shared__ int kd[2][KT];
+  __shared__ int shared_range[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  int id = place(blockIdx.x, gridDim.x);
+  const int split = id % p.nsplit;
+  id /= p.nsplit;
+  const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
+  const Row w = row_of(p, b, kh, r, keys);
+  const Limits lim = limits_of(p, w, r);
+  int t0, t1;
+  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  Frag<T, DP> qf;
+  {
+    const int i = r / p.G, g = r - i * p.G;
+    load_row<T, DP>(qf, p.direct, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + (kh * p.G + g) * p.qs[2]);
+  }
+  const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
+  const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
+  auto issue = [&](int t, int buf) {
+    load_tile<T, DP, KT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? kbase + j * p.ks[1] : nullptr; });
+    load_tile<T, DP, KT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? vbase + j * p.vs[1] : nullptr; });
+    if (kdoc && tid < KT) kd[buf][tid] = t * KT + tid < keys ? kdoc[t * KT + tid] : -1;
+  };
+  f32x16 acc[DP / 32];
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) acc[t] = (f32x16){};
+  float m = -3.4e38f, l = 0.0f;   // the reference of the exponents, at most 8 below the row's maximum so far, and the lane's share of the sum
+  const bool cap = p.cap > 0.0f, bias = p.slopes != nullptr;
+  const float mul = cap || bias ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E;
+  if (t0 < t1) issue(t0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1, j0 = t * KT;
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1, buf ^ 1);
+    bool need;
+    if (!tile_seen<KT>(p, lim, b, t, need)) continue;
+    const char *kt = smem + buf * TB, *vt = smem + (2 + buf) * TB;
+    f32x16 s[KB];
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      s[kb] = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
+      scores<T>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
+      if (need) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int j = 8 * g + 4 * h + 32 * kb;
+          int4 d = make_int4(w.doc, w.doc, w.doc, w.doc);
+          if (kdoc) d = *(const int4*)&kd[buf][j];
+          const int dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[kb][4 * g + e] = j0 + j + e <= w.last && dd[e] == w.doc ? s[kb][4 * g + e] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+    }
+    top *= mul;
+    if (__any(top > m + 8.0f)) {
+      const float to = fmaxf(m, fmaxf(top, other_half(top))), f = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= f;
+#pragma unroll
+      for (int t2 = 0; t2 < DP / 32; ++t2)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t2][e] *= f;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[kb][e] = __builtin_amdgcn_exp2f(s[kb][e] * mul - m);
+        l += s[kb][e];
+      }
+      columns_by<T, DP>(acc, vt, 32 * kb, s[kb], lane);
+    }
+  }
+  l += other_half(l);
+  if (r >= p.R) return;
+  const int i = r / p.G, g = r - i * p.G;
+  if (p.nsplit == 1) {
+    store_row<T, DP>((T*)p.out + b * p.os[0] + i * p.os[1] + (kh * p.G + g) * p.os[2], acc, l == 0.0f ? 0.0f : 1.0f / l, p.dim, p.direct, h);
+    if (p.lse && h == 0) p.lse[((long long)b * p.hq + kh * p.G + g) * p.n + i] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / LOG2E);
+  } else {
+    const long long row = ((long long)split * p.batch * p.hk + pair) * p.R + r;
+    if (l != 0.0f) store_row<float, DP>(p.part + row * p.dim, acc, 1.0f, p.dim, p.direct, h);
+    if (h == 0) { p.part_ml[2 * row] = m; p.part_ml[2 * row + 1] = l; }
+  }
+}
+
+// The parts of a row's keys joined; a wave takes a row
+template <typename T> __global__ void __launch_bounds__(256) attention_join_kernel(Attn p) {
+  const long long rows = (long long)p.batch * p.hk * p.R, row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  float top = -3.4e38f, sum = 0.0f, o[2] = {0.0f, 0.0f};
+  for (int s = 0; s < p.nsplit; ++s) top = fmaxf(top, p.part_ml[2 * (s * rows + row)]);
+  for (int s = 0; s < p.nsplit; ++s) {
+    const float m = p.part_ml[2 * (s * rows + row)], l = p.part_ml[2 * (s * rows + row) + 1];
+    if (l == 0.0f) continue;                     // nothing was written for it
+    const float f = __builtin_amdgcn_exp2f(m - top);
+    sum += l * f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      if (lane + 64 * x < p.dim) o[x] += p.part[(s * rows + row) * p.dim + lane + 64 * x] * f;
+  }
+  const int pair = (int)(row / p.R), r = (int)(row - (long long)pair * p.R), b = pair / p.hk, kh = pair - b * p.hk, i = r / p.G, g = r - i * p.G;
+  T* to = (T*)p.out + b * p.os[0] + i * p.os[1] + (kh * p.G + g) * p.os[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+    if (lane + 64 * x < p.dim) to[lane + 64 * x] = (T)(sum == 0.0f ? 0.0f : o[x] / sum);
+  if (p.lse && lane == 0) p.lse[((long long)b * p.hq + kh * p.G + g) * p.n + i] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.0f / LOG2E);
+}
+
+template <typename T, int DP> int launch(Attn& p, hipStream_t s) {
+  constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
+  const int rc = allow_dynamic_lds((const void*)attention_kernel<T, DP>, bytes);
+  if (rc != PRISM_OK) return rc;
+  const long long rows = (long long)p.batch * p.hk * p.R;
+  {
+    ProfScope prof(PK_ATTENTION, s);
+    hipLaunchKernelGGL((attention_kernel<T, DP>), dim3((unsigned)p.batch * p.hk * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p);
+  }
+  if (p.nsplit > 1) {
+    ProfScope prof(PK_ATTENTION_JOIN, s);
+    hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
+  }
+  return PRISM_OK;
+}
+
+}  // namespace
+
+AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
+  AttnPlan a = {};
+  const long long pairs = (long long)d.batch * d.k_heads, R = (long long)(d.q_heads / d.k_heads) * d.q_len;
+  const int kt = dt == PRISM_F32 ? 32 : 64;
+  // Launches that leave CUs without work are cut along the other axis, into parts of four tiles at least.
+  auto parts = [](long long groups, long long tiles) {
+    if (groups == 0) return 1;
+    const long long want = 512 / groups, most = (tiles + 3) / 4;
+    const long long n = want < most ? want : most;
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+  };
+  a.split = parts(pairs * ((R + 127) / 128), (d.k_len + kt - 1) / kt);
+  a.split_dkv = backward ? parts(pairs * ((d.k_len + 127) / 128), (R + kt - 1) / kt) : 1;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at = (at + bytes + 255) & ~(size_t)255;
+    return o;
+  };
+  if (d.q_doc) take((size_t)d.batch * ((d.q_len + 63) / 64 + (d.k_len + 63) / 64) * sizeof(int4));
+  if (backward) a.o_stat = take((size_t)pairs * 2 * R * sizeof(float));
+  size_t part = a.split > 1 ? (size_t)a.split * pairs * R * d.head_dim * sizeof(float) : 0;
+  const size_t dkv = a.split_dkv > 1 ? (size_t)2 * a.split_dkv * pairs * d.k_len * d.head_dim * sizeof(float) : 0;
+  a.o_part = take(part > dkv ? part : dkv);
+  a.o_ml = take(a.split > 1 && !backward ? (size_t)a.split * pairs * R * 2 * sizeof(float) : 0);
+  a.total = at;
+  return a;
+}
+
+void launch_doc_ranges(const prism_attention_desc& d, int4* to, hipStream_t s) {
+  if (!d.q_doc) return;
+  const int bq = (d.q_len + 63) / 64, bk = (d.k_len + 63) / 64;
+  if (bq) hipLaunchKernelGGL(doc_range_kernel, dim3(((long long)bq * d.batch + 3) / 4), dim3(256), 0, s, d.q_doc, to, d.q_len, bq, d.batch);
+  if (bk) hipLaunchKernelGGL(doc_range_kernel, dim3(((long long)bk * d.batch + 3) / 4), dim3(256), 0, s, d.k_doc, to + (long long)bq * d.batch, d.k_len, bk, d.batch);
+}
+
+int launch_attention(const void* q, const void* k, const void* v, void* out, float* lse, int dt, const prism_attention_desc& d, char* ws, hipStream_t s) {
+  const AttnPlan plan = attention_plan(d, dt, false);
+  Attn p = attn_common(q, k, v, dt, d, ws);
+  launch_doc_ranges(d, (int4*)ws, s);
+  p.out = out;
+  p.lse = lse;
+  set_strides(p.os, d.out);
+  p.nsplit = plan.split;
+  p.part = (float*)(ws + plan.o_part);
+  p.part_ml = (float*)(ws + plan.o_ml);
+  p.direct = p.direct && rows_are_vectors(out, d.out, dt);
+  if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, s) : launch<float, 128>(p, s);
+  return d.head_dim <= 64 ? launch<__bf16, 64>(p, s) : launch<__bf16, 128>(p, s);
+}
+
+}  // namespace prism

@@ -1,0 +1,367 @@
+// Gradients of attention (attention.hip): with p = exp(score - lse), dp = dout.v and the row sums D = sum dout out
+//
+//   ds = p (dp - D) (1 - tanh^2) scale,   dq = ds k,   dk = ds^T q,   dv = p^T dout
+//
+// Two kernels that both compute the scores again: one walks the keys for 128 rows (dq), one the rows for 128 keys (dk, dv; all heads of the group, so
+// shared heads need no sum afterwards).  Seven products instead of five, but no sum across workgroups whose order could change the bits of dq.
+#include "attention_tile.h"
+
+namespace prism {
+namespace {
+
+// 1 - tanh^2 from a capped score (times log2 e, before its bias)
+__device__ inline float slope_of_cap(float capped, float per) {
+  const float t = capped * per;
+  return 1.0f - t * t;
+}
+
+// DELTA: stat[pair][0][r] = log2 of the row's sum of weights, +inf where the row sees nothing (its weights are then 0 everywhere), and stat[pair][1][r] = D.
+// Else: dq, with both.
+// D from the rounded `out` is off by 2^-9 of it, which shows where a row sees few keys (elsewhere in the mean over the keys it does not).  For workgroups
+// that see four tiles at most, bf16 therefore takes D = sum p dp.
+template <typename T, int DP, bool DELTA>
+__global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(Attn p, float* stat) {
+  using L = Lds<T, DP>;
+  constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
+  __shared__ int kd[2][KT];
+  __shared__ int shared_range[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  int id = place(blockIdx.x, gridDim.x);
+  const int split = id % p.nsplit;
+  id /= p.nsplit;
+  const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
+  const Row w = row_of(p, b, kh, r, keys);
+  const Limits lim = limits_of(p, w, r);
+  int t0, t1;
+  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  const int i = r / p.G, head = kh * p.G + r - i * p.G;
+  const bool any = w.last >= 0;
+  Frag<T, DP> qf, dof;
+  load_row<T, DP>(dof, p.direct, p.dim, h, any ? (const T*)p.dout + b * p.dos[0] + i * p.dos[1] + head * p.dos[2] : nullptr);
+  stat += (long long)pair * 2 * p.R;
+  float lse2 = INFINITY, delta = 0.0f;
+  if constexpr (DELTA) {
+    if (r < p.R) {
+      const float lse = p.lse_in[((long long)b * p.hq + head) * p.n + i];
+      if (lse != -INFINITY) lse2 = lse * LOG2E;
+      if (h == 0) stat[r] = lse2;
+    }
+    if (sizeof(T) == 4 || t1 - t0 > 4) {
+      Frag<T, DP> of;
+      load_row<T, DP>(of, p.direct, p.dim, h, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr);
+#pragma unroll
+      for (int s = 0; s < L::STEPS; ++s) {
+        union { u32x4 v; T e[L::EPC]; } x, y;
+        x.v = of[s];
+        y.v = dof[s];
+#pragma unroll
+        for (int e = 0; e < L::EPC; ++e) delta += (float)x.e[e] * (float)y.e[e];
+      }
+      t0 = t1;
+    }
+  } else if (r < p.R) {
+    lse2 = stat[r];
+    delta = stat[p.R + r];
+  }
+  load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
+  const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
+  const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
+  auto issue = [&](int t, int buf) {
+    load_tile<T, DP, KT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? kbase + j * p.ks[1] : nullptr; });
+    load_tile<T, DP, KT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? vbase + j * p.vs[1] : nullptr; });
+    if (kdoc && tid < KT) kd[buf][tid] = t * KT + tid < keys ? kdoc[t * KT + tid] : -1;
+  };
+  f32x16 acc[DP / 32];
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) acc[t] = (f32x16){};
+  const bool cap = p.cap > 0.0f, bias = p.slopes != nullptr;
+  const float mul = cap || bias ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E, per = cap ? 1.0f / out : 0.0f;
+  if (t0 < t1) issue(t0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1, j0 = t * KT;
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1, buf ^ 1);
+    bool need;
+    if (!tile_seen<KT>(p, lim, b, t, need)) continue;
+    const char *kt = smem + buf * TB, *vt = smem + (2 + buf) * TB;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      f32x16 s = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
+      f32x16 ds = rows_by_rows<T, DP>(vt, 32 * kb, dof, lane);
+      if (cap) scores<T>(p, s, w, 0, true, false, in, out);
+      f32x16 f = s;                                          // capped, not yet biased
+      if (bias) scores<T>(p, s, w, j0 + 32 * kb + 4 * h, false, true, cap ? 1.0f : in, out);
+      if (need) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int j = 8 * g + 4 * h + 32 * kb;
+          int4 d = make_int4(w.doc, w.doc, w.doc, w.doc);
+          if (kdoc) d = *(const int4*)&kd[buf][j];
+          const int dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] = j0 + j + e <= w.last && dd[e] == w.doc ? s[4 * g + e] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(s[e] * mul - lse2);
+        if constexpr (DELTA) {
+          delta += s[e] * ds[e];
+        } else {
+          ds[e] = s[e] * (ds[e] - delta);
+          if (cap) ds[e] *= slope_of_cap(f[e], per);
+        }
+      }
+      if constexpr (!DELTA) columns_by<T, DP>(acc, kt, 32 * kb, ds, lane);
+    }
+  }
+  if constexpr (DELTA) {
+    delta += other_half(delta);
+    if (r < p.R && h == 0) stat[p.R + r] = delta;
+    return;
+  }
+  if (r >= p.R) return;
+  if (p.nsplit == 1)
+    store_row<T, DP>((T*)p.dq + b * p.dqs[0] + i * p.dqs[1] + head * p.dqs[2], acc, p.scale, p.dim, p.direct, h);
+  else
+    store_row<float, DP>(p.part + (((long long)split * p.batch * p.hk + pair) * p.R + r) * p.dim, acc, p.scale, p.dim, p.direct, h);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const float* stat) {
+  using L = Lds<T, DP>;
+  constexpr int RT = key_tile<T>(), RBK = RT / 32, TB = RT * L::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each
+  __shared__ __attribute__((aligned(16))) float lse2[2][RT], delta[2][RT], slope[2][RT];
+  __shared__ __attribute__((aligned(16))) int last[2][RT], doc[2][RT], place_of[2][RT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const int key_tiles = (p.m + 127) / 128;
+  int id = place(blockIdx.x, gridDim.x);
+  const int split = id % p.nsplit;
+  id /= p.nsplit;
+  const int tile = id % key_tiles, pair = id / key_tiles, b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), j = tile * 128 + wave * 32 + (lane & 31), wave_j1 = tile * 128 + wave * 32 + 31;
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  int mydoc = j < keys ? 0 : -1;
+  if (kdoc && j < keys) mydoc = max(kdoc[j], -1);
+  // rows that may see one of the workgroup's keys
+  int i0 = 0, i1 = p.n;
+  if (p.causal && !(p.prefix && min(p.prefix[b], keys) > tile * 128)) i0 = max(0, tile * 128 - keys + p.n);
+  if (tile * 128 >= keys) i1 = 0;
+  int dlo = 0, dhi = 0;                    // the wave's documents
+  if (kdoc) {
+    dlo = mydoc < 0 ? 0x7FFFFFFF : mydoc;
+    dhi = mydoc;
+    int lo = 0x7FFFFFFF, hi = -1;
+    const int kblocks = (p.m + 63) / 64, qblocks = (p.n + 63) / 64;
+    for (int x = 2 * tile; x < min(2 * tile + 2, kblocks); ++x) {
+      const int4 k = p.krange[(long long)b * kblocks + x];
+      lo = min(lo, k.x);
+      hi = max(hi, k.y);
+    }
+    // the first and last block of 64 queries with one of them
+    int* sh = &last[0][0];
+    if (tid == 0) { sh[0] = 0x7FFFFFFF; sh[1] = -1; }
+    __syncthreads();
+    int f = 0x7FFFFFFF, e = -1;
+    for (int x = i0 / 64 + tid; x < qblocks; x += NT) {
+      const int4 k = p.qrange[(long long)b * qblocks + x];
+      if (k.x <= hi && k.y >= lo) { f = min(f, x); e = max(e, x); }
+    }
+    if (e >= 0) { atomicMin(&sh[0], f); atomicMax(&sh[1], e); }
+    __syncthreads();
+    if (sh[1] < 0) i1 = 0;
+    else {
+      i0 = max(i0, sh[0] * 64);
+      i1 = min(i1, (sh[1] + 1) * 64);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+      dlo = min(dlo, __shfl_xor(dlo, m));
+      dhi = max(dhi, __shfl_xor(dhi, m));
+    }
+    dlo = __builtin_amdgcn_readfirstlane(dlo);
+    dhi = __builtin_amdgcn_readfirstlane(dhi);
+  }
+  const bool keys_mixed = kdoc && (dlo != dhi || __any(mydoc < 0));
+  const int first_tile = i0 * p.G / RT, end_tile = i0 < i1 ? (i1 * p.G + RT - 1) / RT : first_tile;
+  const int per = (max(end_tile - first_tile, 0) + p.nsplit - 1) / p.nsplit;
+  const int t0 = __builtin_amdgcn_readfirstlane(first_tile + split * per), t1 = __builtin_amdgcn_readfirstlane(min(end_tile, first_tile + (split + 1) * per));
+  Frag<T, DP> kf, vf;
+  load_row<T, DP>(kf, p.direct, p.dim, h, mydoc < 0 ? nullptr : (const T*)p.k + b * p.ks[0] + j * p.ks[1] + kh * p.ks[2]);
+  load_row<T, DP>(vf, p.direct, p.dim, h, mydoc < 0 ? nullptr : (const T*)p.v + b * p.vs[0] + j * p.vs[1] + kh * p.vs[2]);
+  const T* qbase = (const T*)p.q + b * p.qs[0] + kh * p.G * p.qs[2];
+  const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
+  const float* st = stat + (long long)pair * 2 * p.R;
+  auto issue = [&](int t, int buf) {
+    auto at = [&](int x, const T* base, const long long (&s)[3]) -> const T* {
+      const int r = t * RT + x, i = r / p.G, g = r - i * p.G;
+      return r < p.R && st[r] != INFINITY ? base + i * s[1] + g * s[2] : nullptr;
+    };
+    load_tile<T, DP, RT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { return at(x, qbase, p.qs); });
+    load_tile<T, DP, RT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { return at(x, dobase, p.dos); });
+    if (tid < RT) {
+      const int r = t * RT + tid;
+      const Row w = row_of(p, b, kh, r, keys);
+      lse2[buf][tid] = r < p.R ? st[r] : INFINITY;
+      delta[buf][tid] = r < p.R ? st[p.R + r] : 0.0f;
+      last[buf][tid] = w.last;
+      doc[buf][tid] = w.doc;
+      place_of[buf][tid] = w.at;
+      slope[buf][tid] = w.slope;
+    }
+  };
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) { dk[t] = (f32x16){}; dv[t] = (f32x16){}; }
+  const bool cap = p.cap > 0.0f, bias = p.slopes != nullptr;
+  const float mul = cap || bias ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E, per_cap = cap ? 1.0f / out : 0.0f;
+  if (t0 < t1) issue(t0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1, buf ^ 1);
+    // Rows that see nothing have lse2 = +inf and need no mask.  The keys that a row sees grow with its token: the tile's first row says whether all see all.
+    const Row first = row_of(p, b, kh, t * RT, keys);
+    bool need = kdoc || first.last < wave_j1;
+    if (kdoc && !keys_mixed && first.last >= wave_j1) {
+      const int qblocks = (p.n + 63) / 64, x0 = t * RT / p.G / 64, x1 = min(t * RT + RT - 1, p.R - 1) / p.G / 64;
+      const int4 a = p.qrange[(long long)b * qblocks + x0], c = p.qrange[(long long)b * qblocks + x1];
+      need = !(a.x == dlo && a.y == dlo && c.x == dlo && c.y == dlo);
+    }
+    const char *qt = smem + buf * TB, *dot = smem + (2 + buf) * TB;
+#pragma unroll
+    for (int rb = 0; rb < RBK; ++rb) {
+      f32x16 s = rows_by_rows<T, DP>(qt, 32 * rb, kf, lane);
+      f32x16 f;
+      if (cap) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[e] = out * tanh_of(s[e] * in, sizeof(T) == 4);
+          f[e] = slope_of_cap(s[e], per_cap);
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int x = 32 * rb + 8 * g + 4 * h;
+        const f32x4 ls = *(const f32x4*)&lse2[buf][x];
+        if (bias) {
+          const f32x4 sl = *(const f32x4*)&slope[buf][x];
+          const int4 pl = *(const int4*)&place_of[buf][x];
+          const int pp[4] = {pl.x, pl.y, pl.z, pl.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] = s[4 * g + e] * (cap ? 1.0f : in) - sl[e] * fabsf((float)(pp[e] - j));
+        }
+        if (need) {
+          const int4 la = *(const int4*)&last[buf][x], d4 = *(const int4*)&doc[buf][x];
+          const int ll[4] = {la.x, la.y, la.z, la.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] = j <= ll[e] && dd[e] == mydoc ? s[4 * g + e] : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(s[4 * g + e] * mul - ls[e]);
+      }
+      columns_by<T, DP>(dv, dot, 32 * rb, s, lane);
+      f32x16 dp = rows_by_rows<T, DP>(dot, 32 * rb, vf, lane);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 de = *(const f32x4*)&delta[buf][32 * rb + 8 * g + 4 * h];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          dp[4 * g + e] = s[4 * g + e] * (dp[4 * g + e] - de[e]);
+          if (cap) dp[4 * g + e] *= f[4 * g + e];
+        }
+      }
+      columns_by<T, DP>(dk, qt, 32 * rb, dp, lane);
+    }
+  }
+  if (j >= p.m) return;
+  if (p.nsplit == 1) {
+    store_row<T, DP>((T*)p.dk + b * p.dks[0] + j * p.dks[1] + kh * p.dks[2], dk, p.scale, p.dim, p.direct, h);
+    store_row<T, DP>((T*)p.dv + b * p.dvs[0] + j * p.dvs[1] + kh * p.dvs[2], dv, 1.0f, p.dim, p.direct, h);
+  } else {
+    const long long pairs = (long long)p.batch * p.hk, row = (split * pairs + pair) * p.m + j;
+    store_row<float, DP>(p.part + row * p.dim, dk, p.scale, p.dim, p.direct, h);
+    store_row<float, DP>(p.part + (p.nsplit * pairs * p.m + row) * p.dim, dv, 1.0f, p.dim, p.direct, h);
+  }
+}
+
+// to[pair][row] = the sum of the parts, in their order; row -> (token, head) as row / G and row % G
+template <typename T>
+__global__ void __launch_bounds__(256) attention_sum_kernel(const float* part, int nsplit, T* to, long long s0, long long s1, long long s2, int hk, int G, int R, int dim, long long total) {
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  float v = 0.0f;
+  for (int s = 0; s < nsplit; ++s) v += part[s * total + at];
+  const long long row = at / dim;
+  const int d = (int)(at - row * dim), pair = (int)(row / R), r = (int)(row - (long long)pair * R), b = pair / hk, kh = pair - b * hk, i = r / G;
+  to[b * s0 + i * s1 + (kh * G + r - i * G) * s2 + d] = (T)v;
+}
+
+template <typename T> void join(const float* part, int nsplit, void* to, const long long (&st)[3], int batch, int hk, int G, int R, int dim, hipStream_t s) {
+  const long long total = (long long)batch * hk * R * dim;
+  hipLaunchKernelGGL((attention_sum_kernel<T>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, part, nsplit, (T*)to, st[0], st[1], st[2], hk, G, R, dim, total);
+}
+
+template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* stat, hipStream_t s) {
+  constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
+  int rc = allow_dynamic_lds((const void*)attention_dq_kernel<T, DP, true>, bytes);
+  if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)attention_dq_kernel<T, DP, false>, bytes);
+  if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)attention_dkv_kernel<T, DP>, bytes);
+  if (rc != PRISM_OK) return rc;
+  const unsigned pairs = (unsigned)p.batch * p.hk;
+  p.nsplit = 1;
+  if (p.R > 0) {
+    ProfScope prof(PK_ATTENTION_STAT, s);
+    hipLaunchKernelGGL((attention_dq_kernel<T, DP, true>), dim3(pairs * p.row_tiles), dim3(NT), bytes, s, p, stat);
+  }
+  p.nsplit = plan.split;
+  if (p.R > 0) {
+    ProfScope prof(PK_ATTENTION_DQ, s);
+    hipLaunchKernelGGL((attention_dq_kernel<T, DP, false>), dim3(pairs * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p, stat);
+  }
+  if (p.nsplit > 1 && p.R > 0) {
+    ProfScope prof(PK_ATTENTION_JOIN, s);
+    join<T>(p.part, p.nsplit, p.dq, p.dqs, p.batch, p.hk, p.G, p.R, p.dim, s);
+  }
+  if (p.m == 0) return PRISM_OK;
+  p.nsplit = plan.split_dkv;
+  {
+    ProfScope prof(PK_ATTENTION_DKV, s);
+    hipLaunchKernelGGL((attention_dkv_kernel<T, DP>), dim3(pairs * ((p.m + 127) / 128) * p.nsplit), dim3(NT), bytes, s, p, (const float*)stat);
+  }
+  if (p.nsplit > 1) {
+    ProfScope prof(PK_ATTENTION_JOIN, s);
+    join<T>(p.part, p.nsplit, p.dk, p.dks, p.batch, p.hk, 1, p.m, p.dim, s);
+    join<T>(p.part + (long long)p.nsplit * pairs * p.m * p.dim, p.nsplit, p.dv, p.dvs, p.batch, p.hk, 1, p.m, p.dim, s);
+  }
+  return PRISM_OK;
+}
+
+}  // namespace
+
+int launch_attention_backward(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, void* dq, void* dk,
+                              void* dv, int dt, const prism_attention_desc& d, char* ws, hipStream_t s) {
+  const AttnPlan plan = attention_plan(d, dt, true);
+  Attn p = attn_common(q, k, v, dt, d, ws);
+  launch_doc_ranges(d, (int4*)ws, s);
+  p.o = out; p.dout = dout; p.lse_in = lse;
+  p.dq = dq; p.dk = dk; p.dv = dv;
+  set_strides(p.os, d.out); set_strides(p.dos, d.dout);
+  set_strides(p.dqs, d.dq); set_strides(p.dks, d.dk); set_strides(p.dvs, d.dv);
+  p.part = (float*)(ws + plan.o_part);
+  p.direct = p.direct && rows_are_vectors(out, d.out, dt) && rows_are_vectors(dout, d.dout, dt) && rows_are_vectors(dq, d.dq, dt) &&
+             rows_are_vectors(dk, d.dk, dt) && rows_are_vectors(dv, d.dv, dt);
+  float* stat = (float*)(ws + plan.o_stat);
+  if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, plan, stat, s) : launch<float, 128>(p, plan, stat, s);
+  return d.head_dim <= 64 ? launch<__bf16, 64>(p, plan, stat, s) : launch<__bf16, 128>(p, plan, stat, s);
+}
+
+}  // namespace prism

@@ -394,6 +394,8 @@ enum ProfKind {
   PK_FIT_SQUARE,     // the fit and R^2 in one launch
   PK_FLOW,           // all iterations in one launch
   PK_SMALL_ROOT,     // inverse roots of padded order 64, whole calls
+  PK_DROPOUT, PK_NORM_ROPE, PK_NORM_ROPE_BACKWARD,
+  PK_ATTENTION, PK_ATTENTION_JOIN, PK_ATTENTION_STAT, PK_ATTENTION_DQ, PK_ATTENTION_DKV,
   PK_COUNT
 };
 struct ProfScope {   // records an event pair around the launches made during its lifetime

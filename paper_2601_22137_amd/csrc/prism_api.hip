@@ -13,6 +13,7 @@
 #include <utility>
 
 #include "common.h"
+#include "layer.h"
 #include "workspace_cache.h"
 
 namespace prism {
@@ -368,6 +369,19 @@ int get_workspace(size_t bytes, const void* owner, const prism_options* opt, cha
   *out = (char*)p;
   return PRISM_OK;
 }
+
+}  // namespace
+
+int layer_workspace(size_t bytes, void* given, size_t given_bytes, hipStream_t s, char** out) {
+  prism_options opt = {};
+  opt.workspace = given;
+  opt.workspace_bytes = given_bytes;
+  const int rc = get_workspace(bytes, s, &opt, out);
+  if (rc == PRISM_ENOMEM && given) set_last_error("the workspace is too small or not aligned to 256 bytes");
+  return rc;
+}
+
+namespace {
 
 #define CHECK_LAUNCH(expr)                         \
   do {                                             \
@@ -1774,7 +1788,7 @@ int prism_profile_enable(int on) {
 }
 
 int prism_profile_collect(double* ms_by_kind, long long* launches_by_kind, int nkinds) {
-  if (!ms_by_kind || !launches_by_kind || (nkinds < PK_COUNT && nkinds != PK_FIT_SQUARE)) return PRISM_EINVAL;   // (that many: see prism.h)
+  if (!ms_by_kind || !launches_by_kind || (nkinds < PK_COUNT && nkinds != PK_FIT_SQUARE && nkinds != PK_DROPOUT)) return PRISM_EINVAL;   // (these: see prism.h)
   std::lock_guard<std::mutex> lock(g_prof_mu);
   for (int i = 0; i < nkinds; ++i) { ms_by_kind[i] = 0.0; launches_by_kind[i] = 0; }
   for (auto& r : g_prof) {

@@ -9,31 +9,12 @@
 // rounded once; this file must be compiled with floating-point contraction off so that no
 // multiply-add pair is fused.  That makes the stream reproducible bit for bit on any machine.
 #include "common.h"
+#include "philox.h"
 
 #pragma clang fp contract(off)
 
 namespace prism {
 namespace {
-
-struct U4 { unsigned int x, y, z, w; };
-
-__device__ inline U4 philox4x32_10(U4 c, unsigned int k0, unsigned int k1) {
-  const unsigned int M0 = 0xD2511F53u, M1 = 0xCD9E8D57u, W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    const unsigned int hi0 = __umulhi(M0, c.x), lo0 = M0 * c.x;
-    const unsigned int hi1 = __umulhi(M1, c.z), lo1 = M1 * c.z;
-    U4 n;
-    n.x = hi1 ^ c.y ^ k0;
-    n.y = lo1;
-    n.z = hi0 ^ c.w ^ k1;
-    n.w = lo0;
-    c = n;
-    k0 += W0;
-    k1 += W1;
-  }
-  return c;
-}
 
 // sqrt(-2 ln(a 2^-24)), a in [1, 2^24]
 __device__ inline double bm_radius(unsigned int a) {

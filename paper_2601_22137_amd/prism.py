@@ -27,13 +27,16 @@ INFO_DTYPE = np.dtype([("iters", np.int32), ("status", np.int32),
 
 EXPORTS = ("prism_workspace_bytes", "prism_release_workspaces", "prism_polar", "prism_polar_ex", "prism_polar_static", "prism_sqrt", "prism_sqrt_ex",
            "prism_inv_root", "prism_inv_root_ex", "prism_sign", "prism_sign_ex", "prism_inverse", "prism_inverse_ex", "prism_sqrt_newton", "prism_sqrt_newton_ex", "prism_spd_inverse", "prism_run_grouped", "prism_run_grouped_from",
+           "prism_dropout", "prism_qk_norm_rope", "prism_qk_norm_rope_backward", "prism_norm_rope_workspace_bytes",
+           "prism_attention", "prism_attention_backward", "prism_attention_workspace_bytes",
            "prism_sketch", "prism_gauss_parts", "prism_chain_product", "prism_chain_product_bf16", "prism_gemm_f32", "prism_gemm_f32_planes",
            "prism_gemm_f64a", "prism_gemm_bf16_nt", "prism_profile_enable", "prism_profile_collect",
            "prism_last_error")
 
 PROFILE_KINDS = ("prep", "final", "sketch", "chain", "solve", "f32_resid", "f32_polyq", "f32_apply", "f32_store",
                  "f64_mnext", "make_t", "bf16_gram", "bf16_polyq", "bf16_apply", "bf16_store", "spd_inverse", "db_moments",
-                 "db_update_m", "f32_small_polar", "moments", "fit_square", "flow", "small_root")
+                 "db_update_m", "f32_small_polar", "moments", "fit_square", "flow", "small_root",
+                 "dropout", "norm_rope", "norm_rope_backward", "attention", "attention_join", "attention_stat", "attention_dq", "attention_dkv")
 
 
 class Options(ctypes.Structure):
@@ -45,6 +48,26 @@ class Options(ctypes.Structure):
 class Group(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("inv_out", ctypes.c_void_p), ("info", ctypes.c_void_p),
                 ("batch", ctypes.c_int32), ("m", ctypes.c_int32), ("n", ctypes.c_int32)]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class NormRopeDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("batch", "len", "q_heads", "k_heads", "head_dim", "rot_dim", "norm", "interleaved", "start")]
+                + [("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+                + [(f, ctypes.c_void_p) for f in ("positions", "inv_freq", "q_weight", "k_weight")]
+                + [(f, Strides) for f in ("q", "k", "q_out", "k_out", "dq", "dk")]
+                + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("batch", "q_len", "k_len", "q_heads", "k_heads", "head_dim", "causal")]
+                + [("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+                + [(f, ctypes.c_void_p) for f in ("slopes", "prefix", "k_lens", "q_doc", "k_doc")]
+                + [(f, Strides) for f in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+                + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
 
 
 class PrismError(RuntimeError):
@@ -79,6 +102,13 @@ def lib():
         L.prism_spd_inverse.argtypes = [vp, vp, i, i, vp]
         L.prism_run_grouped.argtypes = [i, ctypes.POINTER(Group), i, i, i, i, i, i, u64, dbl, vp, ctypes.POINTER(Options)]
         L.prism_run_grouped_from.argtypes = [i, ctypes.POINTER(Group), vp, i, i, i, i, i, i, u64, dbl, vp, ctypes.POINTER(Options)]
+        L.prism_dropout.argtypes = [vp, vp, vp, ctypes.c_int64, i, dbl, u64, ctypes.c_uint32, vp]
+        L.prism_qk_norm_rope.argtypes = [vp, vp, vp, vp, i, ctypes.POINTER(NormRopeDesc), vp]
+        L.prism_qk_norm_rope_backward.argtypes = [vp] * 8 + [i, ctypes.POINTER(NormRopeDesc), vp]
+        L.prism_norm_rope_workspace_bytes.argtypes = [i, ctypes.POINTER(NormRopeDesc), ctypes.POINTER(ctypes.c_size_t)]
+        L.prism_attention.argtypes = [vp] * 5 + [i, ctypes.POINTER(AttentionDesc), vp]
+        L.prism_attention_backward.argtypes = [vp] * 9 + [i, ctypes.POINTER(AttentionDesc), vp]
+        L.prism_attention_workspace_bytes.argtypes = [i, ctypes.POINTER(AttentionDesc), i, ctypes.POINTER(ctypes.c_size_t)]
         L.prism_sketch.argtypes = [vp, i, i, u64, i, i, vp]
         L.prism_gauss_parts.argtypes = [ctypes.c_uint32, ctypes.c_uint32, vp, vp, vp, vp]
         L.prism_chain_product.argtypes = [vp, vp, vp, i, i, i, vp]
@@ -290,6 +320,205 @@ def read_reports(infos):
         out.append(whole[at:at + h.buf.numel()].view(INFO_DTYPE).copy())
         at += h.buf.numel()
     return out
+
+
+# ---- operators of a transformer layer ----
+#
+# Arrays of heads are tensors [batch, token, head, dim]; dim has to be contiguous, the other strides are free (views into one
+# projection, transposed views).
+
+def _same(ref, *ts):
+    """Each t (None excepted) a CUDA tensor on ref's device."""
+    for t in ts:
+        if t is not None and not (t.is_cuda and t.device == ref.device):
+            raise PrismError("expected CUDA tensors on one device")
+
+
+def _heads(t, name, dtype, shape=None):
+    if t.dim() != 4 or t.dtype != dtype or (t.numel() > 0 and t.shape[3] > 1 and t.stride(3) != 1) or any(s < 0 for s in t.stride()):
+        raise PrismError("%s: expected [batch, token, head, dim] of one dtype with contiguous dim" % name)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise PrismError("%s: expected shape %s" % (name, tuple(shape)))
+    return t
+
+
+def _strides(t):
+    return Strides(t.stride(0), t.stride(1), t.stride(2)) if t is not None else Strides(0, 0, 0)
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _plain(t, name, dtype, shape):
+    """The pointer of an optional contiguous array."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise PrismError("%s: expected a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
+    return t.data_ptr()
+
+
+def _stream_of(t):
+    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def dropout(x, p, seed, offset=0, residual=None, out=None):
+    """residual + dropout(x): every element is kept with probability 1 - p (rounded to 16 bits) and then divided by it.  The mask is a function
+    of (seed, offset, index) and is not stored: the gradient with respect to x is dropout(dy, p, seed, offset).  out may be x or residual."""
+    y = torch.empty_like(x) if out is None else out
+    _same(x, x, residual, y)
+    if any(t is not None and (t.shape != x.shape or t.dtype != x.dtype or not t.is_contiguous()) for t in (x, residual, y)):
+        raise PrismError("expected contiguous tensors of one shape and dtype")
+    with torch.cuda.device(x.device):
+        _check(lib().prism_dropout(x.data_ptr(), _ptr(residual), y.data_ptr(), x.numel(), _dtype_code(x), p, seed, offset, _stream_of(x)))
+    return y
+
+
+def rope_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_len=None, fast=32.0, slow=1.0, device=None):
+    """(inv_freq, scale) for qk_norm_rope: base^(-2i / rot_dim), for contexts `factor` times longer than trained on
+       "linear"    every frequency divided by factor
+       "base"      a larger base, so that the lowest frequency is divided by factor and the highest kept
+       "by_turns"  frequencies that turn less than `slow` times in original_len divided by factor, more than `fast` times kept, a ramp
+                   between; the rotated part is scaled by 0.1 ln(factor) + 1."""
+    if rot_dim < 2 or rot_dim % 2 or not factor > 0:
+        raise PrismError("rot_dim has to be even and positive, factor positive")
+    half = rot_dim // 2
+    if scaling == "base":
+        base = base * factor ** (rot_dim / (rot_dim - 2)) if rot_dim > 2 else base
+    f = base ** (-np.arange(half) / half)
+    scale = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "by_turns":
+        if not original_len:
+            raise PrismError("by_turns needs original_len")
+        keep = np.clip((original_len * f / (2 * np.pi) - slow) / (fast - slow), 0.0, 1.0)
+        f = f * keep + f / factor * (1.0 - keep)
+        scale = 0.1 * np.log(factor) + 1.0 if factor > 1.0 else 1.0
+    elif scaling not in (None, "base"):
+        raise PrismError("unknown scaling %r" % (scaling,))
+    return torch.tensor(f, dtype=torch.float32, device=device), float(scale)
+
+
+def _norm_rope_desc(q, k, positions, start, inv_freq, q_weight, k_weight, norm, interleaved, scale, eps):
+    some = q if q is not None else k
+    if some is None:
+        raise PrismError("expected queries or keys")
+    _same(some, q, k, positions, inv_freq, q_weight, k_weight)
+    if some.dim() != 4:
+        raise PrismError("expected [batch, token, head, dim]")
+    b, n, _, d = some.shape
+    o = NormRopeDesc()
+    o.batch, o.len, o.head_dim = b, n, d
+    for t, name in ((q, "q"), (k, "k")):
+        if t is not None:
+            _heads(t, name, some.dtype, (b, n, t.shape[2] if t.dim() == 4 else 0, d))
+            setattr(o, name + "_heads", t.shape[2])
+            setattr(o, name, _strides(t))
+    o.rot_dim = 2 * inv_freq.numel() if inv_freq is not None else 0
+    o.norm, o.interleaved, o.start, o.eps, o.scale = int(bool(norm)), int(bool(interleaved)), start, eps, scale
+    o.positions = _plain(positions, "positions", torch.int32, (b, n))
+    o.inv_freq = _plain(inv_freq, "inv_freq", torch.float32, (o.rot_dim // 2,))
+    o.q_weight = _plain(q_weight, "q_weight", torch.float32, (d,))
+    o.k_weight = _plain(k_weight, "k_weight", torch.float32, (d,))
+    return some, o
+
+
+def qk_norm_rope(q, k, inv_freq=None, positions=None, start=0, q_weight=None, k_weight=None, norm=True, interleaved=False, scale=1.0, eps=1e-6,
+                 out=None):
+    """RMS norm of every head of q and k [batch, token, head, dim] times q_weight / k_weight (fp32 [dim], None: ones), then the rotation of
+    its first 2 * len(inv_freq) entries by positions (int32 [batch, token], None: from `start` on).  norm=False: rotation only; inv_freq=None: norm only.
+    q or k may be None.  out: the tensors for the results (q and k themselves are allowed).  Returns (q, k)."""
+    some, o = _norm_rope_desc(q, k, positions, start, inv_freq, q_weight, k_weight, norm, interleaved, scale, eps)
+    qo, ko = out if out is not None else tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) if t is not None else None for t in (q, k))
+    _same(some, qo, ko)
+    for t, to, name in ((q, qo, "q_out"), (k, ko, "k_out")):
+        if (t is None) != (to is None):
+            raise PrismError("%s: results go with inputs" % name)
+        if to is not None:
+            _heads(to, name, some.dtype, t.shape)
+            setattr(o, name, _strides(to))
+    with torch.cuda.device(some.device):
+        _check(lib().prism_qk_norm_rope(_ptr(q), _ptr(k), _ptr(qo), _ptr(ko), _dtype_code(some), ctypes.byref(o), _stream_of(some)))
+    return qo, ko
+
+
+def qk_norm_rope_backward(dq_out, dk_out, q, k, inv_freq=None, positions=None, start=0, q_weight=None, k_weight=None, norm=True, interleaved=False,
+                          scale=1.0, eps=1e-6, out=None, workspace=None):
+    """Gradients of qk_norm_rope from those of its results: (dq, dk, dq_weight, dk_weight), the last two fp32 [dim], or None without the norm.
+    q and k are the inputs of the forward call.  out: tensors for dq and dk."""
+    some, o = _norm_rope_desc(q, k, positions, start, inv_freq, q_weight, k_weight, norm, interleaved, scale, eps)
+    dq, dk = out if out is not None else tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) if t is not None else None for t in (q, k))
+    _same(some, dq_out, dk_out, dq, dk, workspace)
+    weights = [None, None]
+    for x, (t, g, to, name) in enumerate(((q, dq_out, dq, "q"), (k, dk_out, dk, "k"))):
+        if (t is None) != (to is None) or (t is None) != (g is None):
+            raise PrismError("%s: gradients go with inputs" % name)
+        if t is not None:
+            setattr(o, name + "_out", _strides(_heads(g, "d%s_out" % name, some.dtype, t.shape)))
+            setattr(o, "d" + name, _strides(_heads(to, "d" + name, some.dtype, t.shape)))
+            if norm:
+                weights[x] = (torch.zeros if t.numel() == 0 else torch.empty)(t.shape[3], dtype=torch.float32, device=t.device)
+    if workspace is not None:
+        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    with torch.cuda.device(some.device):
+        _check(lib().prism_qk_norm_rope_backward(_ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(dq), _ptr(dk), _ptr(weights[0]), _ptr(weights[1]),
+                                                 _dtype_code(some), ctypes.byref(o), _stream_of(some)))
+    return dq, dk, weights[0], weights[1]
+
+
+def _attention_desc(q, k, v, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace):
+    _same(q, q, k, v, slopes, prefix, k_lens, q_doc, k_doc, workspace)
+    _heads(q, "q", q.dtype)
+    b, n, hq, d = q.shape
+    _heads(k, "k", q.dtype)
+    m, hk = k.shape[1], k.shape[2]
+    _heads(k, "k", q.dtype, (b, m, hk, d))
+    _heads(v, "v", q.dtype, (b, m, hk, d))
+    o = AttentionDesc()
+    o.batch, o.q_len, o.k_len, o.q_heads, o.k_heads, o.head_dim = b, n, m, hq, hk, d
+    o.causal, o.softcap, o.scale = int(bool(causal)), softcap, d ** -0.5 if scale is None else scale
+    o.slopes = _plain(slopes, "slopes", torch.float32, (hq,))
+    o.prefix = _plain(prefix, "prefix", torch.int32, (b,))
+    o.k_lens = _plain(k_lens, "k_lens", torch.int32, (b,))
+    o.q_doc = _plain(q_doc, "q_doc", torch.int32, (b, n))
+    o.k_doc = _plain(k_doc, "k_doc", torch.int32, (b, m))
+    o.q, o.k, o.v = _strides(q), _strides(k), _strides(v)
+    if workspace is not None:
+        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return o
+
+
+def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, out=None, workspace=None):
+    """Attention of q [batch, n, q_heads, dim] over k and v [batch, m, k_heads, dim].  scores = scale q.k (scale None: dim^-1/2), capped by softcap tanh(. / softcap),
+    less slopes[head] * distance.  Masks: causal (the last query sits at the last key), prefix [batch] (keys that all see), k_lens [batch] (keys there are), q_doc / k_doc
+    [batch, n] / [batch, m] (documents; negative: padding).  Returns (out, lse); a query that sees nothing gets 0 and -inf."""
+    o = _attention_desc(q, k, v, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace)
+    b, n, hq, d = q.shape
+    y = torch.empty((b, n, hq, d), dtype=q.dtype, device=q.device) if out is None else out
+    _same(q, y)
+    o.out = _strides(_heads(y, "out", q.dtype, q.shape))
+    lse = torch.empty((b, hq, n), dtype=torch.float32, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(lib().prism_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), y.data_ptr(), lse.data_ptr(), _dtype_code(q), ctypes.byref(o), _stream_of(q)))
+    return y, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None,
+                       grads=None, workspace=None):
+    """(dq, dk, dv) from dout; out and lse as attention() returned them for the same arguments.  grads: tensors for the three results."""
+    o = _attention_desc(q, k, v, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace)
+    make = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)   # noqa: E731
+    dq, dk, dv = grads if grads is not None else (make(q), make(k), make(v))
+    _same(q, dout, out, lse, dq, dk, dv)
+    o.out, o.dout = _strides(_heads(out, "out", q.dtype, q.shape)), _strides(_heads(dout, "dout", q.dtype, q.shape))
+    o.dq, o.dk, o.dv = _strides(_heads(dq, "dq", q.dtype, q.shape)), _strides(_heads(dk, "dk", q.dtype, k.shape)), _strides(_heads(dv, "dv", q.dtype, v.shape))
+    _plain(lse, "lse", torch.float32, (q.shape[0], q.shape[2], q.shape[1]))
+    with torch.cuda.device(q.device):
+        _check(lib().prism_attention_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), dq.data_ptr(),
+                                              dk.data_ptr(), dv.data_ptr(), _dtype_code(q), ctypes.byref(o), _stream_of(q)))
+    return dq, dk, dv
 
 
 # ---- single steps (unit tests, profiling) ----
