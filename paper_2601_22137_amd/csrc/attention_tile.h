@@ -45,12 +45,13 @@ struct Attn {
 __device__ const unsigned zero_page[4] = {0, 0, 0, 0};
 
 // Tiles of rows of DP elements in LDS (the head size rounded up to 64 or 128; entries past it are zero), in chunks of 16 bytes.  Chunk c of row r lies at c ^ swizzle(r):
-// both the reads of 16 rows at one chunk (the operand as it is) and those of 4 rows at two chunks (the transposed one) then fall on different banks.
+// the reads of 16 rows at one chunk (the operand as it is), of 4 rows at four chunks (the transposed one, bf16) and of two rows four apart (fp32) then fall on different banks.
 template <typename T, int DP> struct Lds {
   static constexpr int RB = DP * (int)sizeof(T), CPR = RB / 16, EPC = 16 / (int)sizeof(T), STEPS = CPR / 2;
   __device__ static int swizzle(int r) {
-    if constexpr (CPR == 8) return ((r >> 3) & 1) | ((r >> 1) & 1) << 1 | ((r >> 2) & 1) << 2;
-    else return ((r >> 2) & 1) | (r & 1) << 1 | ((r >> 1) & 1) << 2 | (r & 8);
+    if constexpr (CPR == 8) return ((r >> 2) & 3) | ((r >> 1) & 1) << 2;
+    else if constexpr (sizeof(T) == 2) return ((r >> 2) & 3) | (r & 3) << 2;
+    else return (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3;
   }
 };
 
