@@ -25,6 +25,20 @@ __global__ void __launch_bounds__(256) doc_range_kernel(const int* doc, int4* ra
   if ((threadIdx.x & 63) == 0) range[w] = make_int4(lo, hi, none, 0);
 }
 
+// The row's result, or what this part of its keys has of it
+template <typename T, int DP>
+__device__ inline void finish(const Attn& p, const f32x16 (&acc)[DP / 32], float m, float l, int split, int pair, int b, int i, int head, int r, int h) {
+  if (r >= p.R) return;
+  if (p.nsplit == 1) {
+    store_row<T, DP>((T*)p.out + b * p.os[0] + i * p.os[1] + head * p.os[2], acc, l == 0.0f ? 0.0f : 1.0f / l, p.dim, p.direct, h);
+    if (p.lse && h == 0) p.lse[((long long)b * p.hq + head) * p.n + i] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / LOG2E);
+  } else {
+    const long long row = ((long long)split * p.batch * p.hk + pair) * p.R + r;
+    if (l != 0.0f) store_row<float, DP>(p.part + row * p.dim, acc, 1.0f, p.dim, p.direct, h);
+    if (h == 0) { p.part_ml[2 * row] = m; p.part_ml[2 * row + 1] = l; }
+  }
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn p) {
   using L = Lds<T, DP>;
@@ -43,10 +57,8 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
   int t0, t1;
   key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
   Frag<T, DP> qf;
-  {
-    const int i = r / p.G, g = r - i * p.G;
-    load_row<T, DP>(qf, p.direct, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + (kh * p.G + g) * p.qs[2]);
-  }
+  const int i = r / p.G, head = kh * p.G + r - i * p.G;
+  load_row<T, DP>(qf, p.direct, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2]);
   const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
@@ -89,7 +101,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
         }
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+      for (int e = 0; e < 16; ++e) top = max_of(top, s[kb][e]);
     }
     top *= mul;
     if (__any(top > m + 8.0f)) {
@@ -112,16 +124,214 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
     }
   }
   l += other_half(l);
-  if (r >= p.R) return;
-  const int i = r / p.G, g = r - i * p.G;
-  if (p.nsplit == 1) {
-    store_row<T, DP>((T*)p.out + b * p.os[0] + i * p.os[1] + (kh * p.G + g) * p.os[2], acc, l == 0.0f ? 0.0f : 1.0f / l, p.dim, p.direct, h);
-    if (p.lse && h == 0) p.lse[((long long)b * p.hq + kh * p.G + g) * p.n + i] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / LOG2E);
-  } else {
-    const long long row = ((long long)split * p.batch * p.hk + pair) * p.R + r;
-    if (l != 0.0f) store_row<float, DP>(p.part + row * p.dim, acc, 1.0f, p.dim, p.direct, h);
-    if (h == 0) { p.part_ml[2 * row] = m; p.part_ml[2 * row + 1] = l; }
+  finish<T, DP>(p, acc, m, l, split, pair, b, i, head, r, h);
+}
+
+// The same for bf16, with the work of neighbouring tiles interleaved: while the matrix units take K Q^T of tile t + 1, the vector units take the exponentials of
+// tile t, and while those take V^T P^T of tile t, these the exponentials that are left and the maximum of tile t + 1.  The keys run one tile ahead of the
+// values in LDS.  MOD: scores with a cap or a bias.
+template <int DP, bool MOD>
+__global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
+  typedef __bf16 T;
+  using L = Lds<T, DP>;
+  constexpr int KT = 64, TB = KT * L::RB, TD = DP / 32, STEPS = L::STEPS;
+  constexpr int NK = 2 * STEPS, NP = 4 * TD, AHEAD = 3;   // products of a tile: K Q^T, V^T P^T; operands are read AHEAD of them
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
+  __shared__ int kd[2][KT];
+  __shared__ int shared_range[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  int id = place(blockIdx.x, gridDim.x);
+  const int split = id % p.nsplit;
+  id /= p.nsplit;
+  const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
+  const Row w = row_of(p, b, kh, r, keys);
+  const Limits lim = limits_of(p, w, r);
+  int t0, t1;
+  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  Frag<T, DP> qf;
+  const int i = r / p.G, head = kh * p.G + r - i * p.G;
+  load_row<T, DP>(qf, p.direct, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2]);
+  const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
+  const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  Chunks<T, DP, KT> kat, vat;
+  if (p.whole) {
+    kat.set(tid, p.ks[1]);
+    vat.set(tid, p.vs[1]);
   }
+  auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
+  auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, char* to) {
+    if (p.whole && !kdoc && (t + 1) * KT <= keys) at.load(to, (const char*)(base + (long long)t * KT * stride), wave);
+    else load_tile<T, DP, KT>(to, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? base + j * stride : nullptr; });
+  };
+  auto issue_k = [&](int t, int buf) {
+    issue(kbase, p.ks[1], kat, t, smem + buf * TB);
+    if (kdoc && tid < KT) kd[buf][tid] = t * KT + tid < keys ? kdoc[t * KT + tid] : -1;
+  };
+  auto issue_v = [&](int t, int buf) { issue(vbase, p.vs[1], vat, t, smem + (2 + buf) * TB); };
+
+  // addresses of a lane's operands: chunk 2 s + h of row l % 32, and the columns of columns_by; steps and columns are exclusive ors of their low bits
+  const unsigned lds0 = lds_address(smem);
+  const unsigned ka = lds0 + (lane & 31) * L::RB + ((h ^ L::swizzle(lane & 31)) << 4);
+  const int vr = 4 * h + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const unsigned va = lds0 + 2 * TB + vr * L::RB + ((vc ^ L::swizzle(vr)) << 4) + 8 * (lane & 1);
+  auto read_k = [&](int buf, int x) { return lds_read16((ka ^ ((x % STEPS) << 5)) + buf * TB + x / STEPS * 32 * L::RB); };
+  auto read_v = [&](int buf, int x) {
+    const unsigned at = buf * TB + x / TD * 16 * L::RB;
+    return lds_read_columns((va ^ (x % TD << 6)) + at, (va ^ (x % TD << 6) ^ 32) + at + 8 * L::RB);
+  };
+
+  f32x16 acc[TD], sa[2], sb[2];
+#pragma unroll
+  for (int t = 0; t < TD; ++t) acc[t] = (f32x16){};
+  float m = -3.4e38f, l[2] = {0.0f, 0.0f};   // the reference of the exponents, at most 8 below the row's maximum so far, and the lane's share of the sum
+  const bool cap = MOD && p.cap > 0.0f, bias = MOD && p.slopes != nullptr;
+  const float mul = MOD ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E;
+  // Scores of the next tile into n and / or the weights of this one, whose scores s holds, into acc; returns the largest product of n
+  auto products = [&](auto has_next, auto has_this, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) {
+    constexpr bool NEXT = decltype(has_next)::value, THIS = decltype(has_this)::value;
+    float top = -INFINITY;
+    u32x4 kf[AHEAD + 1];
+    bf16x8 vf[AHEAD + 1], weights = {};
+    auto weigh = [&](int e) {
+      s[e >> 4][e & 15] = __builtin_amdgcn_exp2f(s[e >> 4][e & 15] * mul - m);
+      l[e & 1] += s[e >> 4][e & 15];
+    };
+    if constexpr (NEXT) {
+      n[0] = n[1] = (f32x16){};
+      unrolled<AHEAD>([&](auto x) { kf[decltype(x)::value] = read_k(buf ^ 1, decltype(x)::value); });
+      unrolled<NK>([&](auto xt) {
+        constexpr int x = decltype(xt)::value;
+        if constexpr (x + AHEAD < NK) kf[(x + AHEAD) % (AHEAD + 1)] = read_k(buf ^ 1, x + AHEAD);
+        else if constexpr (THIS) vf[x + AHEAD - NK] = read_v(buf, x + AHEAD - NK);
+        n[x / STEPS] = mma<T>(kf[x % (AHEAD + 1)], qf[x % STEPS], n[x / STEPS]);
+        if constexpr (THIS) {
+          unrolled<16 / NK>([&](auto e) { weigh(x * (16 / NK) + decltype(e)::value); });
+          keep(l[0]);
+          keep(l[1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    } else {
+      unrolled<AHEAD>([&](auto x) { vf[decltype(x)::value] = read_v(buf, decltype(x)::value); });
+      unrolled<16>([&](auto e) { weigh(decltype(e)::value); });
+    }
+    if constexpr (THIS) {
+      unrolled<NP>([&](auto xt) {
+        constexpr int x = decltype(xt)::value, g = x / TD, E = 32 / NP;
+        if constexpr (x + AHEAD < NP) vf[(x + AHEAD) % (AHEAD + 1)] = read_v(buf, x + AHEAD);
+        if constexpr (x % TD == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) weights[e] = (__bf16)s[g >> 1][8 * (g & 1) + e];
+        }
+        acc[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x % (AHEAD + 1)], weights, acc[x % TD], 0, 0, 0);
+        if constexpr (x < NP / 2) {
+          unrolled<E>([&](auto e) { weigh(16 + x * E + decltype(e)::value); });
+          keep(l[0]);
+          keep(l[1]);
+        } else if constexpr (NEXT && !MOD) {
+          constexpr int y = (x - NP / 2) * 2 * E;
+          unrolled<E>([&](auto e) { constexpr int z = y + 2 * decltype(e)::value; top = max_of(top, n[z >> 4][z & 15], n[z >> 4][(z & 15) + 1]); });
+          keep(top);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    } else if constexpr (!MOD) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) top = max_of(top, n[e >> 4][e & 15]);
+    }
+    return top;
+  };
+  std::true_type yes;
+  std::false_type no;
+  // what the products of tile t become before the exponential, and the row's reference
+  auto take_scores = [&](int t, int buf, f32x16 (&s)[2], float top, bool need) {
+    const int j0 = t * KT;
+    if constexpr (MOD) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) scores<T>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
+    }
+    if (need) {
+      const int hh = prism::here(h);
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        const int j = 8 * g + 4 * hh;
+        int4 d = make_int4(w.doc, w.doc, w.doc, w.doc);
+        if (kdoc) d = *(const int4*)&kd[buf][j];
+        const int dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = s[g >> 2][4 * (g & 3) + e];
+          s[g >> 2][4 * (g & 3) + e] = j0 + j + e <= w.last && dd[e] == w.doc ? x : -INFINITY;
+        }
+      }
+    }
+    if (MOD || need) {
+      top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) top = max_of(top, s[e >> 4][e & 15]);
+    }
+    top *= mul;
+    if (__any(top > m + 8.0f)) {
+      const float to = fmaxf(m, fmaxf(top, other_half(top))), f = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l[0] *= f;
+      l[1] *= f;
+#pragma unroll
+      for (int t2 = 0; t2 < TD; ++t2)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t2][e] *= f;
+    }
+  };
+  auto landed = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+  };
+  // A tile that the wave's rows do not see is masked, not skipped: one straight path through the loop keeps its registers in place.
+  auto next_scores = [&](int t, int buf, f32x16 (&n)[2], float top) {
+    bool need;
+    const bool any = tile_seen<KT>(p, lim, b, t, need);
+    take_scores(t, buf, n, top, need || !any);
+  };
+  auto step = [&](int t, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) {
+    landed();   // keys t + 1 and values t are there; keys t and values t - 1 have been read by all waves
+    if (t + 2 < t1) issue_k(t + 2, buf);
+    issue_v(t + 1, buf ^ 1);
+    next_scores(t + 1, buf ^ 1, n, products(yes, yes, buf, s, n));
+  };
+  if (t0 < t1 && lim.last < 0) {   // a wave without rows only takes its share of the loads
+    issue_k(t0, 0);
+    for (int t = t0; t < t1; ++t) {
+      const int buf = (t - t0) & 1;
+      landed();
+      if (t + 1 < t1) issue_k(t + 1, buf ^ 1);
+      issue_v(t, buf);
+    }
+    landed();
+  } else if (t0 < t1) {
+    issue_k(t0, 0);
+    landed();
+    if (t0 + 1 < t1) issue_k(t0 + 1, 1);
+    issue_v(t0, 0);
+    next_scores(t0, 0, sa, products(yes, no, 1, sb, sa));
+    int t = t0;
+    for (; t + 2 < t1; t += 2) {
+      step(t, 0, sa, sb);
+      step(t + 1, 1, sb, sa);
+    }
+    if (t + 1 < t1) {
+      step(t, 0, sa, sb);
+      landed();
+      products(no, yes, 1, sb, sa);
+    } else {
+      landed();
+      products(no, yes, 0, sa, sb);
+    }
+  }
+  float sum = l[0] + l[1];
+  sum += other_half(sum);
+  finish<T, DP>(p, acc, m, sum, split, pair, b, i, head, r, h);
 }
 
 // The parts of a row's keys joined; a wave takes a row
@@ -150,12 +360,15 @@ template <typename T> __global__ void __launch_bounds__(256) attention_join_kern
 
 template <typename T, int DP> int launch(Attn& p, hipStream_t s) {
   constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
-  const int rc = allow_dynamic_lds((const void*)attention_kernel<T, DP>, bytes);
+  void (*kernel)(Attn);
+  if constexpr (sizeof(T) == 4) kernel = attention_kernel<T, DP>;
+  else kernel = p.cap > 0.0f || p.slopes ? attention_bf16_kernel<DP, true> : attention_bf16_kernel<DP, false>;
+  const int rc = allow_dynamic_lds((const void*)kernel, bytes);
   if (rc != PRISM_OK) return rc;
   const long long rows = (long long)p.batch * p.hk * p.R;
   {
     ProfScope prof(PK_ATTENTION, s);
-    hipLaunchKernelGGL((attention_kernel<T, DP>), dim3((unsigned)p.batch * p.hk * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.batch * p.hk * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p);
   }
   if (p.nsplit > 1) {
     ProfScope prof(PK_ATTENTION_JOIN, s);

@@ -40,9 +40,19 @@ struct Attn {
   int nsplit;                       // parts of the keys (forward, dq) or rows (dk, dv) of a tile
   float *part, *part_ml;            // results of the parts
   bool direct;                      // rows are whole vectors of 16 bytes
+  bool whole;                       // ... of exactly DP entries, and the offsets within a tile fit 31 bits
 };
 
 __device__ const unsigned zero_page[4] = {0, 0, 0, 0};
+
+// The same value, computed again where it is used: what the rare branches of a loop derive from it is not kept in registers across the loop.
+__device__ inline int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The value is there at this point of the program: a sum is not put off to where it is used.
+__device__ inline void keep(float& a) { asm volatile("" : "+v"(a)); }
 
 // Tiles of rows of DP elements in LDS (the head size rounded up to 64 or 128; entries past it are zero), in chunks of 16 bytes.  Chunk c of row r lies at c ^ swizzle(r):
 // the reads of 16 rows at one chunk (the operand as it is), of 4 rows at four chunks (the transposed one, bf16) and of two rows four apart (fp32) then fall on different banks.
@@ -63,6 +73,7 @@ template <typename T, int DP> using Frag = u32x4[Lds<T, DP>::STEPS];
 template <typename T, int DP, int ROWS, typename F>
 __device__ inline void load_tile(char* lds, bool direct, int dim, int tid, F&& row) {
   using L = Lds<T, DP>;
+  tid = here(tid);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
   for (int u = 0; u < ROWS * L::CPR / NT; ++u) {
@@ -80,6 +91,36 @@ __device__ inline void load_tile(char* lds, bool direct, int dim, int tid, F&& r
       *(u32x4*)(lds + at * 16) = x.v;
     }
   }
+}
+
+// The same for whole tiles of rows of DP entries: byte offsets of a thread's chunks within a tile, and the loads from a uniform address.
+template <typename T, int DP, int ROWS> struct Chunks {
+  static constexpr int N = ROWS * Lds<T, DP>::CPR / NT;
+  unsigned at[N];
+  __device__ void set(int tid, long long stride) {
+    using L = Lds<T, DP>;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int x = u * NT + tid, r = x / L::CPR;
+      at[u] = (unsigned)(r * (int)stride * (int)sizeof(T)) + (((x % L::CPR) ^ L::swizzle(r)) << 4);
+    }
+  }
+  __device__ void load(char* lds, const char* base, int wave) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u) __builtin_amdgcn_global_load_lds((gptr_t)(base + at[u]), (lptr_t)(lds + (u * NW + wave) * 1024), 16, 0, 0);
+  }
+};
+
+typedef const u32x4 __attribute__((address_space(3)))* lds16_t;
+__device__ inline u32x4 lds_read16(unsigned a) { return *(lds16_t)a; }
+__device__ inline unsigned lds_address(const char* p) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)p; }
+
+// The chunks of columns_by in bf16 at their LDS addresses: 8 + 8 rows of four columns' neighbours, transposed
+__device__ inline bf16x8 lds_read_columns(unsigned a0, unsigned a1) {
+  union { s16x4 q[2]; bf16x8 v; } a;
+  a.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a0);
+  a.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a1);
+  return a.v;
 }
 
 // One row as a lane's operand
@@ -167,6 +208,10 @@ __device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int r
     }
   }
 }
+
+// The largest (NaN if one is): the one instruction that needs no quieting of its operands first
+__device__ inline float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ inline float max_of(float a, float b, float c) { return max_of(max_of(a, b), c); }
 
 __device__ inline float other_half(float x) {   // the value of lane l ^ 32
   return __shfl_xor(x, 32);
@@ -378,6 +423,8 @@ inline Attn attn_common(const void* q, const void* k, const void* v, int dt, con
   p.qrange = (const int4*)ws;
   p.krange = p.qrange + (long long)d.batch * ((d.q_len + 63) / 64);
   p.direct = d.head_dim * (dt == PRISM_F32 ? 4 : 2) % 16 == 0 && rows_are_vectors(q, d.q, dt) && rows_are_vectors(k, d.k, dt) && rows_are_vectors(v, d.v, dt);
+  const long long widest = d.k.token > d.v.token ? d.k.token : d.v.token;
+  p.whole = p.direct && (d.head_dim == 64 || d.head_dim == 128) && widest < (1ll << 22);
   return p;
 }
 
