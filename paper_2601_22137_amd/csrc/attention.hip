@@ -157,8 +157,8 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
   Chunks<T, DP, KT> kat, vat;
   if (p.whole) {
-    kat.set(tid, p.ks[1]);
-    vat.set(tid, p.vs[1]);
+    kat.set(tid, 1, p.ks[1], 0);
+    vat.set(tid, 1, p.vs[1], 0);
   }
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
   auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, char* to) {
@@ -399,7 +399,7 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
     return o;
   };
   if (d.q_doc) take((size_t)d.batch * ((d.q_len + 63) / 64 + (d.k_len + 63) / 64) * sizeof(int4));
-  if (backward) a.o_stat = take((size_t)pairs * 2 * R * sizeof(float));
+  if (backward) a.o_stat = take(((size_t)pairs * 2 * R + 64) * sizeof(float));
   size_t part = a.split > 1 ? (size_t)a.split * pairs * R * d.head_dim * sizeof(float) : 0;
   const size_t dkv = a.split_dkv > 1 ? (size_t)2 * a.split_dkv * pairs * d.k_len * d.head_dim * sizeof(float) : 0;
   a.o_part = take(part > dkv ? part : dkv);

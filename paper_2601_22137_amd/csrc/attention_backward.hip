@@ -132,29 +132,17 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
     store_row<float, DP>(p.part + (((long long)split * p.batch * p.hk + pair) * p.R + r) * p.dim, acc, p.scale, p.dim, p.direct, h);
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const float* stat) {
-  using L = Lds<T, DP>;
-  constexpr int RT = key_tile<T>(), RBK = RT / 32, TB = RT * L::RB;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each
-  __shared__ __attribute__((aligned(16))) float lse2[2][RT], delta[2][RT], slope[2][RT];
-  __shared__ __attribute__((aligned(16))) int last[2][RT], doc[2][RT], place_of[2][RT];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-  const int key_tiles = (p.m + 127) / 128;
-  int id = place(blockIdx.x, gridDim.x);
-  const int split = id % p.nsplit;
-  id /= p.nsplit;
-  const int tile = id % key_tiles, pair = id / key_tiles, b = pair / p.hk, kh = pair - b * p.hk;
-  const int keys = keys_of(p, b), j = tile * 128 + wave * 32 + (lane & 31), wave_j1 = tile * 128 + wave * 32 + 31;
-  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
-  int mydoc = j < keys ? 0 : -1;
-  if (kdoc && j < keys) mydoc = max(kdoc[j], -1);
-  // rows that may see one of the workgroup's keys
+// The row tiles [t0, t1) that may see one of the workgroup's keys, and the lowest and highest document of the wave's keys; all threads call it.
+// The workgroups of a pair walk their tiles from the last one down, a part every nsplit-th: whatever their keys, they then read the same rows at about the
+// same time, from the XCD's L2.
+template <int RT>
+__device__ inline void row_range(const Attn& p, int b, int tile, int keys, int mydoc, int* sh, int& t0, int& t1, int& dlo, int& dhi) {
+  const int tid = threadIdx.x;
   int i0 = 0, i1 = p.n;
   if (p.causal && !(p.prefix && min(p.prefix[b], keys) > tile * 128)) i0 = max(0, tile * 128 - keys + p.n);
   if (tile * 128 >= keys) i1 = 0;
-  int dlo = 0, dhi = 0;                    // the wave's documents
-  if (kdoc) {
+  dlo = dhi = 0;
+  if (p.kdoc) {
     dlo = mydoc < 0 ? 0x7FFFFFFF : mydoc;
     dhi = mydoc;
     int lo = 0x7FFFFFFF, hi = -1;
@@ -165,7 +153,6 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
       hi = max(hi, k.y);
     }
     // the first and last block of 64 queries with one of them
-    int* sh = &last[0][0];
     if (tid == 0) { sh[0] = 0x7FFFFFFF; sh[1] = -1; }
     __syncthreads();
     int f = 0x7FFFFFFF, e = -1;
@@ -189,10 +176,52 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
     dlo = __builtin_amdgcn_readfirstlane(dlo);
     dhi = __builtin_amdgcn_readfirstlane(dhi);
   }
-  const bool keys_mixed = kdoc && (dlo != dhi || __any(mydoc < 0));
   const int first_tile = i0 * p.G / RT, end_tile = i0 < i1 ? (i1 * p.G + RT - 1) / RT : first_tile;
-  const int per = (max(end_tile - first_tile, 0) + p.nsplit - 1) / p.nsplit;
-  const int t0 = __builtin_amdgcn_readfirstlane(first_tile + split * per), t1 = __builtin_amdgcn_readfirstlane(min(end_tile, first_tile + (split + 1) * per));
+  t0 = __builtin_amdgcn_readfirstlane(first_tile);
+  t1 = __builtin_amdgcn_readfirstlane(end_tile);
+}
+
+// Key tile, part and pair of a workgroup.  Under the causal mask the first key tiles have the most rows: the first half of a pair's workgroups takes them from the
+// first on, the second half the others from the last on, so that two which share a CU have about the same work together.
+__device__ inline void key_tile_of(const Attn& p, int& tile, int& split, int& pair) {
+  const int key_tiles = (p.m + 127) / 128, id = place(blockIdx.x, gridDim.x) / p.nsplit;
+  split = place(blockIdx.x, gridDim.x) % p.nsplit;
+  pair = id / key_tiles;
+  const int x = id - pair * key_tiles, half = (key_tiles + 1) / 2;
+  tile = x < half ? x : key_tiles - 1 - (x - half);
+}
+
+template <typename T, int DP>
+__device__ inline void store_dkv(const Attn& p, const f32x16 (&dk)[DP / 32], const f32x16 (&dv)[DP / 32], int split, int pair, int b, int kh, int j, int h) {
+  if (j >= p.m) return;
+  if (p.nsplit == 1) {
+    store_row<T, DP>((T*)p.dk + b * p.dks[0] + j * p.dks[1] + kh * p.dks[2], dk, p.scale, p.dim, p.direct, h);
+    store_row<T, DP>((T*)p.dv + b * p.dvs[0] + j * p.dvs[1] + kh * p.dvs[2], dv, 1.0f, p.dim, p.direct, h);
+  } else {
+    const long long pairs = (long long)p.batch * p.hk, row = (split * pairs + pair) * p.m + j;
+    store_row<float, DP>(p.part + row * p.dim, dk, p.scale, p.dim, p.direct, h);
+    store_row<float, DP>(p.part + (p.nsplit * pairs * p.m + row) * p.dim, dv, 1.0f, p.dim, p.direct, h);
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const float* stat) {
+  using L = Lds<T, DP>;
+  constexpr int RT = key_tile<T>(), RBK = RT / 32, TB = RT * L::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each
+  __shared__ __attribute__((aligned(16))) float lse2[2][RT], delta[2][RT], slope[2][RT];
+  __shared__ __attribute__((aligned(16))) int last[2][RT], doc[2][RT], place_of[2][RT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  int tile, split, pair;
+  key_tile_of(p, tile, split, pair);
+  const int b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), j = tile * 128 + wave * 32 + (lane & 31), wave_j1 = tile * 128 + wave * 32 + 31;
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  int mydoc = j < keys ? 0 : -1;
+  if (kdoc && j < keys) mydoc = max(kdoc[j], -1);
+  int t0, t1, dlo, dhi;
+  row_range<RT>(p, b, tile, keys, mydoc, &last[0][0], t0, t1, dlo, dhi);
+  const bool keys_mixed = kdoc && (dlo != dhi || __any(mydoc < 0));
   Frag<T, DP> kf, vf;
   load_row<T, DP>(kf, p.direct, p.dim, h, mydoc < 0 ? nullptr : (const T*)p.k + b * p.ks[0] + j * p.ks[1] + kh * p.ks[2]);
   load_row<T, DP>(vf, p.direct, p.dim, h, mydoc < 0 ? nullptr : (const T*)p.v + b * p.vs[0] + j * p.vs[1] + kh * p.vs[2]);
@@ -222,12 +251,11 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
   for (int t = 0; t < DP / 32; ++t) { dk[t] = (f32x16){}; dv[t] = (f32x16){}; }
   const bool cap = p.cap > 0.0f, bias = p.slopes != nullptr;
   const float mul = cap || bias ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E, per_cap = cap ? 1.0f / out : 0.0f;
-  if (t0 < t1) issue(t0, 0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+  if (t1 - 1 - split >= t0) issue(t1 - 1 - split, 0);
+  for (int t = t1 - 1 - split, buf = 0; t >= t0; t -= p.nsplit, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
-    if (t + 1 < t1) issue(t + 1, buf ^ 1);
+    if (t - p.nsplit >= t0) issue(t - p.nsplit, buf ^ 1);
     // Rows that see nothing have lse2 = +inf and need no mask.  The keys that a row sees grow with its token: the tile's first row says whether all see all.
     const Row first = row_of(p, b, kh, t * RT, keys);
     bool need = kdoc || first.last < wave_j1;
@@ -282,15 +310,202 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
       columns_by<T, DP>(dk, qt, 32 * rb, dp, lane);
     }
   }
-  if (j >= p.m) return;
-  if (p.nsplit == 1) {
-    store_row<T, DP>((T*)p.dk + b * p.dks[0] + j * p.dks[1] + kh * p.dks[2], dk, p.scale, p.dim, p.direct, h);
-    store_row<T, DP>((T*)p.dv + b * p.dvs[0] + j * p.dvs[1] + kh * p.dvs[2], dv, 1.0f, p.dim, p.direct, h);
-  } else {
-    const long long pairs = (long long)p.batch * p.hk, row = (split * pairs + pair) * p.m + j;
-    store_row<float, DP>(p.part + row * p.dim, dk, p.scale, p.dim, p.direct, h);
-    store_row<float, DP>(p.part + (p.nsplit * pairs * p.m + row) * p.dim, dv, 1.0f, p.dim, p.direct, h);
+  store_dkv<T, DP>(p, dk, dv, split, pair, b, kh, j, h);
+}
+
+// dk and dv in bf16.  Per block of 32 rows: scores Q K^T, then dp = dO V^T while the exponentials are taken, then dv while ds is, then dk; the operands of every product are read from LDS a few products ahead.
+// Two waves per SIMD have 256 registers each: 128 of them are sums at DP = 128, so V stays in LDS there (its rows are read again for every block), and
+// tiles of 32 rows leave room for two workgroups per CU.
+template <int DP, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const float* stat) {
+  typedef __bf16 T;
+  using L = Lds<T, DP>;
+  constexpr bool V_IN_LDS = DP > 64;
+  constexpr int RT = DP > 64 ? 32 : 64, TB = RT * L::RB, TD = DP / 32, STEPS = L::STEPS, NC = 2 * TD, AHEAD = DP > 64 ? 2 : 3;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each; the values of the workgroup's keys
+  __shared__ __attribute__((aligned(16))) float lse2[2][64], delta[2][64], slope[2][RT];
+  __shared__ __attribute__((aligned(16))) int last[2][RT], doc[2][RT], place_of[2][RT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  int tile, split, pair;
+  key_tile_of(p, tile, split, pair);
+  const int b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), j = tile * 128 + wave * 32 + (lane & 31), wave_j1 = tile * 128 + wave * 32 + 31;
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  int mydoc = j < keys ? 0 : -1;
+  if (kdoc && j < keys) mydoc = max(kdoc[j], -1);
+  int t0, t1, dlo, dhi;
+  row_range<RT>(p, b, tile, keys, mydoc, &last[0][0], t0, t1, dlo, dhi);
+  const bool keys_mixed = kdoc && (dlo != dhi || __any(mydoc < 0));
+  const T* krow = mydoc < 0 ? nullptr : (const T*)p.k + b * p.ks[0] + j * p.ks[1] + kh * p.ks[2];
+  const T* vrow = mydoc < 0 ? nullptr : (const T*)p.v + b * p.vs[0] + j * p.vs[1] + kh * p.vs[2];
+  Frag<T, DP> kf, vf;
+  load_row<T, DP>(kf, p.direct, p.dim, h, krow);
+  load_row<T, DP>(vf, p.direct, p.dim, h, vrow);
+  const unsigned lds0 = lds_address(smem), row_at = (lane & 31) * L::RB + ((h ^ L::swizzle(lane & 31)) << 4);
+  const unsigned va = lds0 + 4 * TB + wave * 32 * L::RB + row_at;
+  if constexpr (V_IN_LDS) {   // read by the wave that writes it
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) *(__attribute__((address_space(3))) u32x4*)(va ^ (s << 5)) = vf[s];
   }
+  const T* qbase = (const T*)p.q + b * p.qs[0] + kh * p.G * p.qs[2];
+  const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
+  const float* st = stat + (long long)pair * 2 * p.R;
+  // Where the group divides 32, a tile's rows lie alike in every tile
+  const bool alike = p.whole && !p.qdoc;
+  Chunks<T, DP, RT> qat, doat;
+  if (alike) {
+    qat.set(tid, p.G, p.qs[1], p.qs[2]);
+    doat.set(tid, p.G, p.dos[1], p.dos[2]);
+  }
+  auto issue = [&](int t, int buf) {
+    if (alike && (t + 1) * RT <= p.R) {
+      const long long token = (long long)t * RT / p.G;
+      qat.load(smem + buf * TB, (const char*)(qbase + token * p.qs[1]), wave);
+      doat.load(smem + (2 + buf) * TB, (const char*)(dobase + token * p.dos[1]), wave);
+    } else {
+      auto at = [&](int x, const T* base, const long long (&s)[3]) -> const T* {
+        const int r = t * RT + x, i = r / p.G, g = r - i * p.G;
+        return r < p.R && !(p.qdoc && p.qdoc[(long long)b * p.n + i] < 0) ? base + i * s[1] + g * s[2] : nullptr;
+      };
+      load_tile<T, DP, RT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { return at(x, qbase, p.qs); });
+      load_tile<T, DP, RT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { return at(x, dobase, p.dos); });
+    }
+    if ((t + 1) * RT > p.R) {
+      if (tid < RT) {
+        lse2[buf][tid] = t * RT + tid < p.R ? st[t * RT + tid] : INFINITY;
+        delta[buf][tid] = t * RT + tid < p.R ? st[p.R + t * RT + tid] : 0.0f;
+      }
+    } else if (wave == 0) {   // 64 of them; what lies past a tile of 32 (or the last pair, in the pad of the workspace) is not used
+      const __attribute__((address_space(1))) char *x = (const __attribute__((address_space(1))) char*)(st + t * RT), *y = x + (size_t)p.R * sizeof(float);
+      const unsigned at = here(lane) * 4;
+      asm volatile("" : "+s"(x), "+s"(y));
+      __builtin_amdgcn_global_load_lds((gptr_t)(x + at), (lptr_t)lse2[buf], 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t)(y + at), (lptr_t)delta[buf], 4, 0, 0);
+    }
+    if (BIAS || kdoc || (t + 1) * RT > p.R || row_of(p, b, kh, t * RT, keys).last < tile * 128 + 127) {
+      const int x = here(tid);
+      if (x < RT) {
+        const Row w = row_of(p, b, kh, t * RT + x, keys);
+        last[buf][x] = w.last;
+        doc[buf][x] = w.doc;
+        place_of[buf][x] = w.at;
+        slope[buf][x] = w.slope;
+      }
+    }
+  };
+  f32x16 dk[TD], dv[TD];
+#pragma unroll
+  for (int t = 0; t < TD; ++t) { dk[t] = (f32x16){}; dv[t] = (f32x16){}; }
+  const float in = CAP ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E;
+  const unsigned qa = lds0 + row_at;
+  const int cr = 4 * h + ((lane & 15) >> 2), cc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const unsigned ca = lds0 + cr * L::RB + ((cc ^ L::swizzle(cr)) << 4) + 8 * (lane & 1);
+  if (t1 - 1 - split >= t0) issue(t1 - 1 - split, 0);
+  for (int t = t1 - 1 - split, buf = 0; t >= t0; t -= p.nsplit, buf ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+    if (t - p.nsplit >= t0) issue(t - p.nsplit, buf ^ 1);
+    // Rows that see nothing have lse2 = +inf and need no mask.  The keys that a row sees grow with its token: the tile's first row says whether all see all.
+    const Row first = row_of(p, b, kh, t * RT, keys);
+    bool need = kdoc || first.last < wave_j1 || (t + 1) * RT > p.R;
+    if (kdoc && !keys_mixed && first.last >= wave_j1 && (t + 1) * RT <= p.R) {
+      const int qblocks = (p.n + 63) / 64, x0 = t * RT / p.G / 64, x1 = (t * RT + RT - 1) / p.G / 64;
+      const int4 a = p.qrange[(long long)b * qblocks + x0], c = p.qrange[(long long)b * qblocks + x1];
+      need = !(a.x == dlo && a.y == dlo && c.x == dlo && c.y == dlo);
+    }
+#pragma unroll
+    for (int rb = 0; rb < RT / 32; ++rb) {
+      const unsigned at = buf * TB + rb * 32 * L::RB;
+      // operand x of the block: rows of Q, rows of dO, columns of dO, columns of Q
+      auto read = [&](auto xt) -> u32x4 {
+        constexpr int x = decltype(xt)::value;
+        if constexpr (x < STEPS) return lds_read16((qa ^ (x << 5)) + at);
+        else if constexpr (x < 2 * STEPS) return lds_read16((qa ^ ((x - STEPS) << 5)) + at + 2 * TB);
+        else {
+          constexpr int y = (x - 2 * STEPS) % NC, z = y / TD * 16 * L::RB + (x - 2 * STEPS < NC ? 2 * TB : 0);
+          return __builtin_bit_cast(u32x4, lds_read_columns((ca ^ (y % TD << 6)) + at + z, (ca ^ (y % TD << 6) ^ 32) + at + z + 8 * L::RB));
+        }
+      };
+      constexpr int N = 2 * STEPS + 2 * NC;
+      u32x4 op[AHEAD + 1], vop[2];
+      auto next = [&](auto xt) {
+        constexpr int x = decltype(xt)::value;
+        if constexpr (x + AHEAD < N) op[(x + AHEAD) % (AHEAD + 1)] = read(std::integral_constant<int, x + AHEAD>{});
+        return op[x % (AHEAD + 1)];
+      };
+      unrolled<AHEAD>([&](auto x) { op[decltype(x)::value] = read(x); });
+      f32x16 s = {}, dp = {};
+      unrolled<STEPS>([&](auto xt) {
+        constexpr int x = decltype(xt)::value;
+        s = mma<T>(next(xt), kf[x], s);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (V_IN_LDS) vop[0] = lds_read16(va);
+      if (need) {
+        const int hh = here(h);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int x = 32 * rb + 8 * g + 4 * hh;
+          const int4 la = *(const int4*)&last[buf][x], d4 = *(const int4*)&doc[buf][x];
+          const int ll[4] = {la.x, la.y, la.z, la.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] = j <= ll[e] && dd[e] == mydoc ? s[4 * g + e] : -INFINITY;
+        }
+      }
+      bf16x8 weights[2], grads[2];
+      f32x4 row4, slope4;
+      int4 place4;
+      unrolled<STEPS>([&](auto xt) {
+        constexpr int x = decltype(xt)::value, E = 16 / STEPS;
+        u32x4 v;
+        if constexpr (V_IN_LDS) {
+          if constexpr (x + 1 < STEPS) vop[(x + 1) & 1] = lds_read16(va ^ ((x + 1) << 5));
+          v = vop[x & 1];
+        } else {
+          v = vf[x];
+        }
+        dp = mma<T>(next(std::integral_constant<int, STEPS + x>{}), v, dp);
+        unrolled<E>([&](auto et) {
+          constexpr int e = x * E + decltype(et)::value;
+          if constexpr (e % 4 == 0) {
+            constexpr int r4 = 8 * (e / 4);
+            row4 = *(const f32x4*)&lse2[buf][32 * rb + r4 + 4 * h];
+            if constexpr (BIAS) {
+              slope4 = *(const f32x4*)&slope[buf][32 * rb + r4 + 4 * h];
+              place4 = *(const int4*)&place_of[buf][32 * rb + r4 + 4 * h];
+            }
+          }
+          float a = s[e] * in, t2 = 0.0f;
+          if constexpr (CAP) {
+            t2 = tanh_of(a, false);
+            a = t2 * out;
+          }
+          if constexpr (BIAS) a -= slope4[e & 3] * fabsf((float)((e & 3) == 0 ? place4.x - j : (e & 3) == 1 ? place4.y - j : (e & 3) == 2 ? place4.z - j : place4.w - j));
+          if constexpr (CAP) a = s[e] > -INFINITY ? a : -INFINITY;      // the cap has taken a masked score back up
+          s[e] = __builtin_amdgcn_exp2f(a - row4[e & 3]);
+          weights[e >> 3][e & 7] = (__bf16)s[e];
+          if constexpr (CAP) s[e] *= 1.0f - t2 * t2;
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      unrolled<NC>([&](auto xt) {
+        constexpr int x = decltype(xt)::value, E = 16 / NC;
+        dv[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, 2 * STEPS + x>{})), weights[x / TD], dv[x % TD], 0, 0, 0);
+        unrolled<E>([&](auto et) {
+          constexpr int e = x * E + decltype(et)::value;
+          if constexpr (e % 4 == 0) row4 = *(const f32x4*)&delta[buf][32 * rb + 8 * (e / 4) + 4 * h];
+          grads[e >> 3][e & 7] = (__bf16)(s[e] * (dp[e] - row4[e & 3]));
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      unrolled<NC>([&](auto xt) {
+        constexpr int x = decltype(xt)::value;
+        dk[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, 2 * STEPS + NC + x>{})), grads[x / TD], dk[x % TD], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    }
+  }
+  store_dkv<T, DP>(p, dk, dv, split, pair, b, kh, j, h);
 }
 
 // to[pair][row] = the sum of the parts, in their order; row -> (token, head) as row / G and row % G
@@ -314,7 +529,16 @@ template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* s
   constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
   int rc = allow_dynamic_lds((const void*)attention_dq_kernel<T, DP, true>, bytes);
   if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)attention_dq_kernel<T, DP, false>, bytes);
-  if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)attention_dkv_kernel<T, DP>, bytes);
+  void (*dkv)(Attn, const float*);
+  int dkv_bytes = bytes;
+  if constexpr (sizeof(T) == 4) {
+    dkv = attention_dkv_kernel<T, DP>;
+  } else {
+    dkv = p.cap > 0.0f ? (p.slopes ? attention_dkv_bf16_kernel<DP, true, true> : attention_dkv_bf16_kernel<DP, true, false>)
+                       : (p.slopes ? attention_dkv_bf16_kernel<DP, false, true> : attention_dkv_bf16_kernel<DP, false, false>);
+    dkv_bytes = DP > 64 ? (4 * 32 + 128) * Lds<T, DP>::RB : 4 * 64 * Lds<T, DP>::RB;
+  }
+  if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)dkv, dkv_bytes);
   if (rc != PRISM_OK) return rc;
   const unsigned pairs = (unsigned)p.batch * p.hk;
   p.nsplit = 1;
@@ -335,7 +559,7 @@ template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* s
   p.nsplit = plan.split_dkv;
   {
     ProfScope prof(PK_ATTENTION_DKV, s);
-    hipLaunchKernelGGL((attention_dkv_kernel<T, DP>), dim3(pairs * ((p.m + 127) / 128) * p.nsplit), dim3(NT), bytes, s, p, (const float*)stat);
+    hipLaunchKernelGGL(dkv, dim3(pairs * ((p.m + 127) / 128) * p.nsplit), dim3(NT), dkv_bytes, s, p, (const float*)stat);
   }
   if (p.nsplit > 1) {
     ProfScope prof(PK_ATTENTION_JOIN, s);
@@ -359,6 +583,10 @@ int launch_attention_backward(const void* dout, const void* q, const void* k, co
   p.part = (float*)(ws + plan.o_part);
   p.direct = p.direct && rows_are_vectors(out, d.out, dt) && rows_are_vectors(dout, d.dout, dt) && rows_are_vectors(dq, d.dq, dt) &&
              rows_are_vectors(dk, d.dk, dt) && rows_are_vectors(dv, d.dv, dt);
+  // the rows of a tile lie alike in all tiles, their offsets within one fit 31 bits
+  const long long G = d.q_heads / d.k_heads;
+  p.whole = p.whole && p.direct && 32 % G == 0;
+  for (const prism_strides& x : {d.q, d.dout}) p.whole = p.whole && x.token * (32 / G) + x.head * G < (1ll << 28);
   float* stat = (float*)(ws + plan.o_stat);
   if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, plan, stat, s) : launch<float, 128>(p, plan, stat, s);
   return d.head_dim <= 64 ? launch<__bf16, 64>(p, plan, stat, s) : launch<__bf16, 128>(p, plan, stat, s);

@@ -93,21 +93,27 @@ __device__ inline void load_tile(char* lds, bool direct, int dim, int tid, F&& r
   }
 }
 
-// The same for whole tiles of rows of DP entries: byte offsets of a thread's chunks within a tile, and the loads from a uniform address.
+// The same for whole tiles of rows of DP entries.  The chunks of a thread lie a fixed number of rows apart, at which the swizzle repeats: one offset, and a
+// uniform step.
 template <typename T, int DP, int ROWS> struct Chunks {
-  static constexpr int N = ROWS * Lds<T, DP>::CPR / NT;
-  unsigned at[N];
-  __device__ void set(int tid, long long stride) {
+  static constexpr int APART = NT / Lds<T, DP>::CPR, N = ROWS / APART;
+  unsigned at;
+  long long step;
+  // row x is token x / G, head x % G (G divides 32) of the first row's token
+  __device__ void set(int tid, int G, long long token, long long head) {
     using L = Lds<T, DP>;
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int x = u * NT + tid, r = x / L::CPR;
-      at[u] = (unsigned)(r * (int)stride * (int)sizeof(T)) + (((x % L::CPR) ^ L::swizzle(r)) << 4);
-    }
+    const int r = tid / L::CPR, i = r / G;
+    at = (unsigned)((i * (int)token + (r - i * G) * (int)head) * (int)sizeof(T)) + (((tid % L::CPR) ^ L::swizzle(r)) << 4);
+    step = (G > APART ? APART * head : APART / G * token) * (long long)sizeof(T);
   }
   __device__ void load(char* lds, const char* base, int wave) const {
+    // uniform address plus 32-bit offset: added by the load itself, not kept as an address per lane
+    const unsigned off = (unsigned)here((int)at);
 #pragma unroll
-    for (int u = 0; u < N; ++u) __builtin_amdgcn_global_load_lds((gptr_t)(base + at[u]), (lptr_t)(lds + (u * NW + wave) * 1024), 16, 0, 0);
+    for (int u = 0; u < N; ++u) {
+      const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(base + u * step);
+      __builtin_amdgcn_global_load_lds((gptr_t)(from + off), (lptr_t)(lds + (u * NW + wave) * 1024), 16, 0, 0);
+    }
   }
 };
 
