@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
   using L = Lds<T, DP>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
-  __shared__ int kd[2][KT];
+  __shared__ __attribute__((aligned(16))) int kd[2][KT];
   __shared__ int shared_range[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
     __syncthreads();
     if (t + 1 < t1) issue(t + 1, buf ^ 1);
     bool need;
-    if (!tile_seen<KT>(p, lim, b, t, need)) continue;
+    if (!tile_seen<KT>(p, lim, key_docs<KT>(p, b, t), t, need)) continue;
     const char *kt = smem + buf * TB, *vt = smem + (2 + buf) * TB;
     f32x16 s[KB];
     float top = -INFINITY;
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   constexpr int KT = 64, TB = KT * L::RB, TD = DP / 32, STEPS = L::STEPS;
   constexpr int NK = 2 * STEPS, NP = 4 * TD, AHEAD = 3;   // products of a tile: K Q^T, V^T P^T; operands are read AHEAD of them
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
-  __shared__ int kd[2][KT];
+  __shared__ __attribute__((aligned(16))) int kd[2][KT];
   __shared__ int shared_range[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
@@ -161,15 +161,16 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
     vat.set(tid, 1, p.vs[1], 0);
   }
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
-  auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, char* to) {
-    if (p.whole && !kdoc && (t + 1) * KT <= keys) at.load(to, (const char*)(base + (long long)t * KT * stride), wave);
+  auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, bool hidden, char* to) {
+    if (p.whole && !hidden && (t + 1) * KT <= keys) at.load(to, (const char*)(base + (long long)t * KT * stride), wave);
     else load_tile<T, DP, KT>(to, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? base + j * stride : nullptr; });
   };
-  auto issue_k = [&](int t, int buf) {
-    issue(kbase, p.ks[1], kat, t, smem + buf * TB);
-    if (kdoc && tid < KT) kd[buf][tid] = t * KT + tid < keys ? kdoc[t * KT + tid] : -1;
+  // hidden: a key of no document is among the tile's
+  auto issue_k = [&](int t, bool hidden, int buf) {
+    issue(kbase, p.ks[1], kat, t, hidden, smem + buf * TB);
+    if (kdoc && wave == 0) load_ids(kd[buf], kdoc, t * KT, p.m, lane);
   };
-  auto issue_v = [&](int t, int buf) { issue(vbase, p.vs[1], vat, t, smem + (2 + buf) * TB); };
+  auto issue_v = [&](int t, bool hidden, int buf) { issue(vbase, p.vs[1], vat, t, hidden, smem + (2 + buf) * TB); };
 
   // addresses of a lane's operands: chunk 2 s + h of row l % 32, and the columns of columns_by; steps and columns are exclusive ors of their low bits
   const unsigned lds0 = lds_address(smem);
@@ -289,32 +290,37 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
     __syncthreads();
   };
   // A tile that the wave's rows do not see is masked, not skipped: one straight path through the loop keeps its registers in place.
-  auto next_scores = [&](int t, int buf, f32x16 (&n)[2], float top) {
+  auto next_scores = [&](int t, const int4& docs, int buf, f32x16 (&n)[2], float top) {
     bool need;
-    const bool any = tile_seen<KT>(p, lim, b, t, need);
+    const bool any = tile_seen<KT>(p, lim, docs, t, need);
     take_scores(t, buf, n, top, need || !any);
   };
+  int4 docs;   // of the next tile's keys
   auto step = [&](int t, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) {
+    const int4 after = key_docs<KT>(p, b, min(t + 2, t1 - 1));
     landed();   // keys t + 1 and values t are there; keys t and values t - 1 have been read by all waves
-    if (t + 2 < t1) issue_k(t + 2, buf);
-    issue_v(t + 1, buf ^ 1);
-    next_scores(t + 1, buf ^ 1, n, products(yes, yes, buf, s, n));
+    if (t + 2 < t1) issue_k(t + 2, after.z, buf);
+    issue_v(t + 1, docs.z, buf ^ 1);
+    next_scores(t + 1, docs, buf ^ 1, n, products(yes, yes, buf, s, n));
+    docs = after;
   };
   if (t0 < t1 && lim.last < 0) {   // a wave without rows only takes its share of the loads
-    issue_k(t0, 0);
+    issue_k(t0, key_docs<KT>(p, b, t0).z, 0);
     for (int t = t0; t < t1; ++t) {
       const int buf = (t - t0) & 1;
       landed();
-      if (t + 1 < t1) issue_k(t + 1, buf ^ 1);
-      issue_v(t, buf);
+      if (t + 1 < t1) issue_k(t + 1, key_docs<KT>(p, b, t + 1).z, buf ^ 1);
+      issue_v(t, key_docs<KT>(p, b, t).z, buf);
     }
     landed();
   } else if (t0 < t1) {
-    issue_k(t0, 0);
+    const int4 first = key_docs<KT>(p, b, t0);
+    issue_k(t0, first.z, 0);
+    docs = key_docs<KT>(p, b, min(t0 + 1, t1 - 1));
     landed();
-    if (t0 + 1 < t1) issue_k(t0 + 1, 1);
-    issue_v(t0, 0);
-    next_scores(t0, 0, sa, products(yes, no, 1, sb, sa));
+    if (t0 + 1 < t1) issue_k(t0 + 1, docs.z, 1);
+    issue_v(t0, first.z, 0);
+    next_scores(t0, first, 0, sa, products(yes, no, 1, sb, sa));
     int t = t0;
     for (; t + 2 < t1; t += 2) {
       step(t, 0, sa, sb);
@@ -331,7 +337,8 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   }
   float sum = l[0] + l[1];
   sum += other_half(sum);
-  finish<T, DP>(p, acc, m, sum, split, pair, b, i, head, r, h);
+  const int re = tile * 128 + wave * 32 + (prism::here(lane) & 31), ie = re / p.G;   // (again, rather than kept)
+  finish<T, DP>(p, acc, m, sum, split, pair, b, ie, kh * p.G + re - ie * p.G, re, h);
 }
 
 // The parts of a row's keys joined; a wave takes a row
@@ -391,7 +398,27 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
   };
   a.split = parts(pairs * ((R + 127) / 128), (d.k_len + kt - 1) / kt);
-  a.split_dkv = backward ? parts(pairs * ((d.k_len + 127) / 128), (R + kt - 1) / kt) : 1;
+  // dk and dv: the rows of a key tile are many or few under the causal mask.  Up to 512 key tiles (two workgroups per CU) are cut into parts of equal length,
+  // as many as run at once; 2 x 4096 x 16 heads of 128 on 4 key heads: 628 us in two parts each, XXX so.
+  const int key_tiles = (d.k_len + 127) / 128;
+  a.parts = 1;
+  a.items = key_tiles;
+  if (backward && pairs * key_tiles > 0 && pairs * key_tiles <= 512) {
+    long long all = 0;
+    for (int k = 0; k < key_tiles; ++k) all += rows_of_key_tile(d.causal, d.prefix, d.q_len, d.k_len, (int)(R / (d.q_len ? d.q_len : 1)), k);
+    long long chunk = (all * pairs + 511) / 512;
+    for (chunk = chunk < 4 * kt ? 4 * kt : (chunk + 31) / 32 * 32;; chunk += (chunk / 16 + 31) / 32 * 32) {
+      a.items = 0;
+      a.parts = 1;
+      for (int k = 0; k < key_tiles; ++k) {
+        const int n = parts_of(rows_of_key_tile(d.causal, d.prefix, d.q_len, d.k_len, (int)(R / (d.q_len ? d.q_len : 1)), k), (int)chunk);
+        a.items += n;
+        if (n > a.parts) a.parts = n;
+      }
+      if (a.items * pairs <= 512) break;
+    }
+    a.chunk = a.parts > 1 ? (int)chunk : 0;
+  }
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -401,7 +428,7 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
   if (d.q_doc) take((size_t)d.batch * ((d.q_len + 63) / 64 + (d.k_len + 63) / 64) * sizeof(int4));
   if (backward) a.o_stat = take(((size_t)pairs * 2 * R + 64) * sizeof(float));
   size_t part = a.split > 1 ? (size_t)a.split * pairs * R * d.head_dim * sizeof(float) : 0;
-  const size_t dkv = a.split_dkv > 1 ? (size_t)2 * a.split_dkv * pairs * d.k_len * d.head_dim * sizeof(float) : 0;
+  const size_t dkv = a.parts > 1 ? (size_t)2 * a.parts * pairs * d.k_len * d.head_dim * sizeof(float) : 0;
   a.o_part = take(part > dkv ? part : dkv);
   a.o_ml = take(a.split > 1 && !backward ? (size_t)a.split * pairs * R * 2 * sizeof(float) : 0);
   a.total = at;

@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
   using L = Lds<T, DP>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
-  __shared__ int kd[2][KT];
+  __shared__ __attribute__((aligned(16))) int kd[2][KT];
   __shared__ int shared_range[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
       if (lse != -INFINITY) lse2 = lse * LOG2E;
       if (h == 0) stat[r] = lse2;
     }
-    if (sizeof(T) == 4 || t1 - t0 > 4) {
+    {
       Frag<T, DP> of;
       load_row<T, DP>(of, p.direct, p.dim, h, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr);
 #pragma unroll
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
     __syncthreads();
     if (t + 1 < t1) issue(t + 1, buf ^ 1);
     bool need;
-    if (!tile_seen<KT>(p, lim, b, t, need)) continue;
+    if (!tile_seen<KT>(p, lim, key_docs<KT>(p, b, t), t, need)) continue;
     const char *kt = smem + buf * TB, *vt = smem + (2 + buf) * TB;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -132,8 +132,200 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
     store_row<float, DP>(p.part + (((long long)split * p.batch * p.hk + pair) * p.R + r) * p.dim, acc, p.scale, p.dim, p.direct, h);
 }
 
+// The same in bf16.  A tile of 64 keys is taken as two blocks: scores K Q^T and dp = V dO^T of the first, with its exponentials beside the latter; the scores of the second beside
+// ds of the first; dq; and so on.
+template <int DP, bool CAP, bool BIAS, bool DELTA>
+__global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float* stat) {
+  typedef __bf16 T;
+  using L = Lds<T, DP>;
+  constexpr int KT = 64, TB = KT * L::RB, TD = DP / 32, STEPS = L::STEPS, NC = DELTA ? 0 : 2 * TD, AHEAD = 4;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
+  __shared__ __attribute__((aligned(16))) int kd[2][KT];
+  __shared__ int shared_range[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  int id = place(blockIdx.x, gridDim.x);
+  const int split = id % p.nsplit;
+  id /= p.nsplit;
+  const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
+  const Row w = row_of(p, b, kh, r, keys);
+  const Limits lim = limits_of(p, w, r);
+  int t0, t1;
+  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  const int i = r / p.G, head = kh * p.G + r - i * p.G;
+  const bool any = w.last >= 0;
+  Frag<T, DP> qf, dof;
+  load_row<T, DP>(dof, p.direct, p.dim, h, any ? (const T*)p.dout + b * p.dos[0] + i * p.dos[1] + head * p.dos[2] : nullptr);
+  stat += (long long)pair * 2 * p.R;
+  float lse2 = INFINITY, delta = 0.0f;
+  if constexpr (DELTA) {
+    if (r < p.R) {
+      const float lse = p.lse_in[((long long)b * p.hq + head) * p.n + i];
+      if (lse != -INFINITY) lse2 = lse * LOG2E;
+      if (h == 0) stat[r] = lse2;
+    }
+    if (t1 - t0 > 4) {
+      Frag<T, DP> of;
+      load_row<T, DP>(of, p.direct, p.dim, h, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        const bf16x8 x = __builtin_bit_cast(bf16x8, of[s]), y = __builtin_bit_cast(bf16x8, dof[s]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta += (float)x[e] * (float)y[e];
+      }
+      t0 = t1;
+    }
+  } else if (r < p.R) {
+    lse2 = stat[r];
+    delta = stat[p.R + r];
+  }
+  if (t0 < t1) load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
+  const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
+  const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
+  const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
+  Chunks<T, DP, KT> kat, vat;
+  if (p.whole_keys) {
+    kat.set(tid, 1, p.ks[1], 0);
+    vat.set(tid, 1, p.vs[1], 0);
+  }
+  auto issue = [&](int t, bool hidden, int buf) {
+    auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
+    if (p.whole_keys && !hidden && (t + 1) * KT <= keys) {
+      kat.load(smem + buf * TB, (const char*)(kbase + (long long)t * KT * p.ks[1]), wave);
+      vat.load(smem + (2 + buf) * TB, (const char*)(vbase + (long long)t * KT * p.vs[1]), wave);
+    } else {
+      load_tile<T, DP, KT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? kbase + j * p.ks[1] : nullptr; });
+      load_tile<T, DP, KT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? vbase + j * p.vs[1] : nullptr; });
+    }
+    if (kdoc && wave == 0) load_ids(kd[buf], kdoc, t * KT, p.m, lane);
+  };
+  f32x16 acc[TD];
+#pragma unroll
+  for (int t = 0; t < TD; ++t) acc[t] = (f32x16){};
+  const float in = CAP ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E;
+  const unsigned lds0 = lds_address(smem), ka = lds0 + (lane & 31) * L::RB + ((h ^ L::swizzle(lane & 31)) << 4);
+  const int cr = 4 * h + ((lane & 15) >> 2), cc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const unsigned ca = lds0 + cr * L::RB + ((cc ^ L::swizzle(cr)) << 4) + 8 * (lane & 1);
+  int4 docs = make_int4(0, 0, 0, 0);
+  if (t0 < t1) {
+    docs = key_docs<KT>(p, b, t0);
+    issue(t0, docs.z, 0);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1, j0 = t * KT;
+    const int4 after = key_docs<KT>(p, b, min(t + 1, t1 - 1));
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1, after.z, buf ^ 1);
+    bool need;
+    const bool some = tile_seen<KT>(p, lim, docs, t, need);
+    docs = after;
+    if (!some) continue;
+    const unsigned at = buf * TB;
+    // operands in the order of their use: rows of K and of V of the first block, rows of K of the second, columns of K of the first, rows of V and columns of K of the second
+    auto read = [&](auto xt) -> u32x4 {
+      constexpr int x = decltype(xt)::value, S = STEPS;
+      if constexpr (x < S) return lds_read16((ka ^ (x << 5)) + at);
+      else if constexpr (x < 2 * S) return lds_read16((ka ^ ((x - S) << 5)) + at + 2 * TB);
+      else if constexpr (x < 3 * S) return lds_read16((ka ^ ((x - 2 * S) << 5)) + at + 32 * L::RB);
+      else if constexpr (x >= 3 * S + NC && x < 4 * S + NC) return lds_read16((ka ^ ((x - 3 * S - NC) << 5)) + at + 2 * TB + 32 * L::RB);
+      else {
+        constexpr bool second = x >= 4 * S + NC;
+        constexpr int y = second ? x - 4 * S - NC : x - 3 * S, z = (y / TD * 16 + (second ? 32 : 0)) * L::RB;
+        return __builtin_bit_cast(u32x4, lds_read_columns((ca ^ (y % TD << 6)) + at + z, (ca ^ (y % TD << 6) ^ 32) + at + z + 8 * L::RB));
+      }
+    };
+    constexpr int N = 4 * STEPS + 2 * NC;
+    u32x4 op[N];
+    auto next = [&](auto xt) {
+      constexpr int x = decltype(xt)::value;
+      if constexpr (x + AHEAD < N) op[x + AHEAD] = read(std::integral_constant<int, x + AHEAD>{});
+      return op[x];
+    };
+    unrolled<AHEAD>([&](auto x) { op[decltype(x)::value] = read(x); });
+    f32x16 s[2] = {}, dp[2] = {};
+    bf16x8 grads[2];
+    auto mask = [&](auto kbt) {
+      constexpr int kb = decltype(kbt)::value;
+      if (!need) return;
+      const int hh = here(h);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int j = 8 * g + 4 * hh + 32 * kb;
+        int4 d = make_int4(w.doc, w.doc, w.doc, w.doc);
+        if (kdoc) d = *(const int4*)&kd[buf][j];
+        const int dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[kb][4 * g + e] = j0 + j + e <= w.last && dd[e] == w.doc ? s[kb][4 * g + e] : -INFINITY;
+      }
+    };
+    auto weigh = [&](auto kbt, auto et) {      // s becomes the weight
+      constexpr int kb = decltype(kbt)::value, e = decltype(et)::value;
+      float a = s[kb][e] * in, t2 = 0.0f;
+      if constexpr (CAP) {
+        t2 = tanh_of(a, false);
+        a = t2 * out;
+      }
+      if constexpr (BIAS) a -= w.slope * fabsf((float)(w.at - j0 - 4 * h) - (float)(32 * kb + 8 * (e >> 2) + (e & 3)));
+      if constexpr (CAP) a = s[kb][e] > -INFINITY ? a : -INFINITY;      // the cap has taken a masked score back up
+      s[kb][e] = __builtin_amdgcn_exp2f(a - lse2);
+      if constexpr (DELTA) return;
+      if constexpr (CAP) s[kb][e] *= 1.0f - t2 * t2;
+    };
+    auto grad = [&](auto kbt, auto et) {
+      constexpr int kb = decltype(kbt)::value, e = decltype(et)::value;
+      grads[e >> 3][e & 7] = (__bf16)(s[kb][e] * (dp[kb][e] - delta));
+    };
+    // product of rows, with EACH entries of work beside every step
+    auto rows = [&](f32x16& c, const Frag<T, DP>& f, auto first, auto&& work) {
+      unrolled<STEPS>([&](auto xt) {
+        constexpr int x = decltype(xt)::value;
+        c = mma<T>(next(std::integral_constant<int, decltype(first)::value + x>{}), f[x], c);
+        unrolled<16 / STEPS>([&](auto et) { work(std::integral_constant<int, x * (16 / STEPS) + decltype(et)::value>{}); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    auto columns = [&](auto first) {
+      unrolled<NC>([&](auto xt) {
+        constexpr int x = decltype(xt)::value;
+        acc[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, decltype(first)::value + x>{})), grads[x / TD], acc[x % TD], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    std::integral_constant<int, 0> b0;
+    std::integral_constant<int, 1> b1;
+    auto nothing = [](auto) {};
+    rows(s[0], qf, std::integral_constant<int, 0>{}, nothing);
+    mask(b0);
+    rows(dp[0], dof, std::integral_constant<int, STEPS>{}, [&](auto e) { weigh(b0, e); });
+    rows(s[1], qf, std::integral_constant<int, 2 * STEPS>{}, [&](auto e) {
+      if constexpr (DELTA) { delta += s[0][decltype(e)::value] * dp[0][decltype(e)::value]; keep(delta); }
+      else grad(b0, e);
+    });
+    columns(std::integral_constant<int, 3 * STEPS>{});
+    mask(b1);
+    rows(dp[1], dof, std::integral_constant<int, 3 * STEPS + NC>{}, [&](auto e) { weigh(b1, e); });
+    unrolled<16>([&](auto e) {
+      if constexpr (DELTA) delta += s[1][decltype(e)::value] * dp[1][decltype(e)::value];
+      else grad(b1, e);
+    });
+    columns(std::integral_constant<int, 4 * STEPS + NC>{});
+  }
+  if constexpr (DELTA) {
+    delta += other_half(delta);
+    if (r < p.R && h == 0) stat[p.R + r] = delta;
+    return;
+  }
+  const int re = tile * 128 + wave * 32 + (here(lane) & 31), ie = re / p.G;   // (again, rather than kept)
+  if (re >= p.R) return;
+  if (p.nsplit == 1)
+    store_row<T, DP>((T*)p.dq + b * p.dqs[0] + ie * p.dqs[1] + (kh * p.G + re - ie * p.G) * p.dqs[2], acc, p.scale, p.dim, p.direct, h);
+  else
+    store_row<float, DP>(p.part + (((long long)split * p.batch * p.hk + pair) * p.R + re) * p.dim, acc, p.scale, p.dim, p.direct, h);
+}
+
 // The row tiles [t0, t1) that may see one of the workgroup's keys, and the lowest and highest document of the wave's keys; all threads call it.
-// The workgroups of a pair walk their tiles from the last one down, a part every nsplit-th: whatever their keys, they then read the same rows at about the
+// The workgroups of a pair walk their tiles from the last one down, a part every so many-th: whatever their keys, they then read the same rows at about the
 // same time, from the XCD's L2.
 template <int RT>
 __device__ inline void row_range(const Attn& p, int b, int tile, int keys, int mydoc, int* sh, int& t0, int& t1, int& dlo, int& dhi) {
@@ -181,26 +373,35 @@ __device__ inline void row_range(const Attn& p, int b, int tile, int keys, int m
   t1 = __builtin_amdgcn_readfirstlane(end_tile);
 }
 
-// Key tile, part and pair of a workgroup.  Under the causal mask the first key tiles have the most rows: the first half of a pair's workgroups takes them from the
-// first on, the second half the others from the last on, so that two which share a CU have about the same work together.
-__device__ inline void key_tile_of(const Attn& p, int& tile, int& split, int& pair) {
-  const int key_tiles = (p.m + 127) / 128, id = place(blockIdx.x, gridDim.x) / p.nsplit;
-  split = place(blockIdx.x, gridDim.x) % p.nsplit;
-  pair = id / key_tiles;
-  const int x = id - pair * key_tiles, half = (key_tiles + 1) / 2;
-  tile = x < half ? x : key_tiles - 1 - (x - half);
+// Key tile, part (of how many) and pair of a workgroup; the key tiles with the most rows come first
+__device__ inline void key_tile_of(const Attn& p, int& tile, int& part, int& parts, int& pair) {
+  const int id = place(blockIdx.x, gridDim.x);
+  pair = id / p.items;
+  part = id - pair * p.items;
+  tile = 0;
+  parts = 1;
+  if (!p.chunk) {
+    tile = part;
+    part = 0;
+    return;
+  }
+  for (;; ++tile) {
+    parts = parts_of(rows_of_key_tile(p.causal, p.prefix, p.n, p.m, p.G, tile), p.chunk);
+    if (part < parts) return;
+    part -= parts;
+  }
 }
 
 template <typename T, int DP>
-__device__ inline void store_dkv(const Attn& p, const f32x16 (&dk)[DP / 32], const f32x16 (&dv)[DP / 32], int split, int pair, int b, int kh, int j, int h) {
+__device__ inline void store_dkv(const Attn& p, const f32x16 (&dk)[DP / 32], const f32x16 (&dv)[DP / 32], int part, int pair, int b, int kh, int j, int h) {
   if (j >= p.m) return;
-  if (p.nsplit == 1) {
+  if (p.parts == 1) {
     store_row<T, DP>((T*)p.dk + b * p.dks[0] + j * p.dks[1] + kh * p.dks[2], dk, p.scale, p.dim, p.direct, h);
     store_row<T, DP>((T*)p.dv + b * p.dvs[0] + j * p.dvs[1] + kh * p.dvs[2], dv, 1.0f, p.dim, p.direct, h);
   } else {
-    const long long pairs = (long long)p.batch * p.hk, row = (split * pairs + pair) * p.m + j;
+    const long long pairs = (long long)p.batch * p.hk, row = ((long long)part * pairs + pair) * p.m + j;
     store_row<float, DP>(p.part + row * p.dim, dk, p.scale, p.dim, p.direct, h);
-    store_row<float, DP>(p.part + (p.nsplit * pairs * p.m + row) * p.dim, dv, 1.0f, p.dim, p.direct, h);
+    store_row<float, DP>(p.part + (p.parts * pairs * p.m + row) * p.dim, dv, 1.0f, p.dim, p.direct, h);
   }
 }
 
@@ -212,8 +413,8 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
   __shared__ __attribute__((aligned(16))) float lse2[2][RT], delta[2][RT], slope[2][RT];
   __shared__ __attribute__((aligned(16))) int last[2][RT], doc[2][RT], place_of[2][RT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-  int tile, split, pair;
-  key_tile_of(p, tile, split, pair);
+  int tile, part, parts, pair;
+  key_tile_of(p, tile, part, parts, pair);
   const int b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b), j = tile * 128 + wave * 32 + (lane & 31), wave_j1 = tile * 128 + wave * 32 + 31;
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
@@ -251,11 +452,11 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
   for (int t = 0; t < DP / 32; ++t) { dk[t] = (f32x16){}; dv[t] = (f32x16){}; }
   const bool cap = p.cap > 0.0f, bias = p.slopes != nullptr;
   const float mul = cap || bias ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E, per_cap = cap ? 1.0f / out : 0.0f;
-  if (t1 - 1 - split >= t0) issue(t1 - 1 - split, 0);
-  for (int t = t1 - 1 - split, buf = 0; t >= t0; t -= p.nsplit, buf ^= 1) {
+  if (t1 - 1 - part >= t0) issue(t1 - 1 - part, 0);
+  for (int t = t1 - 1 - part, buf = 0; t >= t0; t -= parts, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
-    if (t - p.nsplit >= t0) issue(t - p.nsplit, buf ^ 1);
+    if (t - parts >= t0) issue(t - parts, buf ^ 1);
     // Rows that see nothing have lse2 = +inf and need no mask.  The keys that a row sees grow with its token: the tile's first row says whether all see all.
     const Row first = row_of(p, b, kh, t * RT, keys);
     bool need = kdoc || first.last < wave_j1;
@@ -310,7 +511,14 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
       columns_by<T, DP>(dk, qt, 32 * rb, dp, lane);
     }
   }
-  store_dkv<T, DP>(p, dk, dv, split, pair, b, kh, j, h);
+  store_dkv<T, DP>(p, dk, dv, part, pair, b, kh, j, h);
+}
+
+template <int STEPS, int NC, int AHEAD> constexpr int read_by(int x) {
+  const int ahead = x < STEPS || x >= 2 * STEPS + NC ? 5 : AHEAD, n = 2 * STEPS + 2 * NC;
+  int to = x + 1 + ahead;
+  if (x < STEPS && to > STEPS + AHEAD) to = STEPS + AHEAD;   // the second product's are read no further ahead than its own
+  return to < n ? to : n;
 }
 
 // dk and dv in bf16.  Per block of 32 rows: scores Q K^T, then dp = dO V^T while the exponentials are taken, then dv while ds is, then dk; the operands of every product are read from LDS a few products ahead.
@@ -326,8 +534,8 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   __shared__ __attribute__((aligned(16))) float lse2[2][64], delta[2][64], slope[2][RT];
   __shared__ __attribute__((aligned(16))) int last[2][RT], doc[2][RT], place_of[2][RT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-  int tile, split, pair;
-  key_tile_of(p, tile, split, pair);
+  int tile, part, parts, pair;
+  key_tile_of(p, tile, part, parts, pair);
   const int b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b), j = tile * 128 + wave * 32 + (lane & 31), wave_j1 = tile * 128 + wave * 32 + 31;
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
@@ -351,14 +559,22 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
   const float* st = stat + (long long)pair * 2 * p.R;
   // Where the group divides 32, a tile's rows lie alike in every tile
-  const bool alike = p.whole && !p.qdoc;
   Chunks<T, DP, RT> qat, doat;
-  if (alike) {
+  if (p.whole) {
     qat.set(tid, p.G, p.qs[1], p.qs[2]);
     doat.set(tid, p.G, p.dos[1], p.dos[2]);
   }
+  // documents of the 64-token blocks of a tile's first and last row
+  auto docs_of = [&](int t, int4& x, int4& y) {
+    const int qblocks = (p.n + 63) / 64;
+    x = range_of(p.qrange, (long long)b * qblocks + t * RT / p.G / 64);
+    y = range_of(p.qrange, (long long)b * qblocks + min(t * RT + RT - 1, p.R - 1) / p.G / 64);
+  };
+  int row_doc = doc_of_row(p, b, (t1 - 1 - part) * RT + tid);   // of the tile that is issued next, read while the one before is on its way
   auto issue = [&](int t, int buf) {
-    if (alike && (t + 1) * RT <= p.R) {
+    int4 dx = make_int4(0, 0, 0, 0), dy = dx;
+    if (p.qdoc) docs_of(t, dx, dy);
+    if (p.whole && !dx.z && !dy.z && (t + 1) * RT <= p.R) {
       const long long token = (long long)t * RT / p.G;
       qat.load(smem + buf * TB, (const char*)(qbase + token * p.qs[1]), wave);
       doat.load(smem + (2 + buf) * TB, (const char*)(dobase + token * p.dos[1]), wave);
@@ -382,15 +598,16 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
       __builtin_amdgcn_global_load_lds((gptr_t)(x + at), (lptr_t)lse2[buf], 4, 0, 0);
       __builtin_amdgcn_global_load_lds((gptr_t)(y + at), (lptr_t)delta[buf], 4, 0, 0);
     }
-    if (BIAS || kdoc || (t + 1) * RT > p.R || row_of(p, b, kh, t * RT, keys).last < tile * 128 + 127) {
+    if (BIAS || kdoc || (t + 1) * RT > p.R || row_of(p, b, kh, t * RT, keys, 0).last < tile * 128 + 127) {
       const int x = here(tid);
       if (x < RT) {
-        const Row w = row_of(p, b, kh, t * RT + x, keys);
+        const Row w = row_of(p, b, kh, t * RT + x, keys, row_doc);
         last[buf][x] = w.last;
         doc[buf][x] = w.doc;
         place_of[buf][x] = w.at;
         slope[buf][x] = w.slope;
       }
+      if (tid < RT && t >= parts) row_doc = doc_of_row(p, b, (t - parts) * RT + tid);
     }
   };
   f32x16 dk[TD], dv[TD];
@@ -400,18 +617,18 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   const unsigned qa = lds0 + row_at;
   const int cr = 4 * h + ((lane & 15) >> 2), cc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
   const unsigned ca = lds0 + cr * L::RB + ((cc ^ L::swizzle(cr)) << 4) + 8 * (lane & 1);
-  if (t1 - 1 - split >= t0) issue(t1 - 1 - split, 0);
-  for (int t = t1 - 1 - split, buf = 0; t >= t0; t -= p.nsplit, buf ^= 1) {
+  if (t1 - 1 - part >= t0) issue(t1 - 1 - part, 0);
+  for (int t = t1 - 1 - part, buf = 0; t >= t0; t -= parts, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
-    if (t - p.nsplit >= t0) issue(t - p.nsplit, buf ^ 1);
+    if (t - parts >= t0) issue(t - parts, buf ^ 1);
     // Rows that see nothing have lse2 = +inf and need no mask.  The keys that a row sees grow with its token: the tile's first row says whether all see all.
-    const Row first = row_of(p, b, kh, t * RT, keys);
+    const Row first = row_of(p, b, kh, t * RT, keys, 0);
     bool need = kdoc || first.last < wave_j1 || (t + 1) * RT > p.R;
     if (kdoc && !keys_mixed && first.last >= wave_j1 && (t + 1) * RT <= p.R) {
-      const int qblocks = (p.n + 63) / 64, x0 = t * RT / p.G / 64, x1 = (t * RT + RT - 1) / p.G / 64;
-      const int4 a = p.qrange[(long long)b * qblocks + x0], c = p.qrange[(long long)b * qblocks + x1];
-      need = !(a.x == dlo && a.y == dlo && c.x == dlo && c.y == dlo);
+      int4 x, y;
+      docs_of(t, x, y);
+      need = !(x.x == dlo && x.y == dlo && y.x == dlo && y.y == dlo);
     }
 #pragma unroll
     for (int rb = 0; rb < RT / 32; ++rb) {
@@ -426,14 +643,14 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
           return __builtin_bit_cast(u32x4, lds_read_columns((ca ^ (y % TD << 6)) + at + z, (ca ^ (y % TD << 6) ^ 32) + at + z + 8 * L::RB));
         }
       };
+      // how many operands have been read when product x is taken: more ahead in the first and last product, whose sums leave the registers for it
       constexpr int N = 2 * STEPS + 2 * NC;
-      u32x4 op[AHEAD + 1], vop[2];
+      u32x4 op[N], vop[2];
       auto next = [&](auto xt) {
-        constexpr int x = decltype(xt)::value;
-        if constexpr (x + AHEAD < N) op[(x + AHEAD) % (AHEAD + 1)] = read(std::integral_constant<int, x + AHEAD>{});
-        return op[x % (AHEAD + 1)];
+        constexpr int x = decltype(xt)::value, from = x == 0 ? 0 : read_by<STEPS, NC, AHEAD>(x - 1), to = read_by<STEPS, NC, AHEAD>(x);
+        unrolled<to - from>([&](auto y) { op[from + decltype(y)::value] = read(std::integral_constant<int, from + decltype(y)::value>{}); });
+        return op[x];
       };
-      unrolled<AHEAD>([&](auto x) { op[decltype(x)::value] = read(x); });
       f32x16 s = {}, dp = {};
       unrolled<STEPS>([&](auto xt) {
         constexpr int x = decltype(xt)::value;
@@ -505,66 +722,79 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
       });
     }
   }
-  store_dkv<T, DP>(p, dk, dv, split, pair, b, kh, j, h);
+  store_dkv<T, DP>(p, dk, dv, part, pair, b, kh, j, h);
 }
 
-// to[pair][row] = the sum of the parts, in their order; row -> (token, head) as row / G and row % G
-template <typename T>
-__global__ void __launch_bounds__(256) attention_sum_kernel(const float* part, int nsplit, T* to, long long s0, long long s1, long long s2, int hk, int G, int R, int dim, long long total) {
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+// to[pair][row] = the sum of the parts, in their order; row -> (token, head) as row / G and row % G.  KEYS: dk and dv (blockIdx.y), whose key tiles have their own
+// numbers of parts.
+template <typename T, bool KEYS> __global__ void __launch_bounds__(256) attention_sum_kernel(Attn p, T* to0, T* to1) {
+  const int R = KEYS ? p.m : p.R, G = KEYS ? 1 : p.G;
+  const long long total = (long long)p.batch * p.hk * R * p.dim, at = (long long)blockIdx.x * 256 + threadIdx.x;
   if (at >= total) return;
+  const long long row = at / p.dim;
+  const int d = (int)(at - row * p.dim), pair = (int)(row / R), r = (int)(row - (long long)pair * R), b = pair / p.hk, kh = pair - b * p.hk, i = r / G;
+  const int n = KEYS ? parts_of(rows_of_key_tile(p.causal, p.prefix, p.n, p.m, p.G, r / 128), p.chunk) : p.nsplit;
+  const float* part = p.part + (KEYS && blockIdx.y ? p.parts * total : 0);
   float v = 0.0f;
-  for (int s = 0; s < nsplit; ++s) v += part[s * total + at];
-  const long long row = at / dim;
-  const int d = (int)(at - row * dim), pair = (int)(row / R), r = (int)(row - (long long)pair * R), b = pair / hk, kh = pair - b * hk, i = r / G;
-  to[b * s0 + i * s1 + (kh * G + r - i * G) * s2 + d] = (T)v;
-}
-
-template <typename T> void join(const float* part, int nsplit, void* to, const long long (&st)[3], int batch, int hk, int G, int R, int dim, hipStream_t s) {
-  const long long total = (long long)batch * hk * R * dim;
-  hipLaunchKernelGGL((attention_sum_kernel<T>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, part, nsplit, (T*)to, st[0], st[1], st[2], hk, G, R, dim, total);
+  for (int s = 0; s < n; ++s) v += part[s * total + at];
+  const long long (&st)[3] = !KEYS ? p.dqs : blockIdx.y ? p.dvs : p.dks;
+  (blockIdx.y ? to1 : to0)[b * st[0] + i * st[1] + (kh * G + r - i * G) * st[2] + d] = (T)v;
 }
 
 template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* stat, hipStream_t s) {
   constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
-  int rc = allow_dynamic_lds((const void*)attention_dq_kernel<T, DP, true>, bytes);
-  if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)attention_dq_kernel<T, DP, false>, bytes);
   void (*dkv)(Attn, const float*);
+  void (*dq[2])(Attn, float*);          // D, then dq
   int dkv_bytes = bytes;
   if constexpr (sizeof(T) == 4) {
+    dq[0] = attention_dq_kernel<T, DP, true>;
+    dq[1] = attention_dq_kernel<T, DP, false>;
     dkv = attention_dkv_kernel<T, DP>;
   } else {
-    dkv = p.cap > 0.0f ? (p.slopes ? attention_dkv_bf16_kernel<DP, true, true> : attention_dkv_bf16_kernel<DP, true, false>)
-                       : (p.slopes ? attention_dkv_bf16_kernel<DP, false, true> : attention_dkv_bf16_kernel<DP, false, false>);
+    auto pick = [&](auto cap, auto bias) {
+      constexpr bool C = decltype(cap)::value, B = decltype(bias)::value;
+      dq[0] = attention_dq_bf16_kernel<DP, C, B, true>;
+      dq[1] = attention_dq_bf16_kernel<DP, C, B, false>;
+      dkv = attention_dkv_bf16_kernel<DP, C, B>;
+    };
+    std::true_type yes;
+    std::false_type no;
+    p.cap > 0.0f ? (p.slopes ? pick(yes, yes) : pick(yes, no)) : (p.slopes ? pick(no, yes) : pick(no, no));
     dkv_bytes = DP > 64 ? (4 * 32 + 128) * Lds<T, DP>::RB : 4 * 64 * Lds<T, DP>::RB;
   }
+  int rc = PRISM_OK;
+  for (auto kernel : dq)
+    if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)kernel, bytes);
   if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)dkv, dkv_bytes);
   if (rc != PRISM_OK) return rc;
   const unsigned pairs = (unsigned)p.batch * p.hk;
   p.nsplit = 1;
   if (p.R > 0) {
     ProfScope prof(PK_ATTENTION_STAT, s);
-    hipLaunchKernelGGL((attention_dq_kernel<T, DP, true>), dim3(pairs * p.row_tiles), dim3(NT), bytes, s, p, stat);
+    hipLaunchKernelGGL(dq[0], dim3(pairs * p.row_tiles), dim3(NT), bytes, s, p, stat);
   }
   p.nsplit = plan.split;
   if (p.R > 0) {
     ProfScope prof(PK_ATTENTION_DQ, s);
-    hipLaunchKernelGGL((attention_dq_kernel<T, DP, false>), dim3(pairs * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p, stat);
+    hipLaunchKernelGGL(dq[1], dim3(pairs * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p, stat);
   }
   if (p.nsplit > 1 && p.R > 0) {
     ProfScope prof(PK_ATTENTION_JOIN, s);
-    join<T>(p.part, p.nsplit, p.dq, p.dqs, p.batch, p.hk, p.G, p.R, p.dim, s);
+    const long long total = (long long)pairs * p.R * p.dim;
+    hipLaunchKernelGGL((attention_sum_kernel<T, false>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, p, (T*)p.dq, (T*)nullptr);
   }
   if (p.m == 0) return PRISM_OK;
-  p.nsplit = plan.split_dkv;
+  p.chunk = plan.chunk;
+  p.parts = plan.parts;
+  p.items = plan.items;
   {
     ProfScope prof(PK_ATTENTION_DKV, s);
-    hipLaunchKernelGGL(dkv, dim3(pairs * ((p.m + 127) / 128) * p.nsplit), dim3(NT), dkv_bytes, s, p, (const float*)stat);
+    hipLaunchKernelGGL(dkv, dim3(pairs * p.items), dim3(NT), dkv_bytes, s, p, (const float*)stat);
   }
-  if (p.nsplit > 1) {
+  if (p.parts > 1) {
     ProfScope prof(PK_ATTENTION_JOIN, s);
-    join<T>(p.part, p.nsplit, p.dk, p.dks, p.batch, p.hk, 1, p.m, p.dim, s);
-    join<T>(p.part + (long long)p.nsplit * pairs * p.m * p.dim, p.nsplit, p.dv, p.dvs, p.batch, p.hk, 1, p.m, p.dim, s);
+    const long long total = (long long)pairs * p.m * p.dim;
+    hipLaunchKernelGGL((attention_sum_kernel<T, true>), dim3((unsigned)((total + 255) / 256), 2), dim3(256), 0, s, p, (T*)p.dk, (T*)p.dv);
   }
   return PRISM_OK;
 }
@@ -585,6 +815,7 @@ int launch_attention_backward(const void* dout, const void* q, const void* k, co
              rows_are_vectors(dk, d.dk, dt) && rows_are_vectors(dv, d.dv, dt);
   // the rows of a tile lie alike in all tiles, their offsets within one fit 31 bits
   const long long G = d.q_heads / d.k_heads;
+  p.whole_keys = p.whole;
   p.whole = p.whole && p.direct && 32 % G == 0;
   for (const prism_strides& x : {d.q, d.dout}) p.whole = p.whole && x.token * (32 / G) + x.head * G < (1ll << 28);
   float* stat = (float*)(ws + plan.o_stat);

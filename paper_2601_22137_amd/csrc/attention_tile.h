@@ -37,10 +37,12 @@ struct Attn {
   const float* slopes;
   const int *prefix, *lens, *qdoc, *kdoc;
   const int4 *qrange, *krange;      // of the documents of 64 tokens: lowest, highest, whether a token without one is among them
-  int nsplit;                       // parts of the keys (forward, dq) or rows (dk, dv) of a tile
+  int nsplit;                       // parts of the keys of a row tile (forward, dq)
+  int chunk, parts, items;          // dk, dv: see AttnPlan
   float *part, *part_ml;            // results of the parts
   bool direct;                      // rows are whole vectors of 16 bytes
-  bool whole;                       // ... of exactly DP entries, and the offsets within a tile fit 31 bits
+  bool whole;                       // ... of exactly DP entries, and the offsets within a tile fit 31 bits (dk, dv: of queries and dout)
+  bool whole_keys;                  // backward: the same of keys and values
 };
 
 __device__ const unsigned zero_page[4] = {0, 0, 0, 0};
@@ -127,6 +129,16 @@ __device__ inline bf16x8 lds_read_columns(unsigned a0, unsigned a1) {
   a.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a0);
   a.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a1);
   return a.v;
+}
+
+// The documents of 64 tokens from `at` on, by one wave
+__device__ inline void load_ids(int* lds, const int* doc, int at, int len, int lane) {
+  if (at + 64 <= len) {
+    const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(doc + at);
+    __builtin_amdgcn_global_load_lds((gptr_t)(from + (unsigned)here(lane) * 4), (lptr_t)lds, 4, 0, 0);
+  } else {
+    lds[lane] = at + lane < len ? doc[at + lane] : -1;
+  }
 }
 
 // One row as a lane's operand
@@ -245,7 +257,9 @@ struct Row {
   float slope; // log2(e) times that of its head
 };
 
-__device__ inline Row row_of(const Attn& p, int b, int kh, int r, int keys) {
+__device__ inline int doc_of_row(const Attn& p, int b, int r) { return p.qdoc && r < p.R ? p.qdoc[(long long)b * p.n + r / p.G] : 0; }
+
+__device__ inline Row row_of(const Attn& p, int b, int kh, int r, int keys, int doc) {
   Row w;
   w.at = 0; w.last = -1; w.doc = -2; w.slope = 0.0f;
   if (r < p.R) {
@@ -257,15 +271,14 @@ __device__ inline Row row_of(const Attn& p, int b, int kh, int r, int keys) {
       if (p.prefix) last = max(last, min(p.prefix[b], keys) - 1);
     }
     w.last = max(last, -1);
-    w.doc = 0;
-    if (p.qdoc) {
-      w.doc = p.qdoc[(long long)b * p.n + i];
-      if (w.doc < 0) { w.doc = -2; w.last = -1; }
-    }
+    w.doc = doc;
+    if (doc < 0) { w.doc = -2; w.last = -1; }
     if (p.slopes) w.slope = p.slopes[kh * p.G + g] * LOG2E;
   }
   return w;
 }
+
+__device__ inline Row row_of(const Attn& p, int b, int kh, int r, int keys) { return row_of(p, b, kh, r, keys, doc_of_row(p, b, r)); }
 
 __device__ inline int keys_of(const Attn& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.m) : p.m; }
 
@@ -380,12 +393,23 @@ __device__ inline void key_range(const Attn& p, const Limits& lim, int b, int ke
   t1 = __builtin_amdgcn_readfirstlane(min(end_tile, first_tile + (split + 1) * per));
 }
 
-// Whether the wave's rows see any key of tile t, and whether its scores have to be masked
-template <int KT> __device__ inline bool tile_seen(const Attn& p, const Limits& lim, int b, int t, bool& need) {
+// Documents of a block of 64 tokens: lowest, highest, whether one of none is among them.  Read through the scalar cache: a vector load would have to wait for the
+// tiles on their way.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef const i32x4 __attribute__((address_space(4)))* range_ptr;
+__device__ inline int4 range_of(const int4* ranges, long long block) {
+  const i32x4 x = *(range_ptr)(ranges + block);
+  return make_int4(x[0], x[1], x[2], x[3]);
+}
+template <int KT> __device__ inline int4 key_docs(const Attn& p, int b, int t) {
+  return p.kdoc ? range_of(p.krange, (long long)b * ((p.m + 63) / 64) + t * KT / 64) : make_int4(0, 0, 0, 0);
+}
+
+// Whether the wave's rows see any key of tile t, whose documents are k, and whether its scores have to be masked
+template <int KT> __device__ inline bool tile_seen(const Attn& p, const Limits& lim, const int4& k, int t, bool& need) {
   need = t * KT + KT - 1 > lim.first;
   if (t * KT > lim.last) return false;
   if (p.kdoc) {
-    const int4 k = p.krange[(long long)b * ((p.m + 63) / 64) + t * KT / 64];
     if (k.x > lim.hi || k.y < lim.lo) return false;
     need = need || lim.mixed || k.z || k.x != k.y || k.x != lim.lo;
   }
@@ -409,6 +433,13 @@ __device__ inline void scores(const Attn& p, f32x16& s, const Row& w, int j, boo
     for (int e = 0; e < 16; ++e) s[e] -= w.slope * fabsf(far - (float)(8 * (e >> 2) + (e & 3)));
   }
 }
+
+// Rows that may see one of the 128 keys of a tile, at most; and the parts that they are cut into, alike up to a tile
+__host__ __device__ inline long long rows_of_key_tile(bool causal, bool prefix, int n, int m, int G, int tile) {
+  const long long hidden = causal && !prefix ? tile * 128ll - m + n : 0;
+  return G * (hidden < 0 ? n : hidden > n ? 0 : n - hidden);
+}
+__host__ __device__ inline int parts_of(long long rows, int chunk) { return chunk && rows > chunk ? (int)((rows + chunk - 1) / chunk) : 1; }
 
 // ---- host
 

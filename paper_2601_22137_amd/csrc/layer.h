@@ -18,7 +18,8 @@ int launch_norm_rope_backward(const void* dqo, const void* dko, const void* q, c
                               const prism_norm_rope_desc& d, float* part, hipStream_t s);
 
 struct AttnPlan {
-  int split, split_dkv;                 // parts of the keys of a row tile; of the rows of a key tile
+  int split;                            // parts of the keys of a row tile
+  int chunk, parts, items;              // rows of a part of a key tile's rows (0: whole), the most parts of a key tile, parts of a pair
   size_t o_part, o_ml, o_stat, total;   // bytes from the start of the workspace, where the ranges of the documents lie
 };
 AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward);
