@@ -10,8 +10,8 @@ void set_last_error(const char* msg);
 
 int launch_dropout(const void* x, const void* residual, void* y, long long n, int dt, unsigned limit, uint64_t seed, uint32_t offset, hipStream_t s);
 
-// dw partials of prism_qk_norm_rope_backward: at most this many workgroups for the queries and as many for the keys
-constexpr int NR_MAX_BLOCKS = 1024;
+// workgroups of prism_qk_norm_rope_backward, each with partial sums of the weights' gradients: eight per CU
+constexpr int NR_MAX_BLOCKS = 2048;
 int launch_norm_rope(const void* q, const void* k, void* qo, void* ko, int dt, const prism_norm_rope_desc& d, hipStream_t s);
 size_t norm_rope_backward_bytes(const prism_norm_rope_desc& d);
 int launch_norm_rope_backward(const void* dqo, const void* dko, const void* q, const void* k, void* dq, void* dk, float* dqw, float* dkw, int dt,

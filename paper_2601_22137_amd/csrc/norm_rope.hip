@@ -27,75 +27,75 @@ struct NormRope {
   unsigned items[2];             // tokens x groups
   int blocks_q;                  // backward: the first blocks_q workgroups take queries
   float eps, scale;
-  bool norm, interleaved, vec;
+  bool norm, interleaved;
 };
 
-template <typename T> __device__ inline void load8(const T* p, float (&v)[8]);
-template <> __device__ inline void load8<float>(const float* p, float (&v)[8]) {
-  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
-}
-template <> __device__ inline void load8<__bf16>(const __bf16* p, float (&v)[8]) {
-  const bf16x8 a = *(const bf16x8*)p;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
-}
-template <typename T> __device__ inline void store8(T* p, const float (&v)[8]);
-template <> __device__ inline void store8<float>(float* p, const float (&v)[8]) {
-  f32x4 a, b;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) { a[e] = v[e]; b[e] = v[4 + e]; }
-  *(f32x4*)p = a;
-  *(f32x4*)(p + 4) = b;
-}
-template <> __device__ inline void store8<__bf16>(__bf16* p, const float (&v)[8]) {
-  bf16x8 a;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) a[e] = (__bf16)v[e];
-  *(bf16x8*)p = a;
-}
+// Eight entries as they lie in memory
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+  f32x4 lo, hi;
+  __device__ float get(int e) const { return e < 4 ? lo[e & 3] : hi[e & 3]; }
+  __device__ void set(int e, float x) { if (e < 4) lo[e & 3] = x; else hi[e & 3] = x; }
+};
+template <> struct Eight<__bf16> {
+  bf16x8 v;
+  __device__ float get(int e) const { return (float)v[e]; }
+  __device__ void set(int e, float x) { v[e] = (__bf16)x; }
+};
 
 // Where a unit's elements lie: pair e of unit u holds slots 16 u + 2 e and the next; slots 2 p and 2 p + 1 below rot are pair p.
-struct Unit {
+// VEC: every unit is two whole vectors.
+template <typename T, bool VEC> struct Unit {
   int u, dim, rot;
-  bool split, vec;                       // split: the partners of a pair lie rot / 2 apart
+  bool split;                            // the partners of a pair lie rot / 2 apart
+  struct Raw { Eight<T> a, b; };
   __device__ bool halves() const { return split && 16 * u < rot; }
   __device__ int element(int slot) const { return (!split || slot >= rot) ? slot : (slot & 1) ? (slot >> 1) + rot / 2 : slot >> 1; }
+  __device__ int second() const { return halves() ? rot / 2 + 8 * u : 16 * u + 8; }
 
-  template <typename T> __device__ void load(const T* row, float (&a)[8], float (&b)[8]) const {
-    if (vec) {
-      if (halves()) {
-        load8(row + 8 * u, a);
-        load8(row + rot / 2 + 8 * u, b);
-        return;
-      }
-      float v[2][8] = {};
-      if (16 * u < dim) load8(row + 16 * u, v[0]);
-      if (16 * u + 8 < dim) load8(row + 16 * u + 8, v[1]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) { a[e] = v[e >> 2][2 * (e & 3)]; b[e] = v[e >> 2][2 * (e & 3) + 1]; }
+  __device__ void load(const T* row, Raw& r) const {
+    if constexpr (VEC) {
+      const int f = halves() ? 8 * u : 16 * u, s = second();
+      r = Raw{};
+      if (f < dim) r.a = *(const Eight<T>*)(row + f);
+      if (s < dim) r.b = *(const Eight<T>*)(row + s);
       return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 8; ++e) {       // each half of the pairs by itself
       const int s = 16 * u + 2 * e;
-      a[e] = s < dim ? (float)row[element(s)] : 0.0f;
-      b[e] = s + 1 < dim ? (float)row[element(s + 1)] : 0.0f;
+      r.a.set(e, s < dim ? (float)row[element(s)] : 0.0f);
+      r.b.set(e, s + 1 < dim ? (float)row[element(s + 1)] : 0.0f);
     }
   }
-  template <typename T> __device__ void store(T* row, const float (&a)[8], const float (&b)[8]) const {
-    if (vec) {
-      if (halves()) {
-        store8(row + 8 * u, a);
-        store8(row + rot / 2 + 8 * u, b);
-        return;
-      }
-      float v[2][8];
+  __device__ void pairs(const Raw& r, float (&a)[8], float (&b)[8]) const {
+    if (!VEC || halves()) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { v[e >> 2][2 * (e & 3)] = a[e]; v[e >> 2][2 * (e & 3) + 1] = b[e]; }
-      if (16 * u < dim) store8(row + 16 * u, v[0]);
-      if (16 * u + 8 < dim) store8(row + 16 * u + 8, v[1]);
+      for (int e = 0; e < 8; ++e) { a[e] = r.a.get(e); b[e] = r.b.get(e); }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        a[e] = r.a.get(2 * e); b[e] = r.a.get(2 * e + 1);
+        a[4 + e] = r.b.get(2 * e); b[4 + e] = r.b.get(2 * e + 1);
+      }
+    }
+  }
+  __device__ void store(T* row, const float (&a)[8], const float (&b)[8]) const {
+    if constexpr (VEC) {
+      Raw r;
+      if (halves()) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { r.a.set(e, a[e]); r.b.set(e, b[e]); }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          r.a.set(2 * e, a[e]); r.a.set(2 * e + 1, b[e]);
+          r.b.set(2 * e, a[4 + e]); r.b.set(2 * e + 1, b[4 + e]);
+        }
+      }
+      const int f = halves() ? 8 * u : 16 * u, s = second();
+      if (f < dim) *(Eight<T>*)(row + f) = r.a;
+      if (s < dim) *(Eight<T>*)(row + s) = r.b;
       return;
     }
 #pragma unroll
@@ -107,19 +107,25 @@ struct Unit {
   }
 };
 
-// cos and sin (times scale) of the unit's pairs at a position; pairs past the rotated part stay as they are
-__device__ inline void angles(const NormRope& p, int u, int position, float (&c)[8], float (&s)[8]) {
+// cos and sin (times scale) of the unit's pairs at a position; pairs past the rotated part stay as they are.  The instructions take turns and are off by 1.3e-7 at most
+// on half a turn to either side.
+template <bool VEC> __device__ inline void angles(const NormRope& p, int u, int position, float (&c)[8], float (&s)[8]) {
+  float f[8];
+  if (VEC && 16 * u + 16 <= p.rot) {
+    const Eight<float> x = *(const Eight<float>*)(p.inv_freq + 8 * u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = x.get(e);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = 16 * u + 2 * e < p.rot ? p.inv_freq[8 * u + e] : 0.0f;
+  }
+  const double per_turn = (double)position * 0.15915494309189535;   // 1 / (2 pi)
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    c[e] = 1.0f;
-    s[e] = 0.0f;
-    if (16 * u + 2 * e < p.rot) {
-      const double turns = (double)position * (double)p.inv_freq[8 * u + e] * 0.15915494309189535;   // 1 / (2 pi)
-      float sn, cs;
-      sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-      c[e] = cs * p.scale;
-      s[e] = sn * p.scale;
-    }
+    const double turns = per_turn * (double)f[e];
+    const float x = (float)(turns - rint(turns)), by = 16 * u + 2 * e < p.rot ? p.scale : 1.0f;
+    c[e] = __builtin_amdgcn_cosf(x) * by;
+    s[e] = __builtin_amdgcn_sinf(x) * by;
   }
 }
 
@@ -129,36 +135,41 @@ template <int L> __device__ inline float over_lanes(float v) {
   return v;
 }
 
-__device__ inline void weights(const NormRope& p, const Unit& un, int kind, float (&wa)[8], float (&wb)[8]) {
+template <bool VEC> __device__ inline void weights(const NormRope& p, int u, int kind, float (&wa)[8], float (&wb)[8]) {
+  const Unit<float, VEC> un = {u, p.dim, p.rot, !p.interleaved};
+  if (p.w[kind]) {
+    typename Unit<float, VEC>::Raw r;
+    un.load(p.w[kind], r);
+    un.pairs(r, wa, wb);
+  } else {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int s = 16 * un.u + 2 * e;
-    wa[e] = p.w[kind] && s < p.dim ? p.w[kind][un.element(s)] : 1.0f;
-    wb[e] = p.w[kind] && s + 1 < p.dim ? p.w[kind][un.element(s + 1)] : 1.0f;
+    for (int e = 0; e < 8; ++e) wa[e] = wb[e] = 1.0f;
   }
 }
 
-template <typename T, int L, int HS>
+template <typename T, bool VEC, int L, int HS>
 __global__ void __launch_bounds__(256) norm_rope_kernel(NormRope p) {
   unsigned it = blockIdx.x * (256 / L) + threadIdx.x / L;
   const int kind = it >= p.items[0];
   if (kind) it -= p.items[0];
   if (it >= p.items[kind]) return;             // whole heads leave: the sum below is over the lanes of one
-  const Unit un = {(int)threadIdx.x % L, p.dim, p.rot, !p.interleaved, p.vec};
+  const Unit<T, VEC> un = {(int)threadIdx.x % L, p.dim, p.rot, !p.interleaved};
   const unsigned token = it / p.groups[kind];
   const int h0 = (it - token * p.groups[kind]) * HS, b = token / p.len, i = token - b * p.len;
   const T* x = (const T*)p.x[kind] + b * p.xs[kind][0] + i * p.xs[kind][1];
   T* out = (T*)p.out[kind] + b * p.os[kind][0] + i * p.os[kind][1];
-  float va[HS][8], vb[HS][8], c[8], s[8], wa[8], wb[8];
+  typename Unit<T, VEC>::Raw raw[HS];
+  float c[8], s[8], wa[8], wb[8];
 #pragma unroll
   for (int h = 0; h < HS; ++h)
-    if (h0 + h < p.heads[kind]) un.load(x + (h0 + h) * p.xs[kind][2], va[h], vb[h]);
-  angles(p, un.u, p.pos ? p.pos[token] : p.start + i, c, s);
-  weights(p, un, kind, wa, wb);
+    if (h0 + h < p.heads[kind]) un.load(x + (h0 + h) * p.xs[kind][2], raw[h]);
+  angles<VEC>(p, un.u, p.pos ? p.pos[token] : p.start + i, c, s);
+  weights<VEC>(p, un.u, kind, wa, wb);
 #pragma unroll
   for (int h = 0; h < HS; ++h) {
-    if (h0 + h >= p.heads[kind]) break;
-    float (&a)[8] = va[h], (&bb)[8] = vb[h];
+    if (h0 + h >= p.heads[kind]) continue;
+    float a[8], bb[8];
+    un.pairs(raw[h], a, bb);
     if (p.norm) {
       float q = 0.0f;
 #pragma unroll
@@ -177,30 +188,32 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(NormRope p) {
   }
 }
 
-template <typename T, int L, int HS>
+template <typename T, bool VEC, int L, int HS>
 __global__ void __launch_bounds__(256) norm_rope_backward_kernel(NormRope p) {
   const int kind = (int)blockIdx.x >= p.blocks_q, block = blockIdx.x - (kind ? p.blocks_q : 0), nblocks = kind ? gridDim.x - p.blocks_q : p.blocks_q;
-  const Unit un = {(int)threadIdx.x % L, p.dim, p.rot, !p.interleaved, p.vec};
+  const Unit<T, VEC> un = {(int)threadIdx.x % L, p.dim, p.rot, !p.interleaved};
   float ga[8] = {}, gb[8] = {}, wa[8], wb[8];
-  weights(p, un, kind, wa, wb);
+  weights<VEC>(p, un.u, kind, wa, wb);
   for (unsigned it = block * (256 / L) + threadIdx.x / L; it < p.items[kind]; it += nblocks * (256 / L)) {
     const unsigned token = it / p.groups[kind];
     const int h0 = (it - token * p.groups[kind]) * HS, b = token / p.len, i = token - b * p.len;
     const T* x = (const T*)p.x[kind] + b * p.xs[kind][0] + i * p.xs[kind][1];
     const T* dy = (const T*)p.dy[kind] + b * p.ds[kind][0] + i * p.ds[kind][1];
     T* out = (T*)p.out[kind] + b * p.os[kind][0] + i * p.os[kind][1];
-    float xa[HS][8], xb[HS][8], da[HS][8], db[HS][8], c[8], s[8];
+    typename Unit<T, VEC>::Raw xr[HS], dr[HS];
+    float c[8], s[8];
 #pragma unroll
     for (int h = 0; h < HS; ++h)
       if (h0 + h < p.heads[kind]) {
-        un.load(dy + (h0 + h) * p.ds[kind][2], da[h], db[h]);
-        if (p.norm) un.load(x + (h0 + h) * p.xs[kind][2], xa[h], xb[h]);
+        un.load(dy + (h0 + h) * p.ds[kind][2], dr[h]);
+        if (p.norm) un.load(x + (h0 + h) * p.xs[kind][2], xr[h]);
       }
-    angles(p, un.u, p.pos ? p.pos[token] : p.start + i, c, s);
+    angles<VEC>(p, un.u, p.pos ? p.pos[token] : p.start + i, c, s);
 #pragma unroll
     for (int h = 0; h < HS; ++h) {
-      if (h0 + h >= p.heads[kind]) break;
-      float (&a)[8] = da[h], (&bb)[8] = db[h];
+      if (h0 + h >= p.heads[kind]) continue;
+      float a[8], bb[8];
+      un.pairs(dr[h], a, bb);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float t = a[e] * c[e] + bb[e] * s[e];
@@ -208,20 +221,22 @@ __global__ void __launch_bounds__(256) norm_rope_backward_kernel(NormRope p) {
         a[e] = t;
       }
       if (p.norm) {
+        float xa[8], xb[8];
+        un.pairs(xr[h], xa, xb);
         float q = 0.0f, d = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          q += xa[h][e] * xa[h][e] + xb[h][e] * xb[h][e];
-          d += a[e] * wa[e] * xa[h][e] + bb[e] * wb[e] * xb[h][e];
+          q += xa[e] * xa[e] + xb[e] * xb[e];
+          d += a[e] * wa[e] * xa[e] + bb[e] * wb[e] * xb[e];
         }
         const float r = 1.0f / sqrtf(over_lanes<L>(q) / (float)p.dim + p.eps);
         const float m = over_lanes<L>(d) / (float)p.dim * r * r;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          ga[e] += a[e] * xa[h][e] * r;
-          gb[e] += bb[e] * xb[h][e] * r;
-          a[e] = r * (a[e] * wa[e] - xa[h][e] * m);
-          bb[e] = r * (bb[e] * wb[e] - xb[h][e] * m);
+          ga[e] += a[e] * xa[e] * r;
+          gb[e] += bb[e] * xb[e] * r;
+          a[e] = r * (a[e] * wa[e] - xa[e] * m);
+          bb[e] = r * (bb[e] * wb[e] - xb[e] * m);
         }
       }
       un.store(out + (h0 + h) * p.os[kind][2], a, bb);
@@ -244,20 +259,21 @@ __global__ void __launch_bounds__(256) norm_rope_backward_kernel(NormRope p) {
 }
 
 // dw = the sum of the workgroups' partial sums; a workgroup takes 16 slots of the queries' (blockIdx.y = 0) or keys' weights
-__global__ void __launch_bounds__(256) norm_rope_join_kernel(NormRope p, float* dqw, float* dkw, int blocks_k, int width) {
+__global__ void __launch_bounds__(1024) norm_rope_join_kernel(NormRope p, float* dqw, float* dkw, int blocks_k, int width) {
   const int kind = blockIdx.y, col = blockIdx.x * 16 + (threadIdx.x & 15), blocks = kind ? blocks_k : p.blocks_q;
   float* to = kind ? dkw : dqw;
   if (!to) return;
-  __shared__ float sums[16][17];
+  __shared__ float sums[64][17];
   float v = 0.0f;
-  for (int r = threadIdx.x >> 4; r < blocks; r += 16) v += p.part[kind][(size_t)r * width + col];
+#pragma unroll 8
+  for (int r = threadIdx.x >> 4; r < blocks; r += 64) v += p.part[kind][(size_t)r * width + col];
   sums[threadIdx.x >> 4][threadIdx.x & 15] = v;
   __syncthreads();
   if (threadIdx.x >= 16 || col >= p.dim) return;
   v = 0.0f;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) v += sums[r][threadIdx.x];
-  const Unit un = {0, p.dim, p.rot, !p.interleaved, p.vec};
+  for (int r = 0; r < 64; ++r) v += sums[r][threadIdx.x];
+  const Unit<float, false> un = {0, p.dim, p.rot, !p.interleaved};
   to[un.element(col)] = v;
 }
 
@@ -283,12 +299,15 @@ NormRope common(const void* q, const void* k, const prism_norm_rope_desc& d) {
   return p;
 }
 
-bool sizes_fit_vectors(const prism_norm_rope_desc& d) { return d.head_dim % 8 == 0 && (d.interleaved || d.rot_dim % 16 == 0); }
+bool fits_vectors(const prism_norm_rope_desc& d) {
+  return d.head_dim % 8 == 0 && (d.interleaved || d.rot_dim % 16 == 0) && (((uintptr_t)d.inv_freq | (uintptr_t)d.q_weight | (uintptr_t)d.k_weight) & 15) == 0;
+}
 
-// Heads per lane: four share the sines of their token where that leaves the chip two waves per SIMD at least.
-int heads_per_lane(const prism_norm_rope_desc& d, int L) {
+// Heads per lane share the sines of their token: four (gradients: two, whose operands fill as many registers) where that leaves the chip four waves per SIMD.
+int heads_per_lane(const prism_norm_rope_desc& d, int L, int most) {
   const long long waves = (long long)d.batch * d.len * (d.q_heads + d.k_heads) * L / 64;
-  return waves >= 4 * 2048 ? 4 : 1;
+  while (most > 1 && waves < most * 4096ll) most /= 2;
+  return most;
 }
 
 void set_items(NormRope& p, const prism_norm_rope_desc& d, int HS) {
@@ -298,21 +317,24 @@ void set_items(NormRope& p, const prism_norm_rope_desc& d, int HS) {
   }
 }
 
-template <typename T, int L> void forward(NormRope& p, int HS, hipStream_t s) {
-  const dim3 grid((unsigned)(((unsigned long long)p.items[0] + p.items[1] + 256 / L - 1) / (256 / L)));
-  if (HS == 4) hipLaunchKernelGGL((norm_rope_kernel<T, L, 4>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((norm_rope_kernel<T, L, 1>), grid, dim3(256), 0, s, p);
+template <typename T, bool VEC, int L> void launch(NormRope& p, int HS, int blocks_k, bool back, hipStream_t s) {
+  const dim3 grid(back ? p.blocks_q + blocks_k : (unsigned)(((unsigned long long)p.items[0] + p.items[1] + 256 / L - 1) / (256 / L)));
+  void (*kernel)(NormRope) = back ? norm_rope_backward_kernel<T, VEC, L, 1> : norm_rope_kernel<T, VEC, L, 1>;
+  if constexpr (VEC) {
+    if (HS == 2) kernel = back ? norm_rope_backward_kernel<T, VEC, L, 2> : norm_rope_kernel<T, VEC, L, 2>;
+    else if (HS == 4) kernel = norm_rope_kernel<T, VEC, L, 4>;
+  }
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p);
 }
-template <typename T, int L> void backward(NormRope& p, int HS, int blocks_k, hipStream_t s) {
-  const dim3 grid(p.blocks_q + blocks_k);
-  if (HS == 4) hipLaunchKernelGGL((norm_rope_backward_kernel<T, L, 4>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((norm_rope_backward_kernel<T, L, 1>), grid, dim3(256), 0, s, p);
+template <typename T, bool VEC> void by_lanes(NormRope& p, int L, int HS, int blocks_k, bool back, hipStream_t s) {
+  if (L == 2) launch<T, VEC, 2>(p, HS, blocks_k, back, s);
+  else if (L == 4) launch<T, VEC, 4>(p, HS, blocks_k, back, s);
+  else if (L == 8) launch<T, VEC, 8>(p, HS, blocks_k, back, s);
+  else launch<T, VEC, 16>(p, HS, blocks_k, back, s);
 }
-template <typename T> void by_lanes(NormRope& p, int L, int HS, int blocks_k, bool back, hipStream_t s) {
-  if (L == 2) back ? backward<T, 2>(p, HS, blocks_k, s) : forward<T, 2>(p, HS, s);
-  else if (L == 4) back ? backward<T, 4>(p, HS, blocks_k, s) : forward<T, 4>(p, HS, s);
-  else if (L == 8) back ? backward<T, 8>(p, HS, blocks_k, s) : forward<T, 8>(p, HS, s);
-  else back ? backward<T, 16>(p, HS, blocks_k, s) : forward<T, 16>(p, HS, s);
+void by_type(NormRope& p, int dt, bool vec, int L, int HS, int blocks_k, bool back, hipStream_t s) {
+  if (dt == PRISM_F32) vec ? by_lanes<float, true>(p, L, HS, blocks_k, back, s) : by_lanes<float, false>(p, L, HS, blocks_k, back, s);
+  else vec ? by_lanes<__bf16, true>(p, L, HS, blocks_k, back, s) : by_lanes<__bf16, false>(p, L, HS, blocks_k, back, s);
 }
 
 }  // namespace
@@ -320,14 +342,14 @@ template <typename T> void by_lanes(NormRope& p, int L, int HS, int blocks_k, bo
 int launch_norm_rope(const void* q, const void* k, void* qo, void* ko, int dt, const prism_norm_rope_desc& d, hipStream_t s) {
   ProfScope prof(PK_NORM_ROPE, s);
   NormRope p = common(q, k, d);
-  const int size = dt == PRISM_F32 ? 4 : 2, L = lanes_of(d.head_dim), HS = heads_per_lane(d, L);
+  const int size = dt == PRISM_F32 ? 4 : 2, L = lanes_of(d.head_dim);
   p.out[0] = qo; p.out[1] = ko;
   strides(p.os[0], d.q_out); strides(p.os[1], d.k_out);
-  p.vec = sizes_fit_vectors(d) && (!d.q_heads || (whole_vectors(q, d.q, size) && whole_vectors(qo, d.q_out, size))) &&
+  const bool vec = fits_vectors(d) && (!d.q_heads || (whole_vectors(q, d.q, size) && whole_vectors(qo, d.q_out, size))) &&
           (!d.k_heads || (whole_vectors(k, d.k, size) && whole_vectors(ko, d.k_out, size)));
+  const int HS = vec ? heads_per_lane(d, L, 4) : 1;
   set_items(p, d, HS);
-  if (dt == PRISM_F32) by_lanes<float>(p, L, HS, 0, false, s);
-  else by_lanes<__bf16>(p, L, HS, 0, false, s);
+  by_type(p, dt, vec, L, HS, 0, false, s);
   return PRISM_OK;
 }
 
@@ -339,18 +361,21 @@ int launch_norm_rope_backward(const void* dqo, const void* dko, const void* q, c
                               const prism_norm_rope_desc& d, float* part, hipStream_t s) {
   ProfScope prof(PK_NORM_ROPE_BACKWARD, s);
   NormRope p = common(q, k, d);
-  const int size = dt == PRISM_F32 ? 4 : 2, L = lanes_of(d.head_dim), HS = heads_per_lane(d, L);
+  const int size = dt == PRISM_F32 ? 4 : 2, L = lanes_of(d.head_dim);
   p.dy[0] = dqo; p.dy[1] = dko;
   strides(p.ds[0], d.q_out); strides(p.ds[1], d.k_out);
   p.out[0] = dq; p.out[1] = dk;
   strides(p.os[0], d.dq); strides(p.os[1], d.dk);
-  p.vec = sizes_fit_vectors(d) &&
+  const bool vec = fits_vectors(d) &&
           (!d.q_heads || ((!d.norm || whole_vectors(q, d.q, size)) && whole_vectors(dqo, d.q_out, size) && whole_vectors(dq, d.dq, size))) &&
           (!d.k_heads || ((!d.norm || whole_vectors(k, d.k, size)) && whole_vectors(dko, d.k_out, size) && whole_vectors(dk, d.dk, size)));
+  const int HS = vec ? heads_per_lane(d, L, 2) : 1;
   set_items(p, d, HS);
+  // workgroups in proportion to the work of queries and keys
+  const long long slots = 256 / L, all = (long long)p.items[0] + p.items[1];
   auto blocks = [&](int kind) {
-    const long long n = ((long long)p.items[kind] + 256 / L - 1) / (256 / L);
-    return (int)(n < NR_MAX_BLOCKS ? n : NR_MAX_BLOCKS);
+    const long long need = (p.items[kind] + slots - 1) / slots, share = all ? (NR_MAX_BLOCKS * (long long)p.items[kind] + all - 1) / all : 0;
+    return (int)(need < share ? need : share);
   };
   p.blocks_q = blocks(0);
   const int blocks_k = blocks(1), width = 16 * L;
@@ -358,9 +383,8 @@ int launch_norm_rope_backward(const void* dqo, const void* dko, const void* q, c
     p.part[0] = dqw ? part : nullptr;
     p.part[1] = dkw ? part + (size_t)NR_MAX_BLOCKS * width : nullptr;
   }
-  if (dt == PRISM_F32) by_lanes<float>(p, L, HS, blocks_k, true, s);
-  else by_lanes<__bf16>(p, L, HS, blocks_k, true, s);
-  if (d.norm && (dqw || dkw)) hipLaunchKernelGGL(norm_rope_join_kernel, dim3(L, 2), dim3(256), 0, s, p, dqw, dkw, blocks_k, width);
+  by_type(p, dt, vec, L, HS, blocks_k, true, s);
+  if (d.norm && (dqw || dkw)) hipLaunchKernelGGL(norm_rope_join_kernel, dim3(L, 2), dim3(1024), 0, s, p, dqw, dkw, blocks_k, width);
   return PRISM_OK;
 }
 
