@@ -5,6 +5,7 @@ The library must have been built (python -m paper_2601_22137_amd.build); there i
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -103,12 +104,12 @@ def lib():
         L.prism_run_grouped.argtypes = [i, ctypes.POINTER(Group), i, i, i, i, i, i, u64, dbl, vp, ctypes.POINTER(Options)]
         L.prism_run_grouped_from.argtypes = [i, ctypes.POINTER(Group), vp, i, i, i, i, i, i, u64, dbl, vp, ctypes.POINTER(Options)]
         L.prism_dropout.argtypes = [vp, vp, vp, ctypes.c_int64, i, dbl, u64, ctypes.c_uint32, vp]
-        L.prism_qk_norm_rope.argtypes = [vp, vp, vp, vp, i, ctypes.POINTER(NormRopeDesc), vp]
-        L.prism_qk_norm_rope_backward.argtypes = [vp] * 8 + [i, ctypes.POINTER(NormRopeDesc), vp]
-        L.prism_norm_rope_workspace_bytes.argtypes = [i, ctypes.POINTER(NormRopeDesc), ctypes.POINTER(ctypes.c_size_t)]
-        L.prism_attention.argtypes = [vp] * 5 + [i, ctypes.POINTER(AttentionDesc), vp]
-        L.prism_attention_backward.argtypes = [vp] * 9 + [i, ctypes.POINTER(AttentionDesc), vp]
-        L.prism_attention_workspace_bytes.argtypes = [i, ctypes.POINTER(AttentionDesc), i, ctypes.POINTER(ctypes.c_size_t)]
+        L.prism_qk_norm_rope.argtypes = [vp, vp, vp, vp, i, vp, vp]
+        L.prism_qk_norm_rope_backward.argtypes = [vp] * 8 + [i, vp, vp]
+        L.prism_norm_rope_workspace_bytes.argtypes = [i, vp, ctypes.POINTER(ctypes.c_size_t)]
+        L.prism_attention.argtypes = [vp] * 5 + [i, vp, vp]
+        L.prism_attention_backward.argtypes = [vp] * 9 + [i, vp, vp]
+        L.prism_attention_workspace_bytes.argtypes = [i, vp, i, ctypes.POINTER(ctypes.c_size_t)]
         L.prism_sketch.argtypes = [vp, i, i, u64, i, i, vp]
         L.prism_gauss_parts.argtypes = [ctypes.c_uint32, ctypes.c_uint32, vp, vp, vp, vp]
         L.prism_chain_product.argtypes = [vp, vp, vp, i, i, i, vp]
@@ -325,53 +326,68 @@ def read_reports(infos):
 # ---- operators of a transformer layer ----
 #
 # Arrays of heads are tensors [batch, token, head, dim]; dim has to be contiguous, the other strides are free (views into one
-# projection, transposed views).
+# projection, transposed views).  These calls take a few microseconds on the GPU when they are small, so their descriptions are
+# packed in one step (the layouts of prism_norm_rope_desc and prism_attention_desc) and every tensor is asked once.
 
-def _same(ref, *ts):
-    """Each t (None excepted) a CUDA tensor on ref's device."""
-    for t in ts:
-        if t is not None and not (t.is_cuda and t.device == ref.device):
-            raise PrismError("expected CUDA tensors on one device")
+_NORM_ROPE = struct.Struct("@9i2f4P18qPN")
+_ATTENTION = struct.Struct("@7i2f5P24qPN")
+_NO_STRIDES = (0, 0, 0)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _heads(t, name, dtype, shape=None):
-    if t.dim() != 4 or t.dtype != dtype or (t.numel() > 0 and t.shape[3] > 1 and t.stride(3) != 1) or any(s < 0 for s in t.stride()):
-        raise PrismError("%s: expected [batch, token, head, dim] of one dtype with contiguous dim" % name)
-    if shape is not None and tuple(t.shape) != tuple(shape):
+def _device(t):
+    """Index of a CUDA tensor's device."""
+    i = t.get_device()
+    if i < 0:
+        raise PrismError("expected CUDA tensors")
+    return i
+
+
+def _on(dev, call, *args):
+    """The library call on that device's current stream (passed last); the caller's device stays the current one."""
+    if torch.cuda.current_device() == dev:
+        _check(call(*args, _raw_stream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(call(*args, _raw_stream(dev)))
+
+
+def _heads(t, name, dtype, dev, shape):
+    """Strides of batch, token and head of an array of heads."""
+    if t.shape != shape:
         raise PrismError("%s: expected shape %s" % (name, tuple(shape)))
-    return t
+    s = t.stride()
+    if t.dtype is not dtype or t.get_device() != dev or (s[3] != 1 and shape[3] > 1):
+        raise PrismError("%s: expected the dtype and device of the other arrays, and contiguous dim" % name)
+    return s[:3]
 
 
-def _strides(t):
-    return Strides(t.stride(0), t.stride(1), t.stride(2)) if t is not None else Strides(0, 0, 0)
-
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
-
-
-def _plain(t, name, dtype, shape):
-    """The pointer of an optional contiguous array."""
+def _plain(t, name, dtype, dev, shape):
+    """The address of an optional contiguous array."""
     if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise PrismError("%s: expected a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
+        return 0
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise PrismError("%s: expected a contiguous %s tensor of shape %s on the device of the others" % (name, dtype, tuple(shape)))
     return t.data_ptr()
 
 
-def _stream_of(t):
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+def _given(workspace, dev):
+    if workspace is None:
+        return 0, 0
+    if workspace.get_device() != dev:
+        raise PrismError("workspace: expected a tensor on the device of the others")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def dropout(x, p, seed, offset=0, residual=None, out=None):
     """residual + dropout(x): every element is kept with probability 1 - p (rounded to 16 bits) and then divided by it.  The mask is a function
     of (seed, offset, index) and is not stored: the gradient with respect to x is dropout(dy, p, seed, offset).  out may be x or residual."""
     y = torch.empty_like(x) if out is None else out
-    _same(x, x, residual, y)
-    if any(t is not None and (t.shape != x.shape or t.dtype != x.dtype or not t.is_contiguous()) for t in (x, residual, y)):
-        raise PrismError("expected contiguous tensors of one shape and dtype")
-    with torch.cuda.device(x.device):
-        _check(lib().prism_dropout(x.data_ptr(), _ptr(residual), y.data_ptr(), x.numel(), _dtype_code(x), p, seed, offset, _stream_of(x)))
+    dev = _device(x)
+    for t in (x, y) if residual is None else (x, y, residual):
+        if t.shape != x.shape or t.dtype is not x.dtype or t.get_device() != dev or not t.is_contiguous():
+            raise PrismError("expected contiguous tensors of one shape, dtype and device")
+    _on(dev, lib().prism_dropout, x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(), _dtype_code(x), p, seed, offset)
     return y
 
 
@@ -401,28 +417,39 @@ def rope_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_l
     return torch.tensor(f, dtype=torch.float32, device=device), float(scale)
 
 
-def _norm_rope_desc(q, k, positions, start, inv_freq, q_weight, k_weight, norm, interleaved, scale, eps):
+def _norm_rope_desc(q, k, results, grads, inv_freq, positions, start, q_weight, k_weight, norm, interleaved, scale, eps, workspace):
+    """(a tensor of the call, its device, the packed description).  results: the arrays of the forward results (or their gradients), grads: those of the backward ones."""
     some = q if q is not None else k
-    if some is None:
-        raise PrismError("expected queries or keys")
-    _same(some, q, k, positions, inv_freq, q_weight, k_weight)
-    if some.dim() != 4:
-        raise PrismError("expected [batch, token, head, dim]")
-    b, n, _, d = some.shape
-    o = NormRopeDesc()
-    o.batch, o.len, o.head_dim = b, n, d
-    for t, name in ((q, "q"), (k, "k")):
+    if some is None or some.dim() != 4:
+        raise PrismError("expected queries or keys [batch, token, head, dim]")
+    dev, dtype, (b, n, h, d) = _device(some), some.dtype, some.shape
+    heads, strides = [0, 0], []
+    for x, t in enumerate((q, k)):
         if t is not None:
-            _heads(t, name, some.dtype, (b, n, t.shape[2] if t.dim() == 4 else 0, d))
-            setattr(o, name + "_heads", t.shape[2])
-            setattr(o, name, _strides(t))
-    o.rot_dim = 2 * inv_freq.numel() if inv_freq is not None else 0
-    o.norm, o.interleaved, o.start, o.eps, o.scale = int(bool(norm)), int(bool(interleaved)), start, eps, scale
-    o.positions = _plain(positions, "positions", torch.int32, (b, n))
-    o.inv_freq = _plain(inv_freq, "inv_freq", torch.float32, (o.rot_dim // 2,))
-    o.q_weight = _plain(q_weight, "q_weight", torch.float32, (d,))
-    o.k_weight = _plain(k_weight, "k_weight", torch.float32, (d,))
-    return some, o
+            if t.dim() != 4:
+                raise PrismError("expected [batch, token, head, dim]")
+            heads[x] = t.shape[2]
+    for arrays, names in (((q, k), ("q", "k")), (results, ("q_out", "k_out")), (grads, ("dq", "dk"))):
+        for x, t in enumerate(arrays):
+            if (t is None) != ((q, k)[x] is None) and arrays is not _NONE:
+                raise PrismError("%s: goes with its input" % names[x])
+            strides += _NO_STRIDES if t is None else _heads(t, names[x], dtype, dev, (b, n, heads[x], d))
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    return some, dev, _NORM_ROPE.pack(
+        b, n, heads[0], heads[1], d, rot, 1 if norm else 0, 1 if interleaved else 0, start, eps, scale, _plain(positions, "positions", torch.int32, dev, (b, n)),
+        _plain(inv_freq, "inv_freq", torch.float32, dev, (rot // 2,)), _plain(q_weight, "q_weight", torch.float32, dev, (d,)),
+        _plain(k_weight, "k_weight", torch.float32, dev, (d,)), *strides, *_given(workspace, dev))
+
+
+_NONE = (None, None)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _new(t):
+    return None if t is None else t.new_empty(t.shape)
 
 
 def qk_norm_rope(q, k, inv_freq=None, positions=None, start=0, q_weight=None, k_weight=None, norm=True, interleaved=False, scale=1.0, eps=1e-6,
@@ -430,17 +457,9 @@ def qk_norm_rope(q, k, inv_freq=None, positions=None, start=0, q_weight=None, k_
     """RMS norm of every head of q and k [batch, token, head, dim] times q_weight / k_weight (fp32 [dim], None: ones), then the rotation of
     its first 2 * len(inv_freq) entries by positions (int32 [batch, token], None: from `start` on).  norm=False: rotation only; inv_freq=None: norm only.
     q or k may be None.  out: the tensors for the results (q and k themselves are allowed).  Returns (q, k)."""
-    some, o = _norm_rope_desc(q, k, positions, start, inv_freq, q_weight, k_weight, norm, interleaved, scale, eps)
-    qo, ko = out if out is not None else tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) if t is not None else None for t in (q, k))
-    _same(some, qo, ko)
-    for t, to, name in ((q, qo, "q_out"), (k, ko, "k_out")):
-        if (t is None) != (to is None):
-            raise PrismError("%s: results go with inputs" % name)
-        if to is not None:
-            _heads(to, name, some.dtype, t.shape)
-            setattr(o, name, _strides(to))
-    with torch.cuda.device(some.device):
-        _check(lib().prism_qk_norm_rope(_ptr(q), _ptr(k), _ptr(qo), _ptr(ko), _dtype_code(some), ctypes.byref(o), _stream_of(some)))
+    qo, ko = (_new(q), _new(k)) if out is None else out
+    some, dev, desc = _norm_rope_desc(q, k, (qo, ko), _NONE, inv_freq, positions, start, q_weight, k_weight, norm, interleaved, scale, eps, None)
+    _on(dev, lib().prism_qk_norm_rope, _ptr(q), _ptr(k), _ptr(qo), _ptr(ko), _dtype_code(some), desc)
     return qo, ko
 
 
@@ -448,76 +467,55 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, inv_freq=None, positions=None, s
                           scale=1.0, eps=1e-6, out=None, workspace=None):
     """Gradients of qk_norm_rope from those of its results: (dq, dk, dq_weight, dk_weight), the last two fp32 [dim], or None without the norm.
     q and k are the inputs of the forward call.  out: tensors for dq and dk."""
-    some, o = _norm_rope_desc(q, k, positions, start, inv_freq, q_weight, k_weight, norm, interleaved, scale, eps)
-    dq, dk = out if out is not None else tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) if t is not None else None for t in (q, k))
-    _same(some, dq_out, dk_out, dq, dk, workspace)
-    weights = [None, None]
-    for x, (t, g, to, name) in enumerate(((q, dq_out, dq, "q"), (k, dk_out, dk, "k"))):
-        if (t is None) != (to is None) or (t is None) != (g is None):
-            raise PrismError("%s: gradients go with inputs" % name)
-        if t is not None:
-            setattr(o, name + "_out", _strides(_heads(g, "d%s_out" % name, some.dtype, t.shape)))
-            setattr(o, "d" + name, _strides(_heads(to, "d" + name, some.dtype, t.shape)))
-            if norm:
-                weights[x] = (torch.zeros if t.numel() == 0 else torch.empty)(t.shape[3], dtype=torch.float32, device=t.device)
-    if workspace is not None:
-        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    with torch.cuda.device(some.device):
-        _check(lib().prism_qk_norm_rope_backward(_ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(dq), _ptr(dk), _ptr(weights[0]), _ptr(weights[1]),
-                                                 _dtype_code(some), ctypes.byref(o), _stream_of(some)))
-    return dq, dk, weights[0], weights[1]
+    dq, dk = (_new(q), _new(k)) if out is None else out
+    some, dev, desc = _norm_rope_desc(q, k, (dq_out, dk_out), (dq, dk), inv_freq, positions, start, q_weight, k_weight, norm, interleaved, scale, eps, workspace)
+    dqw, dkw = [t.new_zeros(t.shape[3], dtype=torch.float32) if t.numel() == 0 else t.new_empty(t.shape[3], dtype=torch.float32)
+                if norm and t is not None else None for t in (q, k)]
+    _on(dev, lib().prism_qk_norm_rope_backward, _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(dq), _ptr(dk), _ptr(dqw), _ptr(dkw), _dtype_code(some), desc)
+    return dq, dk, dqw, dkw
 
 
-def _attention_desc(q, k, v, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace):
-    _same(q, q, k, v, slopes, prefix, k_lens, q_doc, k_doc, workspace)
-    _heads(q, "q", q.dtype)
-    b, n, hq, d = q.shape
-    _heads(k, "k", q.dtype)
-    m, hk = k.shape[1], k.shape[2]
-    _heads(k, "k", q.dtype, (b, m, hk, d))
-    _heads(v, "v", q.dtype, (b, m, hk, d))
-    o = AttentionDesc()
-    o.batch, o.q_len, o.k_len, o.q_heads, o.k_heads, o.head_dim = b, n, m, hq, hk, d
-    o.causal, o.softcap, o.scale = int(bool(causal)), softcap, d ** -0.5 if scale is None else scale
-    o.slopes = _plain(slopes, "slopes", torch.float32, (hq,))
-    o.prefix = _plain(prefix, "prefix", torch.int32, (b,))
-    o.k_lens = _plain(k_lens, "k_lens", torch.int32, (b,))
-    o.q_doc = _plain(q_doc, "q_doc", torch.int32, (b, n))
-    o.k_doc = _plain(k_doc, "k_doc", torch.int32, (b, m))
-    o.q, o.k, o.v = _strides(q), _strides(k), _strides(v)
-    if workspace is not None:
-        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    return o
+def _attention_desc(q, k, v, out, back, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace):
+    """(device, the packed description).  back: dout, dq, dk, dv, or ()."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise PrismError("expected [batch, token, head, dim]")
+    dev, dtype, rows, cells = _device(q), q.dtype, q.shape, k.shape
+    b, n, hq, d = rows
+    m, hk = cells[1], cells[2]
+    if cells[0] != b or cells[3] != d:
+        raise PrismError("k: expected the batch and dim of q")
+    strides = _heads(q, "q", dtype, dev, rows) + _heads(k, "k", dtype, dev, cells) + _heads(v, "v", dtype, dev, cells) + _heads(out, "out", dtype, dev, rows)
+    if back:
+        dout, dq, dk, dv = back
+        strides += _heads(dout, "dout", dtype, dev, rows) + _heads(dq, "dq", dtype, dev, rows) + _heads(dk, "dk", dtype, dev, cells) + _heads(dv, "dv", dtype, dev, cells)
+    else:
+        strides += 4 * _NO_STRIDES
+    i32 = torch.int32
+    return dev, _ATTENTION.pack(
+        b, n, m, hq, hk, d, 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap, _plain(slopes, "slopes", torch.float32, dev, (hq,)),
+        _plain(prefix, "prefix", i32, dev, (b,)), _plain(k_lens, "k_lens", i32, dev, (b,)), _plain(q_doc, "q_doc", i32, dev, (b, n)),
+        _plain(k_doc, "k_doc", i32, dev, (b, m)), *strides, *_given(workspace, dev))
 
 
 def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, out=None, workspace=None):
     """Attention of q [batch, n, q_heads, dim] over k and v [batch, m, k_heads, dim].  scores = scale q.k (scale None: dim^-1/2), capped by softcap tanh(. / softcap),
     less slopes[head] * distance.  Masks: causal (the last query sits at the last key), prefix [batch] (keys that all see), k_lens [batch] (keys there are), q_doc / k_doc
     [batch, n] / [batch, m] (documents; negative: padding).  Returns (out, lse); a query that sees nothing gets 0 and -inf."""
-    o = _attention_desc(q, k, v, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace)
-    b, n, hq, d = q.shape
-    y = torch.empty((b, n, hq, d), dtype=q.dtype, device=q.device) if out is None else out
-    _same(q, y)
-    o.out = _strides(_heads(y, "out", q.dtype, q.shape))
-    lse = torch.empty((b, hq, n), dtype=torch.float32, device=q.device)
-    with torch.cuda.device(q.device):
-        _check(lib().prism_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), y.data_ptr(), lse.data_ptr(), _dtype_code(q), ctypes.byref(o), _stream_of(q)))
+    y = q.new_empty(q.shape) if out is None else out
+    dev, desc = _attention_desc(q, k, v, y, (), scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace)
+    lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32)
+    _on(dev, lib().prism_attention, q.data_ptr(), k.data_ptr(), v.data_ptr(), y.data_ptr(), lse.data_ptr(), _dtype_code(q), desc)
     return y, lse
 
 
 def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None,
                        grads=None, workspace=None):
     """(dq, dk, dv) from dout; out and lse as attention() returned them for the same arguments.  grads: tensors for the three results."""
-    o = _attention_desc(q, k, v, scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace)
-    make = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)   # noqa: E731
-    dq, dk, dv = grads if grads is not None else (make(q), make(k), make(v))
-    _same(q, dout, out, lse, dq, dk, dv)
-    o.out, o.dout = _strides(_heads(out, "out", q.dtype, q.shape)), _strides(_heads(dout, "dout", q.dtype, q.shape))
-    o.dq, o.dk, o.dv = _strides(_heads(dq, "dq", q.dtype, q.shape)), _strides(_heads(dk, "dk", q.dtype, k.shape)), _strides(_heads(dv, "dv", q.dtype, v.shape))
-    _plain(lse, "lse", torch.float32, (q.shape[0], q.shape[2], q.shape[1]))
-    with torch.cuda.device(q.device):
-        _check(lib().prism_attention_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), dq.data_ptr(),
-                                              dk.data_ptr(), dv.data_ptr(), _dtype_code(q), ctypes.byref(o), _stream_of(q)))
+    dq, dk, dv = (q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)) if grads is None else grads
+    dev, desc = _attention_desc(q, k, v, out, (dout, dq, dk, dv), scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc, workspace)
+    _plain(lse, "lse", torch.float32, dev, (q.shape[0], q.shape[2], q.shape[1]))
+    _on(dev, lib().prism_attention_backward, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+        dv.data_ptr(), _dtype_code(q), desc)
     return dq, dk, dv
 
 

@@ -419,7 +419,7 @@ def test_attention_other_stream_and_given_workspace(prism):
         out, _ = prism.attention(q, k, v)
     s.synchronize()
     assert torch.equal(out, ref)
-    o = prism._attention_desc(q, k, v, None, False, 0.0, None, None, None, None, None, None)
+    o = prism.AttentionDesc.from_buffer_copy(prism._attention_desc(q, k, v, q, (), None, False, 0.0, None, None, None, None, None, None)[1])
     need = ctypes.c_size_t(0)
     assert prism.lib().prism_attention_workspace_bytes(prism.F32, ctypes.byref(o), 0, ctypes.byref(need)) == prism.OK and need.value > 0
     ws = torch.empty(need.value, dtype=torch.uint8, device="cuda")
@@ -487,7 +487,7 @@ def test_attention_refusals(prism):
     with pytest.raises(prism.PrismError):
         prism.attention_backward(out, q, k, k, out, lse[:, :, :2])
     L = prism.lib()
-    o = prism._attention_desc(q, k, k, None, False, 0.0, None, None, None, None, None, None)
+    o = prism.AttentionDesc.from_buffer_copy(prism._attention_desc(q, k, k, q, (), None, False, 0.0, None, None, None, None, None, None)[1])
     assert L.prism_attention(q.data_ptr(), k.data_ptr(), None, q.data_ptr(), None, prism.F32, ctypes.byref(o), None) == prism.EINVAL
     assert L.prism_attention(q.data_ptr(), k.data_ptr(), k.data_ptr(), q.data_ptr(), None, 9, ctypes.byref(o), None) == prism.EINVAL
     o.q_heads = 3
