@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
     float top = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      s[kb] = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
+      s[kb] = rows_by_rows<T, DP>(kt, 32 * kb, qf, p.dim, lane);
       scores<T>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
       if (need) {
 #pragma unroll
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
         s[kb][e] = __builtin_amdgcn_exp2f(s[kb][e] * mul - m);
         l += s[kb][e];
       }
-      columns_by<T, DP>(acc, vt, 32 * kb, s[kb], lane);
+      columns_by<T, DP>(acc, vt, 32 * kb, s[kb], p.dim, lane);
     }
   }
   l += other_half(l);
@@ -156,9 +156,10 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
   Chunks<T, DP, KT> kat, vat;
+  if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole) {
-    kat.set(tid, 1, p.ks[1], 0);
-    vat.set(tid, 1, p.vs[1], 0);
+    kat.set(tid, 1, p.ks[1], 0, p.dim);
+    vat.set(tid, 1, p.vs[1], 0, p.dim);
   }
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
   auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, bool hidden, char* to) {
@@ -341,35 +342,195 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   finish<T, DP>(p, acc, m, sum, split, pair, b, ie, kh * p.G + re - ie * p.G, re, h);
 }
 
-// The parts of a row's keys joined; a wave takes a row
-template <typename T> __global__ void __launch_bounds__(256) attention_join_kernel(Attn p) {
-  const long long rows = (long long)p.batch * p.hk * p.R, row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int lane = threadIdx.x & 63;
-  float top = -3.4e38f, sum = 0.0f, o[2] = {0.0f, 0.0f};
-  for (int s = 0; s < p.nsplit; ++s) top = fmaxf(top, p.part_ml[2 * (s * rows + row)]);
-  for (int s = 0; s < p.nsplit; ++s) {
-    const float m = p.part_ml[2 * (s * rows + row)], l = p.part_ml[2 * (s * rows + row) + 1];
-    if (l == 0.0f) continue;                     // nothing was written for it
-    const float f = __builtin_amdgcn_exp2f(m - top);
-    sum += l * f;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-      if (lane + 64 * x < p.dim) o[x] += p.part[(s * rows + row) * p.dim + lane + 64 * x] * f;
+// Few rows (32 of a pair at most, as when single tokens are generated for a group of heads): the time is that of reading the keys and values once.  Every wave
+// takes blocks of 32 keys of its own, with no barrier between them, through its own part of LDS (as an operand straight from memory every load of keys would touch 32 lines):
+// the keys are read into registers at once, which makes room for the next block's, the values lie in two blocks.  The waves' results are joined in LDS.
+template <int DP, bool MOD>
+__global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {
+  typedef __bf16 T;
+  using L = Lds<T, DP>;
+  constexpr int STEPS = L::STEPS, TB = 32 * L::RB, TD = DP / 32, LOADS = 32 * L::CPR / 64, LD = DP + 4;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys, and two blocks of values of each wave; at the end [wave][32][LD] floats
+  __shared__ float ml[NW][32][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
+  const int id = place(blockIdx.x, gridDim.x), split = id % p.nsplit, pair = id / p.nsplit, b = pair / p.hk, kh = pair - b * p.hk;
+  const int keys = keys_of(p, b);
+  const Row w = row_of(p, b, kh, r, keys);
+  const Limits lim = limits_of(p, w, r);
+  const int blocks = (lim.last + 32) / 32, per = (blocks + p.nsplit - 1) / p.nsplit, b0 = split * per, b1 = min(blocks, b0 + per);
+  Frag<T, DP> qf, kf;
+  {
+    const int i = r / p.G;
+    load_row<T, DP>(qf, true, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + (kh * p.G + r - i * p.G) * p.qs[2]);
   }
-  const int pair = (int)(row / p.R), r = (int)(row - (long long)pair * p.R), b = pair / p.hk, kh = pair - b * p.hk, i = r / p.G, g = r - i * p.G;
-  T* to = (T*)p.out + b * p.os[0] + i * p.os[1] + (kh * p.G + g) * p.os[2];
+  const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
+  const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
+  char* mine = smem + wave * 3 * TB;
+  // keys past the end: the last one again, masked
+  auto issue = [&](int block, const T* base, long long stride, char* to) {
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
-    if (lane + 64 * x < p.dim) to[lane + 64 * x] = (T)(sum == 0.0f ? 0.0f : o[x] / sum);
-  if (p.lse && lane == 0) p.lse[((long long)b * p.hq + kh * p.G + g) * p.n + i] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.0f / LOG2E);
+    for (int u = 0; u < LOADS; ++u) {
+      const int x = u * 64 + lane, row = x / L::CPR, c = (x % L::CPR) ^ L::swizzle(row);
+      const T* from = base + (long long)min(block * 32 + row, keys - 1) * stride + c * L::EPC;
+      __builtin_amdgcn_global_load_lds((gptr_t)(c * L::EPC < p.dim ? (const void*)from : (const void*)zero_page), (lptr_t)(to + u * 1024), 16, 0, 0);
+    }
+  };
+  f32x16 acc[TD];
+#pragma unroll
+  for (int t = 0; t < TD; ++t) acc[t] = (f32x16){};
+  float m = -3.4e38f, l = 0.0f;
+  const bool cap = MOD && p.cap > 0.0f, bias = MOD && p.slopes != nullptr;
+  const float mul = MOD ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E;
+  int buf = 0;
+  if (b0 + wave < b1) {
+    issue(b0 + wave, kbase, p.ks[1], mine);
+    issue(b0 + wave, vbase, p.vs[1], mine + TB);
+  }
+  for (int block = b0 + wave; block < b1; block += NW, buf ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) kf[x] = lds_read16(lds_address(mine) + r * L::RB + (((2 * x + h) ^ L::swizzle(r)) << 4));
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the keys are in registers, their place is free
+    __builtin_amdgcn_sched_barrier(0);
+    if (block + NW < b1) {
+      issue(block + NW, kbase, p.ks[1], mine);
+      issue(block + NW, vbase, p.vs[1], mine + TB + (buf ^ 1) * TB);
+    }
+    f32x16 s = {};
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) s = mma<T>(kf[x], qf[x], s);
+    const int j0 = block * 32 + 4 * h;
+    if constexpr (MOD) scores<T>(p, s, w, j0, cap, bias, in, out);
+    if (block * 32 + 31 > lim.first) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = j0 + 8 * (e >> 2) + (e & 3) <= w.last ? s[e] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = max_of(top, s[e]);
+    top *= mul;
+    if (__any(top > m + 8.0f)) {
+      const float to = fmaxf(m, fmaxf(top, other_half(top))), f = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < TD; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] *= f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = __builtin_amdgcn_exp2f(s[e] * mul - m);
+      l += s[e];
+    }
+    columns_by<T, DP>(acc, mine + TB + buf * TB, 0, s, DP, lane);
+  }
+  l += other_half(l);
+  __syncthreads();
+  float* all = (float*)smem;
+#pragma unroll
+  for (int t = 0; t < TD; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = acc[t][4 * g + e];
+      *(f32x4*)&all[(wave * 32 + r) * LD + 32 * t + 8 * g + 4 * h] = v;
+    }
+  if (h == 0) { ml[wave][r][0] = m; ml[wave][r][1] = l; }
+  __syncthreads();
+  for (int x = tid; x < p.R * (DP / 4); x += NT) {
+    const int row = x / (DP / 4), d = (x % (DP / 4)) * 4;
+    float top = -3.4e38f, sum = 0.0f;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) top = fmaxf(top, ml[q][row][0]);
+    f32x4 v = {};
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      const float f = __builtin_amdgcn_exp2f(ml[q][row][0] - top);
+      sum += ml[q][row][1] * f;
+      if (ml[q][row][1] != 0.0f) v += *(const f32x4*)&all[(q * 32 + row) * LD + d] * f;
+    }
+    const int i = row / p.G, head = kh * p.G + row - i * p.G;
+    if (p.nsplit > 1) {
+      const long long at = ((long long)split * p.batch * p.hk + pair) * p.R + row;
+      if (d < p.dim) *(f32x4*)(p.part + at * p.dim + d) = v;
+      if (d == 0) { p.part_ml[2 * at] = top; p.part_ml[2 * at + 1] = sum; }
+    } else {
+      if (d < p.dim) store4<T>((T*)p.out + b * p.os[0] + i * p.os[1] + head * p.os[2] + d, v * (sum == 0.0f ? 0.0f : 1.0f / sum), true, 4);
+      if (d == 0 && p.lse) p.lse[((long long)b * p.hq + head) * p.n + i] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.0f / LOG2E);
+    }
+  }
 }
 
-template <typename T, int DP> int launch(Attn& p, hipStream_t s) {
-  constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
+// The parts of a row's keys (64 at most) joined.  MANY: by a workgroup, whose waves take every fourth part; else (eight at most) by a wave.  Nothing is waited for before
+// all parts of a wave are on their way.
+template <typename T, bool MANY> __global__ void __launch_bounds__(256) attention_join_kernel(Attn p) {
+  constexpr int EVERY = MANY ? NW : 1, PARTS = MANY ? 16 : 8;
+  __shared__ float other[MANY ? NW : 1][128];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long rows = (long long)p.batch * p.hk * p.R, row = MANY ? blockIdx.x : (long long)blockIdx.x * NW + wave;
+  if (row >= rows) return;
+  const int first = MANY ? wave : 0;
+  float m = -3.4e38f, l = 0.0f;
+  if (lane < p.nsplit) {
+    m = p.part_ml[2 * (lane * rows + row)];
+    l = p.part_ml[2 * (lane * rows + row) + 1];
+  }
+  float v[PARTS][2];
+#pragma unroll
+  for (int s = 0; s < PARTS; ++s)
+    if (first + EVERY * s < p.nsplit)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (lane + 64 * x < p.dim) v[s][x] = p.part[((first + EVERY * s) * rows + row) * p.dim + lane + 64 * x];
+  float top = m;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+  const float f = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - top);   // 0 too where nothing was written
+  float sum = l * f, o[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+#pragma unroll
+  for (int s = 0; s < PARTS; ++s) {
+    const float fs = __shfl(f, (first + EVERY * s) & 63);
+    if (first + EVERY * s < p.nsplit && fs != 0.0f)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) o[x] += v[s][x] * fs;
+  }
+  const int pair = (int)(row / p.R), r = (int)(row - (long long)pair * p.R), b = pair / p.hk, kh = pair - b * p.hk, i = r / p.G, head = kh * p.G + r - i * p.G;
+  T* to = (T*)p.out + b * p.os[0] + i * p.os[1] + head * p.os[2];
+  if constexpr (MANY) {
+    other[wave][lane] = o[0];
+    other[wave][lane + 64] = o[1];
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d < p.dim) to[d] = (T)(sum == 0.0f ? 0.0f : (other[0][d] + other[1][d] + other[2][d] + other[3][d]) / sum);
+    if (d != 0) return;
+  } else {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      if (lane + 64 * x < p.dim) to[lane + 64 * x] = (T)(sum == 0.0f ? 0.0f : o[x] / sum);
+    if (lane != 0) return;
+  }
+  if (p.lse) p.lse[((long long)b * p.hq + head) * p.n + i] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.0f / LOG2E);
+}
+
+template <typename T, int DP> int launch(Attn& p, bool few, hipStream_t s) {
+  int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
   void (*kernel)(Attn);
-  if constexpr (sizeof(T) == 4) kernel = attention_kernel<T, DP>;
-  else kernel = p.cap > 0.0f || p.slopes ? attention_bf16_kernel<DP, true> : attention_bf16_kernel<DP, false>;
+  if constexpr (sizeof(T) == 4) {
+    kernel = attention_kernel<T, DP>;
+  } else {
+    const bool mod = p.cap > 0.0f || p.slopes;
+    if (few) {
+      kernel = mod ? attention_few_kernel<DP, true> : attention_few_kernel<DP, false>;
+      bytes = NW * 3 * 32 * Lds<T, DP>::RB;
+    } else {
+      kernel = mod ? attention_bf16_kernel<DP, true> : attention_bf16_kernel<DP, false>;
+    }
+  }
   const int rc = allow_dynamic_lds((const void*)kernel, bytes);
   if (rc != PRISM_OK) return rc;
   const long long rows = (long long)p.batch * p.hk * p.R;
@@ -379,7 +540,8 @@ template <typename T, int DP> int launch(Attn& p, hipStream_t s) {
   }
   if (p.nsplit > 1) {
     ProfScope prof(PK_ATTENTION_JOIN, s);
-    hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
+    if (p.nsplit > 8) hipLaunchKernelGGL((attention_join_kernel<T, true>), dim3((unsigned)rows), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((attention_join_kernel<T, false>), dim3((unsigned)((rows + NW - 1) / NW)), dim3(256), 0, s, p);
   }
   return PRISM_OK;
 }
@@ -398,6 +560,13 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
   };
   a.split = parts(pairs * ((R + 127) / 128), (d.k_len + kt - 1) / kt);
+  a.few = !backward && dt == PRISM_BF16 && R <= 32 && !d.q_doc;
+  if (a.few && pairs > 0) {   // parts of 256 keys (two blocks a wave) at least, twice the workgroups that run at once: sequences of unequal length.  8 tokens of 32 heads on 8 key heads
+    // of 128, 4096 to 16384 keys: 512 workgroups 78 us, 1024 84, 1536 95
+    const long long want = (512 + pairs - 1) / pairs, most = (d.k_len + 255) / 256;
+    const long long n = want < most ? want : most;
+    a.split = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+  }
   // dk and dv: the rows of a key tile are many or few under the causal mask.  Up to 512 key tiles (two workgroups per CU) are cut into parts of equal length,
   // as many as run at once; 2 x 4096 x 16 heads of 128 on 4 key heads: 628 us in two parts each, XXX so.
   const int key_tiles = (d.k_len + 127) / 128;
@@ -453,8 +622,10 @@ int launch_attention(const void* q, const void* k, const void* v, void* out, flo
   p.part = (float*)(ws + plan.o_part);
   p.part_ml = (float*)(ws + plan.o_ml);
   p.direct = p.direct && rows_are_vectors(out, d.out, dt);
-  if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, s) : launch<float, 128>(p, s);
-  return d.head_dim <= 64 ? launch<__bf16, 64>(p, s) : launch<__bf16, 128>(p, s);
+  // The parts were counted for the kernel that the sizes ask for; what it cannot read (rows that are no whole vectors) the other one takes in the same parts.
+  const bool few = plan.few && p.direct;
+  if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, few, s) : launch<float, 128>(p, few, s);
+  return d.head_dim <= 64 ? launch<__bf16, 64>(p, few, s) : launch<__bf16, 128>(p, few, s);
 }
 
 }  // namespace prism

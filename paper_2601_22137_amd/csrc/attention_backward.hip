@@ -18,7 +18,7 @@ __device__ inline float slope_of_cap(float capped, float per) {
 // DELTA: stat[pair][0][r] = log2 of the row's sum of weights, +inf where the row sees nothing (its weights are then 0 everywhere), and stat[pair][1][r] = D.
 // Else: dq, with both.
 // D from the rounded `out` is off by 2^-9 of it, which shows where a row sees few keys (elsewhere in the mean over the keys it does not).  For workgroups
-// that see four tiles at most, bf16 therefore takes D = sum p dp.
+// that see eight tiles at most, bf16 therefore takes D = sum p dp.
 template <typename T, int DP, bool DELTA>
 __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(Attn p, float* stat) {
   using L = Lds<T, DP>;
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
     const char *kt = smem + buf * TB, *vt = smem + (2 + buf) * TB;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      f32x16 s = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
-      f32x16 ds = rows_by_rows<T, DP>(vt, 32 * kb, dof, lane);
+      f32x16 s = rows_by_rows<T, DP>(kt, 32 * kb, qf, p.dim, lane);
+      f32x16 ds = rows_by_rows<T, DP>(vt, 32 * kb, dof, p.dim, lane);
       if (cap) scores<T>(p, s, w, 0, true, false, in, out);
       f32x16 f = s;                                          // capped, not yet biased
       if (bias) scores<T>(p, s, w, j0 + 32 * kb + 4 * h, false, true, cap ? 1.0f : in, out);
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
           if (cap) ds[e] *= slope_of_cap(f[e], per);
         }
       }
-      if constexpr (!DELTA) columns_by<T, DP>(acc, kt, 32 * kb, ds, lane);
+      if constexpr (!DELTA) columns_by<T, DP>(acc, kt, 32 * kb, ds, p.dim, lane);
     }
   }
   if constexpr (DELTA) {
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
       if (lse != -INFINITY) lse2 = lse * LOG2E;
       if (h == 0) stat[r] = lse2;
     }
-    if (t1 - t0 > 4) {
+    if (t1 - t0 > 8) {
       Frag<T, DP> of;
       load_row<T, DP>(of, p.direct, p.dim, h, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr);
 #pragma unroll
@@ -184,9 +184,10 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
   Chunks<T, DP, KT> kat, vat;
+  if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole_keys) {
-    kat.set(tid, 1, p.ks[1], 0);
-    vat.set(tid, 1, p.vs[1], 0);
+    kat.set(tid, 1, p.ks[1], 0, p.dim);
+    vat.set(tid, 1, p.vs[1], 0, p.dim);
   }
   auto issue = [&](int t, bool hidden, int buf) {
     auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
     const char *qt = smem + buf * TB, *dot = smem + (2 + buf) * TB;
 #pragma unroll
     for (int rb = 0; rb < RBK; ++rb) {
-      f32x16 s = rows_by_rows<T, DP>(qt, 32 * rb, kf, lane);
+      f32x16 s = rows_by_rows<T, DP>(qt, 32 * rb, kf, p.dim, lane);
       f32x16 f;
       if (cap) {
 #pragma unroll
@@ -497,8 +498,8 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(s[4 * g + e] * mul - ls[e]);
       }
-      columns_by<T, DP>(dv, dot, 32 * rb, s, lane);
-      f32x16 dp = rows_by_rows<T, DP>(dot, 32 * rb, vf, lane);
+      columns_by<T, DP>(dv, dot, 32 * rb, s, p.dim, lane);
+      f32x16 dp = rows_by_rows<T, DP>(dot, 32 * rb, vf, p.dim, lane);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4 de = *(const f32x4*)&delta[buf][32 * rb + 8 * g + 4 * h];
@@ -508,7 +509,7 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
           if (cap) dp[4 * g + e] *= f[4 * g + e];
         }
       }
-      columns_by<T, DP>(dk, qt, 32 * rb, dp, lane);
+      columns_by<T, DP>(dk, qt, 32 * rb, dp, p.dim, lane);
     }
   }
   store_dkv<T, DP>(p, dk, dv, part, pair, b, kh, j, h);
@@ -560,9 +561,10 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   const float* st = stat + (long long)pair * 2 * p.R;
   // Where the group divides 32, a tile's rows lie alike in every tile
   Chunks<T, DP, RT> qat, doat;
+  if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole) {
-    qat.set(tid, p.G, p.qs[1], p.qs[2]);
-    doat.set(tid, p.G, p.dos[1], p.dos[2]);
+    qat.set(tid, p.G, p.qs[1], p.qs[2], p.dim);
+    doat.set(tid, p.G, p.dos[1], p.dos[2], p.dim);
   }
   // documents of the 64-token blocks of a tile's first and last row
   auto docs_of = [&](int t, int4& x, int4& y) {

@@ -41,7 +41,7 @@ struct Attn {
   int chunk, parts, items;          // dk, dv: see AttnPlan
   float *part, *part_ml;            // results of the parts
   bool direct;                      // rows are whole vectors of 16 bytes
-  bool whole;                       // ... of exactly DP entries, and the offsets within a tile fit 31 bits (dk, dv: of queries and dout)
+  bool whole;                       // ... and the offsets within a tile fit 31 bits (dk, dv: of queries and dout)
   bool whole_keys;                  // backward: the same of keys and values
 };
 
@@ -95,22 +95,30 @@ __device__ inline void load_tile(char* lds, bool direct, int dim, int tid, F&& r
   }
 }
 
-// The same for whole tiles of rows of DP entries.  The chunks of a thread lie a fixed number of rows apart, at which the swizzle repeats: one offset, and a
+template <int BYTES> __device__ inline void zero_tiles(char* lds, int tid) {
+  for (int x = tid * 16; x < BYTES; x += NT * 16) *(u32x4*)(lds + x) = (u32x4){0, 0, 0, 0};
+  __syncthreads();
+}
+
+// The same for whole tiles of rows.  The chunks of a thread lie a fixed number of rows apart, at which the swizzle repeats: one offset, and a
 // uniform step.
 template <typename T, int DP, int ROWS> struct Chunks {
   static constexpr int APART = NT / Lds<T, DP>::CPR, N = ROWS / APART;
   unsigned at;
   long long step;
+  bool any;          // a chunk past the head's entries stays as zero_tiles has left it
   // row x is token x / G, head x % G (G divides 32) of the first row's token
-  __device__ void set(int tid, int G, long long token, long long head) {
+  __device__ void set(int tid, int G, long long token, long long head, int dim) {
     using L = Lds<T, DP>;
     const int r = tid / L::CPR, i = r / G;
+    any = ((tid % L::CPR) ^ L::swizzle(r)) * L::EPC < dim;
     at = (unsigned)((i * (int)token + (r - i * G) * (int)head) * (int)sizeof(T)) + (((tid % L::CPR) ^ L::swizzle(r)) << 4);
     step = (G > APART ? APART * head : APART / G * token) * (long long)sizeof(T);
   }
   __device__ void load(char* lds, const char* base, int wave) const {
     // uniform address plus 32-bit offset: added by the load itself, not kept as an address per lane
     const unsigned off = (unsigned)here((int)at);
+    if (!any) return;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(base + u * step);
@@ -176,14 +184,16 @@ template <typename T> __device__ inline f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
 
 // (32 rows of the tile from row0 on) x (the rows held as f): register r of lane (n, h) gets row 8 (r / 4) + 4 h + r % 4 against row n of f
 template <typename T, int DP>
-__device__ inline f32x16 rows_by_rows(const char* lds, int row0, const Frag<T, DP>& f, int lane) {
+__device__ inline f32x16 rows_by_rows(const char* lds, int row0, const Frag<T, DP>& f, int dim, int lane) {
   using L = Lds<T, DP>;
   const int r = lane & 31, h = lane >> 5;
   f32x16 c = {};
 #pragma unroll
   for (int s = 0; s < L::STEPS; ++s) {
-    const u32x4 a = *(const u32x4*)(lds + (row0 + r) * L::RB + (((2 * s + h) ^ L::swizzle(r)) << 4));
-    c = mma<T>(a, f[s], c);
+    if (2 * s * L::EPC < dim) {
+      const u32x4 a = *(const u32x4*)(lds + (row0 + r) * L::RB + (((2 * s + h) ^ L::swizzle(r)) << 4));
+      c = mma<T>(a, f[s], c);
+    }
   }
   return c;
 }
@@ -191,7 +201,7 @@ __device__ inline f32x16 rows_by_rows(const char* lds, int row0, const Frag<T, D
 // acc[t] += (columns 32 t .. of 32 rows of the tile, transposed) x p: entry (d, n) gets sum over the rows of tile[row][d] p[row][n].  p is rounded to the
 // tile's type: in bf16 its relative error of 2^-9 is that of the results themselves.
 template <typename T, int DP>
-__device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int row0, const f32x16& p, int lane) {
+__device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int row0, const f32x16& p, int dim, int lane) {
   using L = Lds<T, DP>;
   const int h = lane >> 5;
   if constexpr (sizeof(T) == 2) {
@@ -220,8 +230,10 @@ __device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int r
       const int row = 8 * (r >> 2) + 4 * h + (r & 3);
 #pragma unroll
       for (int t = 0; t < DP / 32; ++t) {
-        const float a = *(const float*)(lds + (row0 + row) * L::RB + (((8 * t + (n >> 2)) ^ L::swizzle(row)) << 4) + 4 * (n & 3));
-        acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], acc[t], 0, 0, 0);
+        if (32 * t < dim) {
+          const float a = *(const float*)(lds + (row0 + row) * L::RB + (((8 * t + (n >> 2)) ^ L::swizzle(row)) << 4) + 4 * (n & 3));
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], acc[t], 0, 0, 0);
+        }
       }
     }
   }
@@ -461,7 +473,7 @@ inline Attn attn_common(const void* q, const void* k, const void* v, int dt, con
   p.krange = p.qrange + (long long)d.batch * ((d.q_len + 63) / 64);
   p.direct = d.head_dim * (dt == PRISM_F32 ? 4 : 2) % 16 == 0 && rows_are_vectors(q, d.q, dt) && rows_are_vectors(k, d.k, dt) && rows_are_vectors(v, d.v, dt);
   const long long widest = d.k.token > d.v.token ? d.k.token : d.v.token;
-  p.whole = p.direct && (d.head_dim == 64 || d.head_dim == 128) && widest < (1ll << 22);
+  p.whole = p.direct && widest < (1ll << 22);
   return p;
 }
 

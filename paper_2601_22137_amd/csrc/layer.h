@@ -19,6 +19,7 @@ int launch_norm_rope_backward(const void* dqo, const void* dko, const void* q, c
 
 struct AttnPlan {
   int split;                            // parts of the keys of a row tile
+  bool few;                             // at most 32 rows a pair: the kernel for single tokens
   int chunk, parts, items;              // rows of a part of a key tile's rows (0: whole), the most parts of a key tile, parts of a pair
   size_t o_part, o_ml, o_stat, total;   // bytes from the start of the workspace, where the ranges of the documents lie
 };

@@ -332,6 +332,7 @@ def read_reports(infos):
 _NORM_ROPE = struct.Struct("@9i2f4P18qPN")
 _ATTENTION = struct.Struct("@7i2f5P24qPN")
 _NO_STRIDES = (0, 0, 0)
+_NONE = (None, None)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
@@ -439,9 +440,6 @@ def _norm_rope_desc(q, k, results, grads, inv_freq, positions, start, q_weight, 
         b, n, heads[0], heads[1], d, rot, 1 if norm else 0, 1 if interleaved else 0, start, eps, scale, _plain(positions, "positions", torch.int32, dev, (b, n)),
         _plain(inv_freq, "inv_freq", torch.float32, dev, (rot // 2,)), _plain(q_weight, "q_weight", torch.float32, dev, (d,)),
         _plain(k_weight, "k_weight", torch.float32, dev, (d,)), *strides, *_given(workspace, dev))
-
-
-_NONE = (None, None)
 
 
 def _ptr(t):
