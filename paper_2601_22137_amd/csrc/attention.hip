@@ -39,8 +39,9 @@ __device__ inline void finish(const Attn& p, const f32x16 (&acc)[DP / 32], float
   }
 }
 
+// (fp32)
 template <typename T, int DP>
-__global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn p) {
+__global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
   using L = Lds<T, DP>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
@@ -63,7 +64,18 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
+  Chunks<T, DP, KT> kat, vat;
+  if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
+  if (p.whole) {
+    kat.set(tid, 1, p.ks[1], 0, p.dim);
+    vat.set(tid, 1, p.vs[1], 0, p.dim);
+  }
   auto issue = [&](int t, int buf) {
+    if (p.whole && !kdoc && (t + 1) * KT <= keys) {
+      kat.load(smem + buf * TB, (const char*)(kbase + (long long)t * KT * p.ks[1]), wave);
+      vat.load(smem + (2 + buf) * TB, (const char*)(vbase + (long long)t * KT * p.vs[1]), wave);
+      return;
+    }
     load_tile<T, DP, KT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? kbase + j * p.ks[1] : nullptr; });
     load_tile<T, DP, KT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? vbase + j * p.vs[1] : nullptr; });
     if (kdoc && tid < KT) kd[buf][tid] = t * KT + tid < keys ? kdoc[t * KT + tid] : -1;
@@ -92,7 +104,7 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_kernel(Attn
       if (need) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const int j = 8 * g + 4 * h + 32 * kb;
+          const int j = 8 * g + 4 * prism::here(h) + 32 * kb;
           int4 d = make_int4(w.doc, w.doc, w.doc, w.doc);
           if (kdoc) d = *(const int4*)&kd[buf][j];
           const int dd[4] = {d.x, d.y, d.z, d.w};

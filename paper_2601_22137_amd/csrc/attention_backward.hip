@@ -20,7 +20,7 @@ __device__ inline float slope_of_cap(float capped, float per) {
 // D from the rounded `out` is off by 2^-9 of it, which shows where a row sees few keys (elsewhere in the mean over the keys it does not).  For workgroups
 // that see eight tiles at most, bf16 therefore takes D = sum p dp.
 template <typename T, int DP, bool DELTA>
-__global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(Attn p, float* stat) {
+__global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dq_kernel(Attn p, float* stat) {
   using L = Lds<T, DP>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
@@ -70,7 +70,18 @@ __global__ void __launch_bounds__(NT, waves_per_simd<T>()) attention_dq_kernel(A
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
+  Chunks<T, DP, KT> kat, vat;
+  if (p.dim < DP && !DELTA) zero_tiles<4 * TB>(smem, tid);
+  if (p.whole_keys) {
+    kat.set(tid, 1, p.ks[1], 0, p.dim);
+    vat.set(tid, 1, p.vs[1], 0, p.dim);
+  }
   auto issue = [&](int t, int buf) {
+    if (p.whole_keys && !kdoc && (t + 1) * KT <= keys) {
+      kat.load(smem + buf * TB, (const char*)(kbase + (long long)t * KT * p.ks[1]), wave);
+      vat.load(smem + (2 + buf) * TB, (const char*)(vbase + (long long)t * KT * p.vs[1]), wave);
+      return;
+    }
     load_tile<T, DP, KT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? kbase + j * p.ks[1] : nullptr; });
     load_tile<T, DP, KT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? vbase + j * p.vs[1] : nullptr; });
     if (kdoc && tid < KT) kd[buf][tid] = t * KT + tid < keys ? kdoc[t * KT + tid] : -1;
@@ -407,7 +418,7 @@ __device__ inline void store_dkv(const Attn& p, const f32x16 (&dk)[DP / 32], con
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const float* stat) {
+__global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dkv_kernel(Attn p, const float* stat) {
   using L = Lds<T, DP>;
   constexpr int RT = key_tile<T>(), RBK = RT / 32, TB = RT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each
@@ -430,13 +441,25 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
   const T* qbase = (const T*)p.q + b * p.qs[0] + kh * p.G * p.qs[2];
   const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
   const float* st = stat + (long long)pair * 2 * p.R;
+  Chunks<T, DP, RT> qat, doat;
+  if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
+  if (p.whole) {
+    qat.set(tid, p.G, p.qs[1], p.qs[2], p.dim);
+    doat.set(tid, p.G, p.dos[1], p.dos[2], p.dim);
+  }
   auto issue = [&](int t, int buf) {
-    auto at = [&](int x, const T* base, const long long (&s)[3]) -> const T* {
-      const int r = t * RT + x, i = r / p.G, g = r - i * p.G;
-      return r < p.R && st[r] != INFINITY ? base + i * s[1] + g * s[2] : nullptr;
-    };
-    load_tile<T, DP, RT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { return at(x, qbase, p.qs); });
-    load_tile<T, DP, RT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { return at(x, dobase, p.dos); });
+    if (p.whole && !kdoc && (t + 1) * RT <= p.R) {
+      const long long token = (long long)t * RT / p.G;
+      qat.load(smem + buf * TB, (const char*)(qbase + token * p.qs[1]), wave);
+      doat.load(smem + (2 + buf) * TB, (const char*)(dobase + token * p.dos[1]), wave);
+    } else {
+      auto at = [&](int x, const T* base, const long long (&s)[3]) -> const T* {
+        const int r = t * RT + x, i = r / p.G, g = r - i * p.G;
+        return r < p.R && st[r] != INFINITY ? base + i * s[1] + g * s[2] : nullptr;
+      };
+      load_tile<T, DP, RT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { return at(x, qbase, p.qs); });
+      load_tile<T, DP, RT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { return at(x, dobase, p.dos); });
+    }
     if (tid < RT) {
       const int r = t * RT + tid;
       const Row w = row_of(p, b, kh, r, keys);

@@ -21,7 +21,7 @@ typedef const void __attribute__((address_space(1)))* gptr_t;
 typedef void __attribute__((address_space(3)))* lptr_t;
 
 constexpr int NW = 4, NT = 64 * NW;       // waves and threads of a workgroup
-template <typename T> constexpr int waves_per_simd() { return sizeof(T) == 2 ? 2 : 1; }   // fp32 operands take twice the registers
+constexpr int waves_per_simd(int DP) { return DP > 64 ? 1 : 2; }   // gradients in fp32: 256 registers do not hold two rows of 128 and a sum
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Attn {
@@ -100,29 +100,36 @@ template <int BYTES> __device__ inline void zero_tiles(char* lds, int tid) {
   __syncthreads();
 }
 
-// The same for whole tiles of rows.  The chunks of a thread lie a fixed number of rows apart, at which the swizzle repeats: one offset, and a
-// uniform step.
+// The same for whole tiles of rows.  The chunks of a thread lie a fixed number of rows apart: one offset and a uniform step where the swizzle repeats at that distance,
+// two offsets in turn for rows of 512 bytes (8 apart).
 template <typename T, int DP, int ROWS> struct Chunks {
-  static constexpr int APART = NT / Lds<T, DP>::CPR, N = ROWS / APART;
-  unsigned at;
+  static constexpr int APART = NT / Lds<T, DP>::CPR, N = ROWS / APART, KINDS = APART < 16 ? 2 : 1;
+  unsigned at[KINDS];
   long long step;
-  bool any;          // a chunk past the head's entries stays as zero_tiles has left it
+  bool any[KINDS];   // a chunk past the head's entries stays as zero_tiles has left it
   // row x is token x / G, head x % G (G divides 32) of the first row's token
   __device__ void set(int tid, int G, long long token, long long head, int dim) {
     using L = Lds<T, DP>;
     const int r = tid / L::CPR, i = r / G;
-    any = ((tid % L::CPR) ^ L::swizzle(r)) * L::EPC < dim;
-    at = (unsigned)((i * (int)token + (r - i * G) * (int)head) * (int)sizeof(T)) + (((tid % L::CPR) ^ L::swizzle(r)) << 4);
+#pragma unroll
+    for (int k = 0; k < KINDS; ++k) {
+      const int c = (tid % L::CPR) ^ L::swizzle(r + k * APART);
+      any[k] = c * L::EPC < dim;
+      at[k] = (unsigned)((i * (int)token + (r - i * G) * (int)head) * (int)sizeof(T)) + (c << 4);
+    }
     step = (G > APART ? APART * head : APART / G * token) * (long long)sizeof(T);
   }
   __device__ void load(char* lds, const char* base, int wave) const {
-    // uniform address plus 32-bit offset: added by the load itself, not kept as an address per lane
-    const unsigned off = (unsigned)here((int)at);
-    if (!any) return;
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(base + u * step);
-      __builtin_amdgcn_global_load_lds((gptr_t)(from + off), (lptr_t)(lds + (u * NW + wave) * 1024), 16, 0, 0);
+    for (int k = 0; k < KINDS; ++k) {
+      // uniform address plus 32-bit offset: added by the load itself, not kept as an address per lane
+      const unsigned off = (unsigned)here((int)at[k]);
+      if (any[k])
+#pragma unroll
+        for (int u = k; u < N; u += KINDS) {
+          const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(base + u * step);
+          __builtin_amdgcn_global_load_lds((gptr_t)(from + off), (lptr_t)(lds + (u * NW + wave) * 1024), 16, 0, 0);
+        }
     }
   }
 };
