@@ -10,17 +10,21 @@
 namespace prism {
 namespace {
 
-__global__ void __launch_bounds__(256) doc_range_kernel(const int* doc, int4* range, int len, int blocks, int batch) {
-  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (w >= (long long)blocks * batch) return;
-  const int b = (int)(w / blocks), i = (int)(w % blocks) * 64 + (threadIdx.x & 63);
-  const int d = i < len ? doc[(long long)b * len + i] : -1;
+// Documents of every block of 64 tokens: queries', then keys'
+__global__ void __launch_bounds__(256) doc_range_kernel(const int* qdoc, const int* kdoc, int4* range, int n, int m, int batch) {
+  const int bq = (n + 63) / 64, bk = (m + 63) / 64;
+  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), queries = (long long)bq * batch;
+  if (w >= queries + (long long)bk * batch) return;
+  const bool key = w >= queries;
+  const long long x = key ? w - queries : w;
+  const int blocks = key ? bk : bq, len = key ? m : n, b = (int)(x / blocks), i = (int)(x % blocks) * 64 + (threadIdx.x & 63);
+  const int d = i < len ? (key ? kdoc : qdoc)[(long long)b * len + i] : -1;
   int lo = d < 0 ? 0x7FFFFFFF : d, hi = d, none = d < 0;
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    lo = min(lo, __shfl_xor(lo, m));
-    hi = max(hi, __shfl_xor(hi, m));
-    none |= __shfl_xor(none, m);
+  for (int s = 1; s < 64; s *= 2) {
+    lo = min(lo, __shfl_xor(lo, s));
+    hi = max(hi, __shfl_xor(hi, s));
+    none |= __shfl_xor(none, s);
   }
   if ((threadIdx.x & 63) == 0) range[w] = make_int4(lo, hi, none, 0);
 }
@@ -46,7 +50,7 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
   __shared__ __attribute__((aligned(16))) int kd[2][KT];
-  __shared__ int shared_range[4];
+  __shared__ int shared_range[5];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
   const int split = id % p.nsplit;
@@ -54,9 +58,9 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
   const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
   const Row w = row_of(p, b, kh, r, keys);
-  const Limits lim = limits_of(p, w, r);
-  int t0, t1;
-  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  const Limits lim = limits_of(p, w, b, kh, r, keys);
+  int all0, all1, t0, t1;
+  key_range<KT>(p, lim, b, kh, tile, keys, split, shared_range, all0, all1, t0, t1);
   Frag<T, DP> qf;
   const int i = r / p.G, head = kh * p.G + r - i * p.G;
   load_row<T, DP>(qf, p.direct, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2]);
@@ -143,14 +147,14 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
 // tile t, and while those take V^T P^T of tile t, these the exponentials that are left and the maximum of tile t + 1.  The keys run one tile ahead of the
 // values in LDS.  MOD: scores with a cap or a bias.
 template <int DP, bool MOD>
-__global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
+__global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Attn p) {
   typedef __bf16 T;
   using L = Lds<T, DP>;
   constexpr int KT = 64, TB = KT * L::RB, TD = DP / 32, STEPS = L::STEPS;
   constexpr int NK = 2 * STEPS, NP = 4 * TD, AHEAD = 3;   // products of a tile: K Q^T, V^T P^T; operands are read AHEAD of them
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
   __shared__ __attribute__((aligned(16))) int kd[2][KT];
-  __shared__ int shared_range[4];
+  __shared__ int shared_range[5];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
   const int split = id % p.nsplit;
@@ -158,9 +162,9 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
   const Row w = row_of(p, b, kh, r, keys);
-  const Limits lim = limits_of(p, w, r);
-  int t0, t1;
-  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  const Limits lim = limits_of(p, w, b, kh, r, keys);
+  int all0, all1, t0, t1;
+  key_range<KT>(p, lim, b, kh, tile, keys, split, shared_range, all0, all1, t0, t1);
   Frag<T, DP> qf;
   const int i = r / p.G, head = kh * p.G + r - i * p.G;
   load_row<T, DP>(qf, p.direct, p.dim, h, w.last < 0 ? nullptr : (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2]);
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
     vat.set(tid, 1, p.vs[1], 0, p.dim);
   }
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
-  auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, bool hidden, char* to) {
+  auto issue = [&](const T* base, long long stride, const Chunks<T, DP, KT>& at, int t, bool hidden, char* to) __attribute__((always_inline)) {
     if (p.whole && !hidden && (t + 1) * KT <= keys) at.load(to, (const char*)(base + (long long)t * KT * stride), wave);
     else load_tile<T, DP, KT>(to, p.direct, p.dim, tid, [&](int x) { const int j = t * KT + x; return seen(j) ? base + j * stride : nullptr; });
   };
@@ -203,36 +207,36 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
   const bool cap = MOD && p.cap > 0.0f, bias = MOD && p.slopes != nullptr;
   const float mul = MOD ? 1.0f : p.scale * LOG2E, in = cap ? p.scale / p.cap : p.scale * LOG2E, out = p.cap * LOG2E;
   // Scores of the next tile into n and / or the weights of this one, whose scores s holds, into acc; returns the largest product of n
-  auto products = [&](auto has_next, auto has_this, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) {
+  auto products = [&](auto has_next, auto has_this, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(has_next)::value, THIS = decltype(has_this)::value;
     float top = -INFINITY;
     u32x4 kf[AHEAD + 1];
     bf16x8 vf[AHEAD + 1], weights = {};
-    auto weigh = [&](int e) {
+    auto weigh = [&](int e) __attribute__((always_inline)) {
       s[e >> 4][e & 15] = __builtin_amdgcn_exp2f(s[e >> 4][e & 15] * mul - m);
       l[e & 1] += s[e >> 4][e & 15];
     };
     if constexpr (NEXT) {
       n[0] = n[1] = (f32x16){};
-      unrolled<AHEAD>([&](auto x) { kf[decltype(x)::value] = read_k(buf ^ 1, decltype(x)::value); });
-      unrolled<NK>([&](auto xt) {
+      steps<AHEAD>([&](auto x) { kf[decltype(x)::value] = read_k(buf ^ 1, decltype(x)::value); });
+      steps<NK>([&](auto xt) {
         constexpr int x = decltype(xt)::value;
         if constexpr (x + AHEAD < NK) kf[(x + AHEAD) % (AHEAD + 1)] = read_k(buf ^ 1, x + AHEAD);
         else if constexpr (THIS) vf[x + AHEAD - NK] = read_v(buf, x + AHEAD - NK);
         n[x / STEPS] = mma<T>(kf[x % (AHEAD + 1)], qf[x % STEPS], n[x / STEPS]);
         if constexpr (THIS) {
-          unrolled<16 / NK>([&](auto e) { weigh(x * (16 / NK) + decltype(e)::value); });
+          steps<16 / NK>([&](auto e) { weigh(x * (16 / NK) + decltype(e)::value); });
           keep(l[0]);
           keep(l[1]);
         }
         __builtin_amdgcn_sched_barrier(0);
       });
     } else {
-      unrolled<AHEAD>([&](auto x) { vf[decltype(x)::value] = read_v(buf, decltype(x)::value); });
-      unrolled<16>([&](auto e) { weigh(decltype(e)::value); });
+      steps<AHEAD>([&](auto x) { vf[decltype(x)::value] = read_v(buf, decltype(x)::value); });
+      steps<16>([&](auto e) { weigh(decltype(e)::value); });
     }
     if constexpr (THIS) {
-      unrolled<NP>([&](auto xt) {
+      steps<NP>([&](auto xt) {
         constexpr int x = decltype(xt)::value, g = x / TD, E = 32 / NP;
         if constexpr (x + AHEAD < NP) vf[(x + AHEAD) % (AHEAD + 1)] = read_v(buf, x + AHEAD);
         if constexpr (x % TD == 0) {
@@ -241,12 +245,12 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
         }
         acc[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x % (AHEAD + 1)], weights, acc[x % TD], 0, 0, 0);
         if constexpr (x < NP / 2) {
-          unrolled<E>([&](auto e) { weigh(16 + x * E + decltype(e)::value); });
+          steps<E>([&](auto e) { weigh(16 + x * E + decltype(e)::value); });
           keep(l[0]);
           keep(l[1]);
         } else if constexpr (NEXT && !MOD) {
           constexpr int y = (x - NP / 2) * 2 * E;
-          unrolled<E>([&](auto e) { constexpr int z = y + 2 * decltype(e)::value; top = max_of(top, n[z >> 4][z & 15], n[z >> 4][(z & 15) + 1]); });
+          steps<E>([&](auto e) { constexpr int z = y + 2 * decltype(e)::value; top = max_of(top, n[z >> 4][z & 15], n[z >> 4][(z & 15) + 1]); });
           keep(top);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -309,7 +313,7 @@ __global__ void __launch_bounds__(NT, 2) attention_bf16_kernel(Attn p) {
     take_scores(t, buf, n, top, need || !any);
   };
   int4 docs;   // of the next tile's keys
-  auto step = [&](int t, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) {
+  auto step = [&](int t, int buf, f32x16 (&s)[2], f32x16 (&n)[2]) __attribute__((always_inline)) {
     const int4 after = key_docs<KT>(p, b, min(t + 2, t1 - 1));
     landed();   // keys t + 1 and values t are there; keys t and values t - 1 have been read by all waves
     if (t + 2 < t1) issue_k(t + 2, after.z, buf);
@@ -368,7 +372,7 @@ __global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {
   const int id = place(blockIdx.x, gridDim.x), split = id % p.nsplit, pair = id / p.nsplit, b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b);
   const Row w = row_of(p, b, kh, r, keys);
-  const Limits lim = limits_of(p, w, r);
+  const Limits lim = limits_of(p, w, b, kh, r, keys);
   const int blocks = (lim.last + 32) / 32, per = (blocks + p.nsplit - 1) / p.nsplit, b0 = split * per, b1 = min(blocks, b0 + per);
   Frag<T, DP> qf, kf;
   {
@@ -617,10 +621,10 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
 }
 
 void launch_doc_ranges(const prism_attention_desc& d, int4* to, hipStream_t s) {
-  if (!d.q_doc) return;
-  const int bq = (d.q_len + 63) / 64, bk = (d.k_len + 63) / 64;
-  if (bq) hipLaunchKernelGGL(doc_range_kernel, dim3(((long long)bq * d.batch + 3) / 4), dim3(256), 0, s, d.q_doc, to, d.q_len, bq, d.batch);
-  if (bk) hipLaunchKernelGGL(doc_range_kernel, dim3(((long long)bk * d.batch + 3) / 4), dim3(256), 0, s, d.k_doc, to + (long long)bq * d.batch, d.k_len, bk, d.batch);
+  const long long blocks = ((long long)(d.q_len + 63) / 64 + (d.k_len + 63) / 64) * d.batch;
+  if (!d.q_doc || blocks == 0) return;
+  ProfScope prof(PK_ATTENTION_DOCS, s);
+  hipLaunchKernelGGL(doc_range_kernel, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, s, d.q_doc, d.k_doc, to, d.q_len, d.k_len, d.batch);
 }
 
 int launch_attention(const void* q, const void* k, const void* v, void* out, float* lse, int dt, const prism_attention_desc& d, char* ws, hipStream_t s) {

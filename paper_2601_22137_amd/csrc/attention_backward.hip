@@ -15,17 +15,38 @@ __device__ inline float slope_of_cap(float capped, float per) {
   return 1.0f - t * t;
 }
 
-// DELTA: stat[pair][0][r] = log2 of the row's sum of weights, +inf where the row sees nothing (its weights are then 0 everywhere), and stat[pair][1][r] = D.
-// Else: dq, with both.
-// D from the rounded `out` is off by 2^-9 of it, which shows where a row sees few keys (elsewhere in the mean over the keys it does not).  For workgroups
-// that see eight tiles at most, bf16 therefore takes D = sum p dp.
-template <typename T, int DP, bool DELTA>
-__global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dq_kernel(Attn p, float* stat) {
+__device__ inline float lse2_of(const Attn& p, int b, int i, int head, int r) {
+  if (r >= p.R) return INFINITY;
+  const float lse = p.lse_in[((long long)b * p.hq + head) * p.n + i];
+  return lse == -INFINITY ? INFINITY : lse * LOG2E;
+}
+
+// A lane's share of the product of two rows
+template <typename T, int DP> __device__ inline float product_with_row(const Frag<T, DP>& f, const Attn& p, const T* row, int h) {
+  using L = Lds<T, DP>;
+  Frag<T, DP> o;
+  load_row<T, DP>(o, p.direct, p.dim, h, row);
+  float d = 0.0f;
+#pragma unroll
+  for (int s = 0; s < L::STEPS; ++s) {
+    union { u32x4 v; T e[L::EPC]; } x, y;
+    x.v = o[s];
+    y.v = f[s];
+#pragma unroll
+    for (int e = 0; e < L::EPC; ++e) d += (float)x.e[e] * (float)y.e[e];
+  }
+  return d;
+}
+
+// Also, by the first part of a row tile's keys: stat[pair][0][r] = log2 of the row's sum of weights, +inf where the row sees nothing (its weights are then 0
+// everywhere), and stat[pair][1][r] = D, for dk and dv.  (fp32)
+template <typename T, int DP>
+__global__ void __launch_bounds__(NT, 1) attention_dq_kernel(Attn p, float* stat) {
   using L = Lds<T, DP>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
   __shared__ __attribute__((aligned(16))) int kd[2][KT];
-  __shared__ int shared_range[4];
+  __shared__ int shared_range[5];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
   const int split = id % p.nsplit;
@@ -33,45 +54,25 @@ __global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dq_kernel(At
   const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
   const Row w = row_of(p, b, kh, r, keys);
-  const Limits lim = limits_of(p, w, r);
-  int t0, t1;
-  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  const Limits lim = limits_of(p, w, b, kh, r, keys);
+  int all0, all1, t0, t1;
+  key_range<KT>(p, lim, b, kh, tile, keys, split, shared_range, all0, all1, t0, t1);
   const int i = r / p.G, head = kh * p.G + r - i * p.G;
   const bool any = w.last >= 0;
   Frag<T, DP> qf, dof;
   load_row<T, DP>(dof, p.direct, p.dim, h, any ? (const T*)p.dout + b * p.dos[0] + i * p.dos[1] + head * p.dos[2] : nullptr);
   stat += (long long)pair * 2 * p.R;
-  float lse2 = INFINITY, delta = 0.0f;
-  if constexpr (DELTA) {
-    if (r < p.R) {
-      const float lse = p.lse_in[((long long)b * p.hq + head) * p.n + i];
-      if (lse != -INFINITY) lse2 = lse * LOG2E;
-      if (h == 0) stat[r] = lse2;
-    }
-    {
-      Frag<T, DP> of;
-      load_row<T, DP>(of, p.direct, p.dim, h, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr);
-#pragma unroll
-      for (int s = 0; s < L::STEPS; ++s) {
-        union { u32x4 v; T e[L::EPC]; } x, y;
-        x.v = of[s];
-        y.v = dof[s];
-#pragma unroll
-        for (int e = 0; e < L::EPC; ++e) delta += (float)x.e[e] * (float)y.e[e];
-      }
-      t0 = t1;
-    }
-  } else if (r < p.R) {
-    lse2 = stat[r];
-    delta = stat[p.R + r];
-  }
+  const float lse2 = lse2_of(p, b, i, head, r);
+  float delta = product_with_row<T, DP>(dof, p, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr, h);
+  delta += other_half(delta);
+  if (split == 0 && h == 0 && r < p.R) { stat[r] = lse2; stat[p.R + r] = delta; }
   load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
   const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
   auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
   Chunks<T, DP, KT> kat, vat;
-  if (p.dim < DP && !DELTA) zero_tiles<4 * TB>(smem, tid);
+  if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole_keys) {
     kat.set(tid, 1, p.ks[1], 0, p.dim);
     vat.set(tid, 1, p.vs[1], 0, p.dim);
@@ -120,21 +121,11 @@ __global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dq_kernel(At
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(s[e] * mul - lse2);
-        if constexpr (DELTA) {
-          delta += s[e] * ds[e];
-        } else {
-          ds[e] = s[e] * (ds[e] - delta);
-          if (cap) ds[e] *= slope_of_cap(f[e], per);
-        }
+        ds[e] = __builtin_amdgcn_exp2f(s[e] * mul - lse2) * (ds[e] - delta);
+        if (cap) ds[e] *= slope_of_cap(f[e], per);
       }
-      if constexpr (!DELTA) columns_by<T, DP>(acc, kt, 32 * kb, ds, p.dim, lane);
+      columns_by<T, DP>(acc, kt, 32 * kb, ds, p.dim, lane);
     }
-  }
-  if constexpr (DELTA) {
-    delta += other_half(delta);
-    if (r < p.R && h == 0) stat[p.R + r] = delta;
-    return;
   }
   if (r >= p.R) return;
   if (p.nsplit == 1)
@@ -144,15 +135,16 @@ __global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dq_kernel(At
 }
 
 // The same in bf16.  A tile of 64 keys is taken as two blocks: scores K Q^T and dp = V dO^T of the first, with its exponentials beside the latter; the scores of the second beside
-// ds of the first; dq; and so on.
-template <int DP, bool CAP, bool BIAS, bool DELTA>
+// ds of the first; dq; and so on.  D from the rounded `out` is off by 2^-9 of it, which shows where a row sees few keys (elsewhere in the mean over the keys it does not): a
+// workgroup that sees eight tiles at most takes D = sum p dp, in a walk of its own through them.  (Packed documents of 8 x 1024, 12 heads of 64: 45 us, in two launches 54.)
+template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float* stat) {
   typedef __bf16 T;
   using L = Lds<T, DP>;
-  constexpr int KT = 64, TB = KT * L::RB, TD = DP / 32, STEPS = L::STEPS, NC = DELTA ? 0 : 2 * TD, AHEAD = 4;
+  constexpr int KT = 64, TB = KT * L::RB, TD = DP / 32, STEPS = L::STEPS, AHEAD = 4;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
   __shared__ __attribute__((aligned(16))) int kd[2][KT];
-  __shared__ int shared_range[4];
+  __shared__ int shared_range[5];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   int id = place(blockIdx.x, gridDim.x);
   const int split = id % p.nsplit;
@@ -160,37 +152,19 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
   const int tile = p.row_tiles - 1 - id % p.row_tiles, pair = id / p.row_tiles, b = pair / p.hk, kh = pair - b * p.hk;
   const int keys = keys_of(p, b), r = tile * 128 + wave * 32 + (lane & 31);
   const Row w = row_of(p, b, kh, r, keys);
-  const Limits lim = limits_of(p, w, r);
-  int t0, t1;
-  key_range<KT>(p, lim, b, keys, split, shared_range, t0, t1);
+  const Limits lim = limits_of(p, w, b, kh, r, keys);
+  int all0, all1, t0, t1;
+  key_range<KT>(p, lim, b, kh, tile, keys, split, shared_range, all0, all1, t0, t1);
   const int i = r / p.G, head = kh * p.G + r - i * p.G;
   const bool any = w.last >= 0;
   Frag<T, DP> qf, dof;
   load_row<T, DP>(dof, p.direct, p.dim, h, any ? (const T*)p.dout + b * p.dos[0] + i * p.dos[1] + head * p.dos[2] : nullptr);
   stat += (long long)pair * 2 * p.R;
-  float lse2 = INFINITY, delta = 0.0f;
-  if constexpr (DELTA) {
-    if (r < p.R) {
-      const float lse = p.lse_in[((long long)b * p.hq + head) * p.n + i];
-      if (lse != -INFINITY) lse2 = lse * LOG2E;
-      if (h == 0) stat[r] = lse2;
-    }
-    if (t1 - t0 > 8) {
-      Frag<T, DP> of;
-      load_row<T, DP>(of, p.direct, p.dim, h, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr);
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const bf16x8 x = __builtin_bit_cast(bf16x8, of[s]), y = __builtin_bit_cast(bf16x8, dof[s]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) delta += (float)x[e] * (float)y[e];
-      }
-      t0 = t1;
-    }
-  } else if (r < p.R) {
-    lse2 = stat[r];
-    delta = stat[p.R + r];
-  }
-  if (t0 < t1) load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
+  const float lse2 = lse2_of(p, b, i, head, r);
+  float delta = 0.0f;
+  const bool exact = all1 - all0 <= 8;
+  if (!exact) delta = product_with_row<T, DP>(dof, p, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr, h);
+  load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
   const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
@@ -200,7 +174,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
     kat.set(tid, 1, p.ks[1], 0, p.dim);
     vat.set(tid, 1, p.vs[1], 0, p.dim);
   }
-  auto issue = [&](int t, bool hidden, int buf) {
+  auto issue = [&](int t, bool hidden, int buf) __attribute__((always_inline)) {
     auto seen = [&](int j) { return j < keys && !(kdoc && kdoc[j] < 0); };
     if (p.whole_keys && !hidden && (t + 1) * KT <= keys) {
       kat.load(smem + buf * TB, (const char*)(kbase + (long long)t * KT * p.ks[1]), wave);
@@ -218,6 +192,10 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
   const unsigned lds0 = lds_address(smem), ka = lds0 + (lane & 31) * L::RB + ((h ^ L::swizzle(lane & 31)) << 4);
   const int cr = 4 * h + ((lane & 15) >> 2), cc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
   const unsigned ca = lds0 + cr * L::RB + ((cc ^ L::swizzle(cr)) << 4) + 8 * (lane & 1);
+  // walk through tiles [t0, t1), for D or for dq
+  auto walk = [&](auto for_delta, int t0, int t1) {
+  constexpr bool DELTA = decltype(for_delta)::value;
+  constexpr int NC = DELTA ? 0 : 2 * TD;
   int4 docs = make_int4(0, 0, 0, 0);
   if (t0 < t1) {
     docs = key_docs<KT>(p, b, t0);
@@ -254,7 +232,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
       if constexpr (x + AHEAD < N) op[x + AHEAD] = read(std::integral_constant<int, x + AHEAD>{});
       return op[x];
     };
-    unrolled<AHEAD>([&](auto x) { op[decltype(x)::value] = read(x); });
+    steps<AHEAD>([&](auto x) { op[decltype(x)::value] = read(x); });
     f32x16 s[2] = {}, dp[2] = {};
     bf16x8 grads[2];
     auto mask = [&](auto kbt) {
@@ -290,15 +268,15 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
     };
     // product of rows, with EACH entries of work beside every step
     auto rows = [&](f32x16& c, const Frag<T, DP>& f, auto first, auto&& work) {
-      unrolled<STEPS>([&](auto xt) {
+      steps<STEPS>([&](auto xt) {
         constexpr int x = decltype(xt)::value;
         c = mma<T>(next(std::integral_constant<int, decltype(first)::value + x>{}), f[x], c);
-        unrolled<16 / STEPS>([&](auto et) { work(std::integral_constant<int, x * (16 / STEPS) + decltype(et)::value>{}); });
+        steps<16 / STEPS>([&](auto et) { work(std::integral_constant<int, x * (16 / STEPS) + decltype(et)::value>{}); });
         __builtin_amdgcn_sched_barrier(0);
       });
     };
     auto columns = [&](auto first) {
-      unrolled<NC>([&](auto xt) {
+      steps<NC>([&](auto xt) {
         constexpr int x = decltype(xt)::value;
         acc[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, decltype(first)::value + x>{})), grads[x / TD], acc[x % TD], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -317,17 +295,20 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
     columns(std::integral_constant<int, 3 * STEPS>{});
     mask(b1);
     rows(dp[1], dof, std::integral_constant<int, 3 * STEPS + NC>{}, [&](auto e) { weigh(b1, e); });
-    unrolled<16>([&](auto e) {
+    steps<16>([&](auto e) {
       if constexpr (DELTA) delta += s[1][decltype(e)::value] * dp[1][decltype(e)::value];
       else grad(b1, e);
     });
     columns(std::integral_constant<int, 4 * STEPS + NC>{});
   }
-  if constexpr (DELTA) {
-    delta += other_half(delta);
-    if (r < p.R && h == 0) stat[p.R + r] = delta;
-    return;
+  };
+  if (exact) {
+    walk(std::true_type{}, all0, all1);
+    __syncthreads();   // the tiles are filled again
   }
+  delta += other_half(delta);
+  if (split == 0 && h == 0 && r < p.R) { stat[r] = lse2; stat[p.R + r] = delta; }
+  walk(std::false_type{}, t0, t1);
   const int re = tile * 128 + wave * 32 + (here(lane) & 31), ie = re / p.G;   // (again, rather than kept)
   if (re >= p.R) return;
   if (p.nsplit == 1)
@@ -418,7 +399,7 @@ __device__ inline void store_dkv(const Attn& p, const f32x16 (&dk)[DP / 32], con
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(NT, waves_per_simd(DP)) attention_dkv_kernel(Attn p, const float* stat) {
+__global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const float* stat) {
   using L = Lds<T, DP>;
   constexpr int RT = key_tile<T>(), RBK = RT / 32, TB = RT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each
@@ -596,7 +577,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
     y = range_of(p.qrange, (long long)b * qblocks + min(t * RT + RT - 1, p.R - 1) / p.G / 64);
   };
   int row_doc = doc_of_row(p, b, (t1 - 1 - part) * RT + tid);   // of the tile that is issued next, read while the one before is on its way
-  auto issue = [&](int t, int buf) {
+  auto issue = [&](int t, int buf) __attribute__((always_inline)) {
     int4 dx = make_int4(0, 0, 0, 0), dy = dx;
     if (p.qdoc) docs_of(t, dx, dy);
     if (p.whole && !dx.z && !dy.z && (t + 1) * RT <= p.R) {
@@ -673,11 +654,11 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
       u32x4 op[N], vop[2];
       auto next = [&](auto xt) {
         constexpr int x = decltype(xt)::value, from = x == 0 ? 0 : read_by<STEPS, NC, AHEAD>(x - 1), to = read_by<STEPS, NC, AHEAD>(x);
-        unrolled<to - from>([&](auto y) { op[from + decltype(y)::value] = read(std::integral_constant<int, from + decltype(y)::value>{}); });
+        steps<to - from>([&](auto y) { op[from + decltype(y)::value] = read(std::integral_constant<int, from + decltype(y)::value>{}); });
         return op[x];
       };
       f32x16 s = {}, dp = {};
-      unrolled<STEPS>([&](auto xt) {
+      steps<STEPS>([&](auto xt) {
         constexpr int x = decltype(xt)::value;
         s = mma<T>(next(xt), kf[x], s);
         __builtin_amdgcn_sched_barrier(0);
@@ -697,7 +678,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
       bf16x8 weights[2], grads[2];
       f32x4 row4, slope4;
       int4 place4;
-      unrolled<STEPS>([&](auto xt) {
+      steps<STEPS>([&](auto xt) {
         constexpr int x = decltype(xt)::value, E = 16 / STEPS;
         u32x4 v;
         if constexpr (V_IN_LDS) {
@@ -707,7 +688,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
           v = vf[x];
         }
         dp = mma<T>(next(std::integral_constant<int, STEPS + x>{}), v, dp);
-        unrolled<E>([&](auto et) {
+        steps<E>([&](auto et) {
           constexpr int e = x * E + decltype(et)::value;
           if constexpr (e % 4 == 0) {
             constexpr int r4 = 8 * (e / 4);
@@ -730,17 +711,17 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      unrolled<NC>([&](auto xt) {
+      steps<NC>([&](auto xt) {
         constexpr int x = decltype(xt)::value, E = 16 / NC;
         dv[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, 2 * STEPS + x>{})), weights[x / TD], dv[x % TD], 0, 0, 0);
-        unrolled<E>([&](auto et) {
+        steps<E>([&](auto et) {
           constexpr int e = x * E + decltype(et)::value;
           if constexpr (e % 4 == 0) row4 = *(const f32x4*)&delta[buf][32 * rb + 8 * (e / 4) + 4 * h];
           grads[e >> 3][e & 7] = (__bf16)(s[e] * (dp[e] - row4[e & 3]));
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      unrolled<NC>([&](auto xt) {
+      steps<NC>([&](auto xt) {
         constexpr int x = decltype(xt)::value;
         dk[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, 2 * STEPS + NC + x>{})), grads[x / TD], dk[x % TD], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -769,17 +750,15 @@ template <typename T, bool KEYS> __global__ void __launch_bounds__(256) attentio
 template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* stat, hipStream_t s) {
   constexpr int bytes = 4 * key_tile<T>() * Lds<T, DP>::RB;
   void (*dkv)(Attn, const float*);
-  void (*dq[2])(Attn, float*);          // D, then dq
+  void (*dq)(Attn, float*);
   int dkv_bytes = bytes;
   if constexpr (sizeof(T) == 4) {
-    dq[0] = attention_dq_kernel<T, DP, true>;
-    dq[1] = attention_dq_kernel<T, DP, false>;
+    dq = attention_dq_kernel<T, DP>;
     dkv = attention_dkv_kernel<T, DP>;
   } else {
     auto pick = [&](auto cap, auto bias) {
       constexpr bool C = decltype(cap)::value, B = decltype(bias)::value;
-      dq[0] = attention_dq_bf16_kernel<DP, C, B, true>;
-      dq[1] = attention_dq_bf16_kernel<DP, C, B, false>;
+      dq = attention_dq_bf16_kernel<DP, C, B>;
       dkv = attention_dkv_bf16_kernel<DP, C, B>;
     };
     std::true_type yes;
@@ -787,21 +766,14 @@ template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* s
     p.cap > 0.0f ? (p.slopes ? pick(yes, yes) : pick(yes, no)) : (p.slopes ? pick(no, yes) : pick(no, no));
     dkv_bytes = DP > 64 ? (4 * 32 + 128) * Lds<T, DP>::RB : 4 * 64 * Lds<T, DP>::RB;
   }
-  int rc = PRISM_OK;
-  for (auto kernel : dq)
-    if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)kernel, bytes);
+  int rc = allow_dynamic_lds((const void*)dq, bytes);
   if (rc == PRISM_OK) rc = allow_dynamic_lds((const void*)dkv, dkv_bytes);
   if (rc != PRISM_OK) return rc;
   const unsigned pairs = (unsigned)p.batch * p.hk;
-  p.nsplit = 1;
-  if (p.R > 0) {
-    ProfScope prof(PK_ATTENTION_STAT, s);
-    hipLaunchKernelGGL(dq[0], dim3(pairs * p.row_tiles), dim3(NT), bytes, s, p, stat);
-  }
   p.nsplit = plan.split;
   if (p.R > 0) {
     ProfScope prof(PK_ATTENTION_DQ, s);
-    hipLaunchKernelGGL(dq[1], dim3(pairs * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p, stat);
+    hipLaunchKernelGGL(dq, dim3(pairs * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p, stat);
   }
   if (p.nsplit > 1 && p.R > 0) {
     ProfScope prof(PK_ATTENTION_JOIN, s);

@@ -21,7 +21,6 @@ typedef const void __attribute__((address_space(1)))* gptr_t;
 typedef void __attribute__((address_space(3)))* lptr_t;
 
 constexpr int NW = 4, NT = 64 * NW;       // waves and threads of a workgroup
-constexpr int waves_per_simd(int DP) { return DP > 64 ? 1 : 2; }   // gradients in fp32: 256 registers do not hold two rows of 128 and a sum
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Attn {
@@ -46,6 +45,14 @@ struct Attn {
 };
 
 __device__ const unsigned zero_page[4] = {0, 0, 0, 0};
+
+// f(0) .. f(D - 1), the numbers as types; in place whatever its size: its operands are registers
+template <int D, typename F> __device__ __forceinline__ void steps(F&& f) {
+  if constexpr (D > 0) {
+    steps<D - 1>(f);
+    f(std::integral_constant<int, D - 1>{});
+  }
+}
 
 // The same value, computed again where it is used: what the rare branches of a loop derive from it is not kept in registers across the loop.
 __device__ inline int here(int x) {
@@ -352,8 +359,16 @@ struct Limits {
   bool mixed;                // whether the rows are of more than one document, or of none
 };
 
-__device__ inline Limits limits_of(const Attn& p, const Row& w, int r) {
+__device__ inline Limits limits_of(const Attn& p, const Row& w, int b, int kh, int r, int keys) {
   Limits x;
+  if (!p.qdoc) {     // what a row sees grows with its token: the wave's first and last row say it all
+    const int r0 = __builtin_amdgcn_readfirstlane(r);
+    x.first = r0 < p.R ? row_of(p, b, kh, r0, keys, 0).last : 0x7FFFFFFF;
+    x.last = r0 < p.R ? row_of(p, b, kh, min(r0 + 31, p.R - 1), keys, 0).last : -1;
+    x.lo = x.hi = 0;
+    x.mixed = false;
+    return x;
+  }
   x.last = w.last;
   x.first = r < p.R ? w.last : 0x7FFFFFFF;
   x.lo = r < p.R && w.doc >= 0 ? w.doc : 0x7FFFFFFF;
@@ -375,41 +390,40 @@ __device__ inline Limits limits_of(const Attn& p, const Row& w, int r) {
   return x;
 }
 
-// The key tiles [t0, t1) of part `split` of what the workgroup's rows see; all threads call it
+// The key tiles [all0, all1) that the rows of row tile `tile` see, and [t0, t1), part `split` of them; all threads call it
 template <int KT>
-__device__ inline void key_range(const Attn& p, const Limits& lim, int b, int keys, int split, int* sh, int& t0, int& t1) {
-  if (threadIdx.x < 4) sh[threadIdx.x] = threadIdx.x == 0 ? -1 : threadIdx.x == 1 ? 0x7FFFFFFF : threadIdx.x == 2 ? -1 : 0;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) {
-    atomicMax(&sh[0], lim.last);
-    atomicMin(&sh[1], lim.lo);
-    atomicMax(&sh[2], lim.hi);
-  }
-  __syncthreads();
-  const int last = sh[0], lo = sh[1], hi = sh[2];
-  int first_tile = 0, end_tile = last / KT + 1;
-  if (last < 0) end_tile = 0;
-  if (p.kdoc && last >= 0) {                  // from the first to the last block of 64 keys with one of the workgroup's documents
+__device__ inline void key_range(const Attn& p, const Limits& lim, int b, int kh, int tile, int keys, int split, int* sh, int& all0, int& all1, int& t0, int& t1) {
+  int first_tile = 0, end_tile = 0;
+  if (!p.kdoc) {
+    end_tile = (row_of(p, b, kh, min(tile * 128 + 127, p.R - 1), keys, 0).last + KT) / KT;
+  } else {           // from the first to the last block of 64 keys with one of the workgroup's documents
+    if (threadIdx.x < 5) sh[threadIdx.x] = threadIdx.x == 1 || threadIdx.x == 3 ? 0x7FFFFFFF : -1;
     __syncthreads();
-    if (threadIdx.x == 0) { sh[0] = 0x7FFFFFFF; sh[1] = -1; }
+    if ((threadIdx.x & 63) == 0) {
+      atomicMax(&sh[0], lim.last);
+      atomicMin(&sh[1], lim.lo);
+      atomicMax(&sh[2], lim.hi);
+    }
     __syncthreads();
-    const int blocks = (p.m + 63) / 64, upto = last / 64;
+    const int last = sh[0], lo = sh[1], hi = sh[2];
+    const int blocks = (p.m + 63) / 64, upto = last < 0 ? -1 : last / 64;
     int f = 0x7FFFFFFF, e = -1;
     for (int x = threadIdx.x; x <= upto; x += NT) {
       const int4 k = p.krange[(long long)b * blocks + x];
       if (k.x <= hi && k.y >= lo) { f = min(f, x); e = max(e, x); }
     }
-    if (e >= 0) { atomicMin(&sh[0], f); atomicMax(&sh[1], e); }
+    if (e >= 0) { atomicMin(&sh[3], f); atomicMax(&sh[4], e); }
     __syncthreads();
-    if (sh[1] < 0) end_tile = 0;
-    else {
-      first_tile = sh[0] * 64 / KT;
-      end_tile = min(end_tile, (sh[1] + 1) * 64 / KT);
+    if (sh[4] >= 0) {
+      first_tile = sh[3] * 64 / KT;
+      end_tile = min(last / KT + 1, (sh[4] + 1) * 64 / KT);
     }
   }
-  const int per = (max(end_tile - first_tile, 0) + p.nsplit - 1) / p.nsplit;
-  t0 = __builtin_amdgcn_readfirstlane(first_tile + split * per);
-  t1 = __builtin_amdgcn_readfirstlane(min(end_tile, first_tile + (split + 1) * per));
+  all0 = __builtin_amdgcn_readfirstlane(first_tile);
+  all1 = __builtin_amdgcn_readfirstlane(max(end_tile, first_tile));
+  const int per = (all1 - all0 + p.nsplit - 1) / p.nsplit;
+  t0 = min(all0 + split * per, all1);
+  t1 = min(all0 + (split + 1) * per, all1);
 }
 
 // Documents of a block of 64 tokens: lowest, highest, whether one of none is among them.  Read through the scalar cache: a vector load would have to wait for the

@@ -395,7 +395,7 @@ enum ProfKind {
   PK_FLOW,           // all iterations in one launch
   PK_SMALL_ROOT,     // inverse roots of padded order 64, whole calls
   PK_DROPOUT, PK_NORM_ROPE, PK_NORM_ROPE_BACKWARD,
-  PK_ATTENTION, PK_ATTENTION_JOIN, PK_ATTENTION_STAT, PK_ATTENTION_DQ, PK_ATTENTION_DKV,
+  PK_ATTENTION, PK_ATTENTION_JOIN, PK_ATTENTION_DOCS, PK_ATTENTION_DQ, PK_ATTENTION_DKV,
   PK_COUNT
 };
 struct ProfScope {   // records an event pair around the launches made during its lifetime
