@@ -732,19 +732,35 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
 }
 
 // to[pair][row] = the sum of the parts, in their order; row -> (token, head) as row / G and row % G.  KEYS: dk and dv (blockIdx.y), whose key tiles have their own
-// numbers of parts.
-template <typename T, bool KEYS> __global__ void __launch_bounds__(256) attention_sum_kernel(Attn p, T* to0, T* to1) {
+// numbers of parts.  A thread takes E entries: four where rows are whole vectors.
+template <typename T, bool KEYS, int E> __global__ void __launch_bounds__(256) attention_sum_kernel(Attn p, T* to0, T* to1) {
   const int R = KEYS ? p.m : p.R, G = KEYS ? 1 : p.G;
-  const long long total = (long long)p.batch * p.hk * R * p.dim, at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long total = (long long)p.batch * p.hk * R * p.dim, at = ((long long)blockIdx.x * 256 + threadIdx.x) * E;
   if (at >= total) return;
   const long long row = at / p.dim;
   const int d = (int)(at - row * p.dim), pair = (int)(row / R), r = (int)(row - (long long)pair * R), b = pair / p.hk, kh = pair - b * p.hk, i = r / G;
   const int n = KEYS ? parts_of(rows_of_key_tile(p.causal, p.prefix, p.n, p.m, p.G, r / 128), p.chunk) : p.nsplit;
-  const float* part = p.part + (KEYS && blockIdx.y ? p.parts * total : 0);
-  float v = 0.0f;
-  for (int s = 0; s < n; ++s) v += part[s * total + at];
+  const float* part = p.part + (KEYS && blockIdx.y ? p.parts * total : 0) + at;
   const long long (&st)[3] = !KEYS ? p.dqs : blockIdx.y ? p.dvs : p.dks;
-  (blockIdx.y ? to1 : to0)[b * st[0] + i * st[1] + (kh * G + r - i * G) * st[2] + d] = (T)v;
+  T* to = (blockIdx.y ? to1 : to0) + b * st[0] + i * st[1] + (kh * G + r - i * G) * st[2] + d;
+  if constexpr (E == 4) {
+    f32x4 v = {};
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) v += *(const f32x4*)(part + s * total);
+    store4<T>(to, v, true, 4);
+  } else {
+    float v = 0.0f;
+    for (int s = 0; s < n; ++s) v += part[s * total];
+    *to = (T)v;
+  }
+}
+
+template <typename T, bool KEYS> void sum_parts(const Attn& p, void* to0, void* to1, hipStream_t s) {
+  ProfScope prof(PK_ATTENTION_JOIN, s);
+  const long long total = (long long)p.batch * p.hk * (KEYS ? p.m : p.R) * p.dim, threads = p.direct ? total / 4 : total;
+  const dim3 grid((unsigned)((threads + 255) / 256), to1 ? 2 : 1);
+  if (p.direct) hipLaunchKernelGGL((attention_sum_kernel<T, KEYS, 4>), grid, dim3(256), 0, s, p, (T*)to0, (T*)to1);
+  else hipLaunchKernelGGL((attention_sum_kernel<T, KEYS, 1>), grid, dim3(256), 0, s, p, (T*)to0, (T*)to1);
 }
 
 template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* stat, hipStream_t s) {
@@ -775,11 +791,7 @@ template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* s
     ProfScope prof(PK_ATTENTION_DQ, s);
     hipLaunchKernelGGL(dq, dim3(pairs * p.row_tiles * p.nsplit), dim3(NT), bytes, s, p, stat);
   }
-  if (p.nsplit > 1 && p.R > 0) {
-    ProfScope prof(PK_ATTENTION_JOIN, s);
-    const long long total = (long long)pairs * p.R * p.dim;
-    hipLaunchKernelGGL((attention_sum_kernel<T, false>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, p, (T*)p.dq, (T*)nullptr);
-  }
+  if (p.nsplit > 1 && p.R > 0) sum_parts<T, false>(p, p.dq, nullptr, s);
   if (p.m == 0) return PRISM_OK;
   p.chunk = plan.chunk;
   p.parts = plan.parts;
@@ -788,11 +800,7 @@ template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* s
     ProfScope prof(PK_ATTENTION_DKV, s);
     hipLaunchKernelGGL(dkv, dim3(pairs * p.items), dim3(NT), dkv_bytes, s, p, (const float*)stat);
   }
-  if (p.parts > 1) {
-    ProfScope prof(PK_ATTENTION_JOIN, s);
-    const long long total = (long long)pairs * p.m * p.dim;
-    hipLaunchKernelGGL((attention_sum_kernel<T, true>), dim3((unsigned)((total + 255) / 256), 2), dim3(256), 0, s, p, (T*)p.dk, (T*)p.dv);
-  }
+  if (p.parts > 1) sum_parts<T, true>(p, p.dk, p.dv, s);
   return PRISM_OK;
 }
 
