@@ -584,14 +584,14 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
     a.split = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
   }
   // dk and dv: the rows of a key tile are many or few under the causal mask.  Up to 512 key tiles (two workgroups per CU) are cut into parts of equal length,
-  // as many as run at once; 2 x 4096 x 16 heads of 128 on 4 key heads: 628 us in two parts each, 518 so.
+  // 1024 at most; 2 x 4096 x 16 heads of 128 on 4 key heads: 628 us in two parts each, 545 in 512 parts of equal length, 509 in 1024 (with their sum).
   const int key_tiles = (d.k_len + 127) / 128;
   a.parts = 1;
   a.items = key_tiles;
   if (backward && pairs * key_tiles > 0 && pairs * key_tiles <= 512) {
     long long all = 0;
     for (int k = 0; k < key_tiles; ++k) all += rows_of_key_tile(d.causal, d.prefix, d.q_len, d.k_len, (int)(R / (d.q_len ? d.q_len : 1)), k);
-    long long chunk = (all * pairs + 511) / 512;
+    long long chunk = (all * pairs + 1023) / 1024;
     for (chunk = chunk < 4 * kt ? 4 * kt : (chunk + 31) / 32 * 32;; chunk += (chunk / 16 + 31) / 32 * 32) {
       a.items = 0;
       a.parts = 1;
@@ -600,7 +600,7 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
         a.items += n;
         if (n > a.parts) a.parts = n;
       }
-      if (a.items * pairs <= 512) break;
+      if (a.items * pairs <= 1024) break;
     }
     a.chunk = a.parts > 1 ? (int)chunk : 0;
   }
