@@ -35,6 +35,8 @@ template <typename F> int guarded(F&& f) {
 bool is_type(int dt) { return dt == PRISM_F32 || dt == PRISM_BF16; }
 bool aligned_to(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) == 0; }
 
+template <typename... S> bool negative(const S&... s) { return ((s.batch < 0 || s.token < 0 || s.head < 0) || ...); }
+
 int check(const prism_norm_rope_desc* d, int dt) {
   if (!d || !is_type(dt)) return refuse("null description or unknown type");
   if (d->batch < 0 || d->len < 0 || d->q_heads < 0 || d->k_heads < 0 || d->head_dim < 1) return refuse("negative size, or a head without entries");
@@ -42,6 +44,7 @@ int check(const prism_norm_rope_desc* d, int dt) {
   if (d->rot_dim > 0 && !d->inv_freq) return refuse("rot_dim without inv_freq");
   if (!std::isfinite(d->scale) || (d->norm && !(d->eps >= 0.0f && std::isfinite(d->eps)))) return refuse("scale or eps is not finite, or eps negative");
   if (!d->norm && (d->q_weight || d->k_weight)) return refuse("weights without the norm");
+  if (negative(d->q, d->k, d->q_out, d->k_out, d->dq, d->dk)) return refuse("a stride is negative");
   if (d->head_dim > PRISM_MAX_NORM_HEAD) return refuse("head_dim is over PRISM_MAX_NORM_HEAD", PRISM_EUNSUPPORTED);
   if ((long long)d->batch * d->len > MAX_ROWS / (d->q_heads + (long long)d->k_heads + 1)) return refuse("more than 2^31 - 1 heads in a call", PRISM_EUNSUPPORTED);
   return PRISM_OK;
@@ -56,6 +59,7 @@ int check(const prism_attention_desc* d, int dt) {
   if (!(d->softcap >= 0.0f) || !std::isfinite(d->softcap)) return refuse("softcap has to be finite and not negative");
   if (!d->q_doc != !d->k_doc) return refuse("q_doc and k_doc go together");
   if (d->prefix && !d->causal) return refuse("a prefix needs the causal mask");
+  if (negative(d->q, d->k, d->v, d->out, d->dout, d->dq, d->dk, d->dv)) return refuse("a stride is negative");
   if (d->head_dim > PRISM_MAX_ATTENTION_HEAD) return refuse("head_dim is over PRISM_MAX_ATTENTION_HEAD", PRISM_EUNSUPPORTED);
   if (!d->k_heads || !d->batch) return PRISM_OK;
   const long long G = d->q_heads / d->k_heads, R = G * d->q_len, pairs = (long long)d->batch * d->k_heads;

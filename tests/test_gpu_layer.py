@@ -493,5 +493,8 @@ def test_attention_refusals(prism):
     o.q_heads = 3
     assert L.prism_attention(q.data_ptr(), k.data_ptr(), k.data_ptr(), q.data_ptr(), None, prism.F32, ctypes.byref(o), None) == prism.EINVAL
     assert "multiple" in L.prism_last_error().decode()
+    o.q_heads, o.q.token = 4, -1
+    assert L.prism_attention(q.data_ptr(), k.data_ptr(), k.data_ptr(), q.data_ptr(), None, prism.F32, ctypes.byref(o), None) == prism.EINVAL
+    o.q.token = 256
     o.q_heads, o.batch, o.k_len = 4, 1 << 20, 1 << 20
     assert L.prism_attention(q.data_ptr(), k.data_ptr(), k.data_ptr(), q.data_ptr(), None, prism.F32, ctypes.byref(o), None) == prism.EUNSUPPORTED
