@@ -283,7 +283,8 @@ struct Row {
   float slope; // log2(e) times that of its head
 };
 
-__device__ inline int doc_of_row(const Attn& p, int b, int r) { return p.qdoc && r < p.R ? p.qdoc[(long long)b * p.n + r / p.G] : 0; }
+// 0 for rows there are not, before the first one too: a key tile without rows asks for the one before its range
+__device__ inline int doc_of_row(const Attn& p, int b, int r) { return p.qdoc && r >= 0 && r < p.R ? p.qdoc[(long long)b * p.n + r / p.G] : 0; }
 
 __device__ inline Row row_of(const Attn& p, int b, int kh, int r, int keys, int doc) {
   Row w;

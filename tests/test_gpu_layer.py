@@ -373,6 +373,15 @@ def test_attention_in_parts(prism, dtype, causal, docs):
     _check_attention(prism, dtype, 3, 1, 2000, 4, 2, 128, causal=causal, k_lens=[2000, 0, 130], softcap=20.0, train=False, seed=13, poison=True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n,m", [(1, 1), (5, 300), (70, 400), (300, 20)])
+def test_attention_keys_whose_documents_no_query_has(prism, dtype, causal, n, m):
+    """Key tiles without rows, the first sequence's too: nothing lies before its documents."""
+    q_doc, k_doc = [[1] * n, [2] * n], [[7] * m, [2] * (m // 2) + [9] * (m - m // 2)]
+    _check_attention(prism, dtype, 2, n, m, 4, 2, 64, causal=causal, q_doc=q_doc, k_doc=k_doc, seed=17)
+
+
 def test_attention_large_scores_stay_finite(prism):
     _check_attention(prism, F32, 1, 40, 200, 1, 1, 64, q_scale=200.0, seed=14, train=False)
     _check_attention(prism, BF16, 1, 40, 200, 1, 1, 64, q_scale=200.0, seed=15, train=False)
