@@ -1,0 +1,118 @@
+"""The layer operators for autograd, and the attention half of a transformer layer made of them: the part of a model whose 2-D weights
+optim.muon_orthogonalize updates.
+
+Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.
+"""
+import torch
+
+from . import prism
+
+
+class _NormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, options):
+        ctx.save_for_backward(q, k, q_weight, k_weight)
+        ctx.options = options
+        return prism.qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, **options)
+
+    @staticmethod
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight = ctx.saved_tensors
+        # the gradient of a result that nothing reads is None
+        dq_out, dk_out = (torch.zeros_like(t) if g is None else _rows(g) for g, t in ((dq_out, q), (dk_out, k)))
+        dq, dk, dqw, dkw = prism.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight=q_weight, k_weight=k_weight, **ctx.options)
+        return dq, dk, dqw if q_weight is not None else None, dkw if k_weight is not None else None, None
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, options):
+        out, lse = prism.attention(q, k, v, **options)
+        ctx.save_for_backward(q, k, v, out, lse)
+        ctx.options = options
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        return prism.attention_backward(_rows(dout), *ctx.saved_tensors, **ctx.options) + (None,)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed, offset):
+        ctx.args = p, seed, offset
+        return prism.dropout(x, p, seed, offset=offset, residual=residual)
+
+    @staticmethod
+    def backward(ctx, dy):
+        p, seed, offset = ctx.args
+        dx = prism.dropout(dy.contiguous(), p, seed, offset=offset) if ctx.needs_input_grad[0] else None
+        return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
+
+
+def _rows(t):
+    """The entries of every head next to each other (autograd hands out expanded gradients)."""
+    return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
+
+
+def norm_rope(q, k, q_weight=None, k_weight=None, **options):
+    """prism.qk_norm_rope of queries and keys with gradients for them and the weights; options: inv_freq, positions, start, norm, interleaved, scale, eps."""
+    return _NormRope.apply(q, k, q_weight, k_weight, options)
+
+
+def attention(q, k, v, **options):
+    """prism.attention with gradients for q, k and v; options: scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc."""
+    return _Attention.apply(q, k, v, options)
+
+
+def dropout(x, p, seed, offset=0, residual=None):
+    """prism.dropout with gradients for x and the residual."""
+    return _Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(), p, seed, offset)
+
+
+class SelfAttention(torch.nn.Module):
+    """x + dropout(attention(x w_qkv) w_out): one projection for queries, keys and values, whose parts are used as views; norms of the heads of queries and
+    keys, rotation by position, scores capped at will; queries in groups of heads / k_heads share a key head."""
+
+    def __init__(self, width, heads, k_heads=None, head_dim=None, rot_dim=None, softcap=0.0, p=0.0, base=10000.0, dtype=torch.bfloat16, device="cuda"):
+        super().__init__()
+        self.heads, self.k_heads, self.dim = heads, k_heads or heads, head_dim or width // heads
+        self.softcap, self.p = softcap, p
+        inner = (self.heads + 2 * self.k_heads) * self.dim
+        self.w_qkv = torch.nn.Parameter(torch.randn(inner, width, dtype=dtype, device=device) * width ** -0.5)
+        self.w_out = torch.nn.Parameter(torch.randn(width, self.heads * self.dim, dtype=dtype, device=device) * (self.heads * self.dim) ** -0.5)
+        self.q_weight = torch.nn.Parameter(torch.ones(self.dim, device=device))
+        self.k_weight = torch.nn.Parameter(torch.ones(self.dim, device=device))
+        inv_freq, self.rope_scale = prism.rope_frequencies(rot_dim or self.dim, base=base, device=device)
+        self.register_buffer("inv_freq", inv_freq, persistent=False)
+
+    def _project(self, x, positions):
+        b, n, _ = x.shape
+        hq, hk, d = self.heads, self.k_heads, self.dim
+        q, k, v = (x @ self.w_qkv.t()).view(b, n, hq + 2 * hk, d).split([hq, hk, hk], dim=2)
+        q, k = norm_rope(q, k, self.q_weight, self.k_weight, inv_freq=self.inv_freq, positions=positions, scale=self.rope_scale)
+        return q, k, v
+
+    def forward(self, x, positions=None, doc=None, seed=0, offset=0):
+        """x [batch, token, width]; positions and documents int32 [batch, token] (a negative document is padding)."""
+        b, n, _ = x.shape
+        q, k, v = self._project(x, positions)
+        y = attention(q, k, v, causal=True, softcap=self.softcap, q_doc=doc, k_doc=doc).reshape(b, n, -1) @ self.w_out.t()
+        return dropout(y, self.p if self.training else 0.0, seed, offset, residual=x)
+
+    def new_cache(self, batch, length):
+        """Keys and values of up to `length` tokens, and how many there are of each sequence."""
+        make = lambda: torch.zeros(batch, length, self.k_heads, self.dim, dtype=self.w_qkv.dtype, device=self.w_qkv.device)   # noqa: E731
+        return make(), make(), torch.zeros(batch, dtype=torch.int32, device=self.w_qkv.device)
+
+    @torch.no_grad()
+    def step(self, x, cache):
+        """One token of each sequence, x [batch, 1, width], behind the tokens in the cache, which takes it in."""
+        keys, values, lens = cache
+        b = x.shape[0]
+        q, k, v = self._project(x, lens.view(b, 1))
+        at = torch.arange(b, device=x.device), lens.long()
+        keys[at], values[at] = k[:, 0], v[:, 0]
+        lens += 1
+        out, _ = prism.attention(q, keys, values, softcap=self.softcap, k_lens=lens)
+        return x + out.reshape(b, 1, -1) @ self.w_out.t()
