@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
     float top = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      s[kb] = rows_by_rows<T, DP>(kt, 32 * kb, qf, p.dim, lane);
+      s[kb] = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
       scores<T>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
       if (need) {
 #pragma unroll
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
         s[kb][e] = __builtin_amdgcn_exp2f(s[kb][e] * mul - m);
         l += s[kb][e];
       }
-      columns_by<T, DP>(acc, vt, 32 * kb, s[kb], p.dim, lane);
+      columns_by<T, DP>(acc, vt, 32 * kb, s[kb], lane);
     }
   }
   l += other_half(l);
@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {
       s[e] = __builtin_amdgcn_exp2f(s[e] * mul - m);
       l += s[e];
     }
-    columns_by<T, DP>(acc, mine + TB + buf * TB, 0, s, DP, lane);
+    columns_by<T, DP>(acc, mine + TB + buf * TB, 0, s, lane);
   }
   l += other_half(l);
   __syncthreads();
@@ -568,10 +568,13 @@ AttnPlan attention_plan(const prism_attention_desc& d, int dt, bool backward) {
   AttnPlan a = {};
   const long long pairs = (long long)d.batch * d.k_heads, R = (long long)(d.q_heads / d.k_heads) * d.q_len;
   const int kt = dt == PRISM_F32 ? 32 : 64;
-  // Launches that leave CUs without work are cut along the other axis, into parts of four tiles at least.
-  auto parts = [](long long groups, long long tiles) {
+  // Launches that leave CUs without work are cut along the other axis, into parts of four tiles at least: 512 workgroups, two per CU.  Under the causal mask parts are of
+  // unequal length; in fp32, where products outweigh the join, twice as many even that out (2 x 2048 x 8 heads of 80: forward 222 us with 512, 153 with 1024; gradients of heads of
+  // 64: 462 and 392).  Not where one workgroup fits a CU (gradients of heads of 80: 547 and 562) nor in bf16 (2 x 1111, heads of 128: 88 and 101).
+  const int target = dt == PRISM_F32 && d.causal && !(backward && d.head_dim > 64) ? 1024 : 512;
+  auto parts = [target](long long groups, long long tiles) {
     if (groups == 0) return 1;
-    const long long want = 512 / groups, most = (tiles + 3) / 4;
+    const long long want = target / groups, most = (tiles + 3) / 4;
     const long long n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
   };
@@ -640,7 +643,8 @@ int launch_attention(const void* q, const void* k, const void* v, void* out, flo
   p.direct = p.direct && rows_are_vectors(out, d.out, dt);
   // The parts were counted for the kernel that the sizes ask for; what it cannot read (rows that are no whole vectors) the other one takes in the same parts.
   const bool few = plan.few && p.direct;
-  if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, few, s) : launch<float, 128>(p, few, s);
+  if (dt == PRISM_F32)
+    return d.head_dim <= 32 ? launch<float, 32>(p, few, s) : d.head_dim <= 64 ? launch<float, 64>(p, few, s) : d.head_dim <= 96 ? launch<float, 96>(p, few, s) : launch<float, 128>(p, few, s);
   return d.head_dim <= 64 ? launch<__bf16, 64>(p, few, s) : launch<__bf16, 128>(p, few, s);
 }
 

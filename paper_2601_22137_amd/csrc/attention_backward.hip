@@ -39,9 +39,10 @@ template <typename T, int DP> __device__ inline float product_with_row(const Fra
 }
 
 // Also, by the first part of a row tile's keys: stat[pair][0][r] = log2 of the row's sum of weights, +inf where the row sees nothing (its weights are then 0
-// everywhere), and stat[pair][1][r] = D, for dk and dv.  (fp32)
+// everywhere), and stat[pair][1][r] = D, for dk and dv.  (fp32)  Two waves per SIMD where that needs no spill: heads up to 64; with heads of 80 to 96 252 bytes of scratch made both
+// gradients of 2 x 2048 x 8 heads of 80 545 -> 764 us.
 template <typename T, int DP>
-__global__ void __launch_bounds__(NT, 1) attention_dq_kernel(Attn p, float* stat) {
+__global__ void __launch_bounds__(NT, DP <= 64 ? 2 : 1) attention_dq_kernel(Attn p, float* stat) {
   using L = Lds<T, DP>;
   constexpr int KT = key_tile<T>(), KB = KT / 32, TB = KT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys and values, two tiles of each
@@ -103,8 +104,8 @@ __global__ void __launch_bounds__(NT, 1) attention_dq_kernel(Attn p, float* stat
     const char *kt = smem + buf * TB, *vt = smem + (2 + buf) * TB;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      f32x16 s = rows_by_rows<T, DP>(kt, 32 * kb, qf, p.dim, lane);
-      f32x16 ds = rows_by_rows<T, DP>(vt, 32 * kb, dof, p.dim, lane);
+      f32x16 s = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
+      f32x16 ds = rows_by_rows<T, DP>(vt, 32 * kb, dof, lane);
       if (cap) scores<T>(p, s, w, 0, true, false, in, out);
       f32x16 f = s;                                          // capped, not yet biased
       if (bias) scores<T>(p, s, w, j0 + 32 * kb + 4 * h, false, true, cap ? 1.0f : in, out);
@@ -124,7 +125,7 @@ __global__ void __launch_bounds__(NT, 1) attention_dq_kernel(Attn p, float* stat
         ds[e] = __builtin_amdgcn_exp2f(s[e] * mul - lse2) * (ds[e] - delta);
         if (cap) ds[e] *= slope_of_cap(f[e], per);
       }
-      columns_by<T, DP>(acc, kt, 32 * kb, ds, p.dim, lane);
+      columns_by<T, DP>(acc, kt, 32 * kb, ds, lane);
     }
   }
   if (r >= p.R) return;
@@ -398,8 +399,9 @@ __device__ inline void store_dkv(const Attn& p, const f32x16 (&dk)[DP / 32], con
   }
 }
 
+// dk and dv in fp32.  One wave per SIMD above heads of 32: at two, heads of 64 spilled 312 bytes and took 532 us in place of 402 (both gradients, 2 x 2048 x 8 heads).
 template <typename T, int DP>
-__global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const float* stat) {
+__global__ void __launch_bounds__(NT, DP <= 32 ? 2 : 1) attention_dkv_kernel(Attn p, const float* stat) {
   using L = Lds<T, DP>;
   constexpr int RT = key_tile<T>(), RBK = RT / 32, TB = RT * L::RB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // queries and dout, two tiles of each
@@ -473,7 +475,7 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
     const char *qt = smem + buf * TB, *dot = smem + (2 + buf) * TB;
 #pragma unroll
     for (int rb = 0; rb < RBK; ++rb) {
-      f32x16 s = rows_by_rows<T, DP>(qt, 32 * rb, kf, p.dim, lane);
+      f32x16 s = rows_by_rows<T, DP>(qt, 32 * rb, kf, lane);
       f32x16 f;
       if (cap) {
 #pragma unroll
@@ -502,8 +504,8 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(s[4 * g + e] * mul - ls[e]);
       }
-      columns_by<T, DP>(dv, dot, 32 * rb, s, p.dim, lane);
-      f32x16 dp = rows_by_rows<T, DP>(dot, 32 * rb, vf, p.dim, lane);
+      columns_by<T, DP>(dv, dot, 32 * rb, s, lane);
+      f32x16 dp = rows_by_rows<T, DP>(dot, 32 * rb, vf, lane);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4 de = *(const f32x4*)&delta[buf][32 * rb + 8 * g + 4 * h];
@@ -513,7 +515,7 @@ __global__ void __launch_bounds__(NT, 1) attention_dkv_kernel(Attn p, const floa
           if (cap) dp[4 * g + e] *= f[4 * g + e];
         }
       }
-      columns_by<T, DP>(dk, qt, 32 * rb, dp, p.dim, lane);
+      columns_by<T, DP>(dk, qt, 32 * rb, dp, lane);
     }
   }
   store_dkv<T, DP>(p, dk, dv, part, pair, b, kh, j, h);
@@ -824,7 +826,8 @@ int launch_attention_backward(const void* dout, const void* q, const void* k, co
   p.whole = p.whole && p.direct && 32 % G == 0;
   for (const prism_strides& x : {d.q, d.dout}) p.whole = p.whole && x.token * (32 / G) + x.head * G < (1ll << 28);
   float* stat = (float*)(ws + plan.o_stat);
-  if (dt == PRISM_F32) return d.head_dim <= 64 ? launch<float, 64>(p, plan, stat, s) : launch<float, 128>(p, plan, stat, s);
+  if (dt == PRISM_F32)
+    return d.head_dim <= 32 ? launch<float, 32>(p, plan, stat, s) : d.head_dim <= 64 ? launch<float, 64>(p, plan, stat, s) : d.head_dim <= 96 ? launch<float, 96>(p, plan, stat, s) : launch<float, 128>(p, plan, stat, s);
   return d.head_dim <= 64 ? launch<__bf16, 64>(p, plan, stat, s) : launch<__bf16, 128>(p, plan, stat, s);
 }
 

@@ -63,10 +63,11 @@ __device__ inline int here(int x) {
 // The value is there at this point of the program: a sum is not put off to where it is used.
 __device__ inline void keep(float& a) { asm volatile("" : "+v"(a)); }
 
-// Tiles of rows of DP elements in LDS (the head size rounded up to 64 or 128; entries past it are zero), in chunks of 16 bytes.  Chunk c of row r lies at c ^ swizzle(r):
+// Tiles of rows in LDS, of 64 or 128 elements, of which products take the first DP (the head size rounded up: bf16 to 64 or 128, fp32 to 32, 64, 96 or 128; entries past
+// the head are zero), in chunks of 16 bytes.  Chunk c of row r lies at c ^ swizzle(r):
 // the reads of 16 rows at one chunk (the operand as it is), of 4 rows at four chunks (the transposed one, bf16) and of two rows four apart (fp32) then fall on different banks.
 template <typename T, int DP> struct Lds {
-  static constexpr int RB = DP * (int)sizeof(T), CPR = RB / 16, EPC = 16 / (int)sizeof(T), STEPS = CPR / 2;
+  static constexpr int RB = (DP > 64 ? 128 : 64) * (int)sizeof(T), CPR = RB / 16, EPC = 16 / (int)sizeof(T), STEPS = DP / EPC / 2;
   __device__ static int swizzle(int r) {
     if constexpr (CPR == 8) return ((r >> 2) & 3) | ((r >> 1) & 1) << 2;
     else if constexpr (sizeof(T) == 2) return ((r >> 2) & 3) | (r & 3) << 2;
@@ -198,16 +199,14 @@ template <typename T> __device__ inline f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
 
 // (32 rows of the tile from row0 on) x (the rows held as f): register r of lane (n, h) gets row 8 (r / 4) + 4 h + r % 4 against row n of f
 template <typename T, int DP>
-__device__ inline f32x16 rows_by_rows(const char* lds, int row0, const Frag<T, DP>& f, int dim, int lane) {
+__device__ inline f32x16 rows_by_rows(const char* lds, int row0, const Frag<T, DP>& f, int lane) {
   using L = Lds<T, DP>;
   const int r = lane & 31, h = lane >> 5;
   f32x16 c = {};
 #pragma unroll
   for (int s = 0; s < L::STEPS; ++s) {
-    if (2 * s * L::EPC < dim) {
-      const u32x4 a = *(const u32x4*)(lds + (row0 + r) * L::RB + (((2 * s + h) ^ L::swizzle(r)) << 4));
-      c = mma<T>(a, f[s], c);
-    }
+    const u32x4 a = *(const u32x4*)(lds + (row0 + r) * L::RB + (((2 * s + h) ^ L::swizzle(r)) << 4));
+    c = mma<T>(a, f[s], c);
   }
   return c;
 }
@@ -215,7 +214,7 @@ __device__ inline f32x16 rows_by_rows(const char* lds, int row0, const Frag<T, D
 // acc[t] += (columns 32 t .. of 32 rows of the tile, transposed) x p: entry (d, n) gets sum over the rows of tile[row][d] p[row][n].  p is rounded to the
 // tile's type: in bf16 its relative error of 2^-9 is that of the results themselves.
 template <typename T, int DP>
-__device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int row0, const f32x16& p, int dim, int lane) {
+__device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int row0, const f32x16& p, int lane) {
   using L = Lds<T, DP>;
   const int h = lane >> 5;
   if constexpr (sizeof(T) == 2) {
@@ -244,10 +243,8 @@ __device__ inline void columns_by(f32x16 (&acc)[DP / 32], const char* lds, int r
       const int row = 8 * (r >> 2) + 4 * h + (r & 3);
 #pragma unroll
       for (int t = 0; t < DP / 32; ++t) {
-        if (32 * t < dim) {
-          const float a = *(const float*)(lds + (row0 + row) * L::RB + (((8 * t + (n >> 2)) ^ L::swizzle(row)) << 4) + 4 * (n & 3));
-          acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], acc[t], 0, 0, 0);
-        }
+        const float a = *(const float*)(lds + (row0 + row) * L::RB + (((8 * t + (n >> 2)) ^ L::swizzle(row)) << 4) + 4 * (n & 3));
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], acc[t], 0, 0, 0);
       }
     }
   }
