@@ -5,6 +5,10 @@
 // A workgroup takes 128 rows (32 per wave, on the lanes) of a pair and walks the keys in tiles that all four waves share in LDS, two of them in
 // flight.  Scores come out of the product K Q^T with a row per lane, so a row's maximum and sum are plain arithmetic in its own two lanes, and the
 // weights go from the registers straight into V^T P^T (attention_tile.h).
+//
+// Scores, maxima, sums and results are held in 32 bits; the weights are rounded to the type of the values for the second product.  Long prompts in bf16 are bound by the reads of
+// LDS (every wave reads all keys and values of a tile for its 32 rows) and the power limit: 8192 tokens, 32 heads of 128 on 8, causal: 520 us, 1.06 PFLOP/s of the 1.32 that a large
+// product of the vendor library reaches.  Twice the rows per wave halve the reads, but leave one wave per SIMD: 614 us.
 #include "attention_tile.h"
 
 namespace prism {
@@ -43,7 +47,8 @@ __device__ inline void finish(const Attn& p, const f32x16 (&acc)[DP / 32], float
   }
 }
 
-// (fp32)
+// (fp32) Bound by the matrix units' waits for its operands and, in short calls, by how evenly the parts fill the chip: 2 x 2048 x 8 heads of 128, causal: 199 us, 86 TFLOP/s of the
+// pairs that are seen; 2 x 4096, all seen, 1094 us, 126 of 154.
 template <typename T, int DP>
 __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
   using L = Lds<T, DP>;
@@ -361,6 +366,8 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
 // Few rows (32 of a pair at most, as when single tokens are generated for a group of heads): the time is that of reading the keys and values once.  Every wave
 // takes blocks of 32 keys of its own, with no barrier between them, through its own part of LDS (as an operand straight from memory every load of keys would touch 32 lines):
 // the keys are read into registers at once, which makes room for the next block's, the values lie in two blocks.  The waves' results are joined in LDS.
+// 8 tokens of 32 heads on 8 of 128, 4096 to 16384 keys, capped: 75 us and 5 for the join, 4.5 TB/s; with the kernel above 105.  One token of 8 heads on 2, 32768 keys: 13.9 and 20.2; 8 on
+// 2048 keys each: 21.9 and 19.5, where its join of four waves shows.
 template <int DP, bool MOD>
 __global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {
   typedef __bf16 T;

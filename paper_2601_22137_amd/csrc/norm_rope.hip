@@ -6,6 +6,9 @@
 // A head is cut into units of eight pairs, a lane takes one: two vectors of eight elements, from the two halves of the rotated part or next to each
 // other, so the partner of an element is always in the same lane.  2, 4, 8 or 16 lanes make a head and share the sum of squares.  The angle is taken in
 // turns in 64 bits (32 would lose 0.004 rad at position 10^5); a lane computes its eight sines and cosines once and uses them for HS heads of its token.
+//
+// Bound by memory: every entry is read and written once (gradients: two read, one written), sums and statistics are in 32 bits, results are rounded once.  4 x 4096 tokens,
+// 32 + 8 heads of 128, bf16: 80 us (335 MB, 4.2 TB/s) and gradients 109 + 6 us (503 MB, 4.6 TB/s); a large copy runs at 4.6 to 5.4.
 #include "layer.h"
 
 namespace prism {
@@ -304,6 +307,7 @@ bool fits_vectors(const prism_norm_rope_desc& d) {
 }
 
 // Heads per lane share the sines of their token: four (gradients: two, whose operands fill as many registers) where that leaves the chip four waves per SIMD.
+// 4 x 4096 tokens, 32 + 8 heads of 128: one head a lane 114 us and gradients 111, shared 84 and 106; 2048 tokens: 13.9 and 23.2, shared 12.4 and 21.3 (always two: 22.5).
 int heads_per_lane(const prism_norm_rope_desc& d, int L, int most) {
   const long long waves = (long long)d.batch * d.len * (d.q_heads + d.k_heads) * L / 64;
   while (most > 1 && waves < most * 4096ll) most /= 2;
