@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
         else if constexpr (THIS) vf[x + AHEAD - NK] = read_v(buf, x + AHEAD - NK);
         n[x / STEPS] = mma<T>(kf[x % (AHEAD + 1)], qf[x % STEPS], n[x / STEPS]);
         if constexpr (THIS) {
-          steps<16 / NK>([&](auto e) { weigh(x * (16 / NK) + decltype(e)::value); });
+          share<NK, 16>(xt, [&](auto e) { weigh(decltype(e)::value); });
           keep(l[0]);
           keep(l[1]);
         }
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
     }
     if constexpr (THIS) {
       steps<NP>([&](auto xt) {
-        constexpr int x = decltype(xt)::value, g = x / TD, E = 32 / NP;
+        constexpr int x = decltype(xt)::value, g = x / TD;
         if constexpr (x + AHEAD < NP) vf[(x + AHEAD) % (AHEAD + 1)] = read_v(buf, x + AHEAD);
         if constexpr (x % TD == 0) {
 #pragma unroll
@@ -250,12 +250,11 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
         }
         acc[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x % (AHEAD + 1)], weights, acc[x % TD], 0, 0, 0);
         if constexpr (x < NP / 2) {
-          steps<E>([&](auto e) { weigh(16 + x * E + decltype(e)::value); });
+          share<NP / 2, 16>(xt, [&](auto e) { weigh(16 + decltype(e)::value); });
           keep(l[0]);
           keep(l[1]);
         } else if constexpr (NEXT && !MOD) {
-          constexpr int y = (x - NP / 2) * 2 * E;
-          steps<E>([&](auto e) { constexpr int z = y + 2 * decltype(e)::value; top = max_of(top, n[z >> 4][z & 15], n[z >> 4][(z & 15) + 1]); });
+          share<NP / 2, 16>(std::integral_constant<int, x - NP / 2>{}, [&](auto e) { constexpr int z = 2 * decltype(e)::value; top = max_of(top, n[z >> 4][z & 15], n[z >> 4][(z & 15) + 1]); });
           keep(top);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -652,7 +651,7 @@ int launch_attention(const void* q, const void* k, const void* v, void* out, flo
   const bool few = plan.few && p.direct;
   if (dt == PRISM_F32)
     return d.head_dim <= 32 ? launch<float, 32>(p, few, s) : d.head_dim <= 64 ? launch<float, 64>(p, few, s) : d.head_dim <= 96 ? launch<float, 96>(p, few, s) : launch<float, 128>(p, few, s);
-  return d.head_dim <= 64 ? launch<__bf16, 64>(p, few, s) : launch<__bf16, 128>(p, few, s);
+  return d.head_dim <= 64 ? launch<__bf16, 64>(p, few, s) : d.head_dim <= 96 ? launch<__bf16, 96>(p, few, s) : launch<__bf16, 128>(p, few, s);
 }
 
 }  // namespace prism

@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
         steps<STEPS>([&](auto xt) {
           constexpr int x = decltype(xt)::value;
           c = mma<T>(next(std::integral_constant<int, decltype(first)::value + x>{}), f[x], c);
-          steps<16 / STEPS>([&](auto et) { work(std::integral_constant<int, x * (16 / STEPS) + decltype(et)::value>{}); });
+          share<STEPS, 16>(xt, work);
           __builtin_amdgcn_sched_barrier(0);
         });
       };
@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
       f32x4 row4, slope4;
       int4 place4;
       steps<STEPS>([&](auto xt) {
-        constexpr int x = decltype(xt)::value, E = 16 / STEPS;
+        constexpr int x = decltype(xt)::value;
         u32x4 v;
         if constexpr (V_IN_LDS) {
           if constexpr (x + 1 < STEPS) vop[(x + 1) & 1] = lds_read16(va ^ ((x + 1) << 5));
@@ -694,8 +694,8 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
           v = vf[x];
         }
         dp = mma<T>(next(std::integral_constant<int, STEPS + x>{}), v, dp);
-        steps<E>([&](auto et) {
-          constexpr int e = x * E + decltype(et)::value;
+        share<STEPS, 16>(xt, [&](auto et) {
+          constexpr int e = decltype(et)::value;
           if constexpr (e % 4 == 0) {
             constexpr int r4 = 8 * (e / 4);
             row4 = *(const f32x4*)&lse2[buf][32 * rb + r4 + 4 * h];
@@ -718,10 +718,10 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
         __builtin_amdgcn_sched_barrier(0);
       });
       steps<NC>([&](auto xt) {
-        constexpr int x = decltype(xt)::value, E = 16 / NC;
+        constexpr int x = decltype(xt)::value;
         dv[x % TD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, next(std::integral_constant<int, 2 * STEPS + x>{})), weights[x / TD], dv[x % TD], 0, 0, 0);
-        steps<E>([&](auto et) {
-          constexpr int e = x * E + decltype(et)::value;
+        share<NC, 16>(xt, [&](auto et) {
+          constexpr int e = decltype(et)::value;
           if constexpr (e % 4 == 0) row4 = *(const f32x4*)&delta[buf][32 * rb + 8 * (e / 4) + 4 * h];
           grads[e >> 3][e & 7] = (__bf16)(s[e] * (dp[e] - row4[e & 3]));
         });
@@ -832,7 +832,7 @@ int launch_attention_backward(const void* dout, const void* q, const void* k, co
   float* stat = (float*)(ws + plan.o_stat);
   if (dt == PRISM_F32)
     return d.head_dim <= 32 ? launch<float, 32>(p, plan, stat, s) : d.head_dim <= 64 ? launch<float, 64>(p, plan, stat, s) : d.head_dim <= 96 ? launch<float, 96>(p, plan, stat, s) : launch<float, 128>(p, plan, stat, s);
-  return d.head_dim <= 64 ? launch<__bf16, 64>(p, plan, stat, s) : launch<__bf16, 128>(p, plan, stat, s);
+  return d.head_dim <= 64 ? launch<__bf16, 64>(p, plan, stat, s) : d.head_dim <= 96 ? launch<__bf16, 96>(p, plan, stat, s) : launch<__bf16, 128>(p, plan, stat, s);
 }
 
 }  // namespace prism

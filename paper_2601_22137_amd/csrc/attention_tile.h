@@ -54,6 +54,12 @@ template <int D, typename F> __device__ __forceinline__ void steps(F&& f) {
   }
 }
 
+// f(e) for step x's share of TOTAL entries that are spread over N steps
+template <int N, int TOTAL, int X, typename F> __device__ __forceinline__ void share(std::integral_constant<int, X>, F&& f) {
+  constexpr int from = X * TOTAL / N, to = (X + 1) * TOTAL / N;
+  steps<to - from>([&](auto e) __attribute__((always_inline)) { f(std::integral_constant<int, from + decltype(e)::value>{}); });
+}
+
 // The same value, computed again where it is used: what the rare branches of a loop derive from it is not kept in registers across the loop.
 __device__ inline int here(int x) {
   asm volatile("" : "+v"(x));
@@ -63,8 +69,8 @@ __device__ inline int here(int x) {
 // The value is there at this point of the program: a sum is not put off to where it is used.
 __device__ inline void keep(float& a) { asm volatile("" : "+v"(a)); }
 
-// Tiles of rows in LDS, of 64 or 128 elements, of which products take the first DP (the head size rounded up: bf16 to 64 or 128, fp32 to 32, 64, 96 or 128; entries past
-// the head are zero), in chunks of 16 bytes.  Chunk c of row r lies at c ^ swizzle(r):
+// Tiles of rows in LDS, of 64 or 128 elements, of which products take the first DP (the head size rounded up to 64, 96 or 128, fp32 also 32; entries past
+// the head are zero), in chunks of 16 bytes.  2 x 4096 x 8 heads of 80, causal, bf16: 103 us and gradients 349 with products of 128 entries, 91 and 297 with 96.  Chunk c of row r lies at c ^ swizzle(r):
 // the reads of 16 rows at one chunk (the operand as it is), of 4 rows at four chunks (the transposed one, bf16) and of two rows four apart (fp32) then fall on different banks.
 template <typename T, int DP> struct Lds {
   static constexpr int RB = (DP > 64 ? 128 : 64) * (int)sizeof(T), CPR = RB / 16, EPC = 16 / (int)sizeof(T), STEPS = DP / EPC / 2;

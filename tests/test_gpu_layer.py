@@ -338,6 +338,16 @@ def test_attention_cap_and_bias(prism, dtype, softcap, bias):
     _check_attention(prism, dtype, 1, 70, 150, 4, 2, 64, softcap=softcap, slopes=_slopes(4) if bias else None, q_scale=6.0, seed=3)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [24, 32, 40, 65, 72, 80, 96, 104])
+@pytest.mark.parametrize("softcap,bias", [(0.0, False), (0.0, True), (10.0, False), (10.0, True)])
+def test_attention_widths_of_the_products(prism, dtype, d, softcap, bias):
+    """Heads on both sides of every width that products come in; then few rows against many keys."""
+    kw = dict(softcap=softcap, slopes=_slopes(4) if bias else None, q_scale=3.0)
+    _check_attention(prism, dtype, 1, 203, 203, 4, 2, d, causal=True, seed=d, **kw)
+    _check_attention(prism, dtype, 2, 3, 700, 4, 2, d, causal=True, k_lens=[700, 333], seed=d + 1, **kw)
+
+
 def _docs(lengths, pad=0):
     return sum([[i] * x for i, x in enumerate(lengths)], []) + [-1] * pad
 
