@@ -7,7 +7,7 @@
 // weights go from the registers straight into V^T P^T (attention_tile.h).
 //
 // Scores, maxima, sums and results are held in 32 bits; the weights are rounded to the type of the values for the second product.  Long prompts in bf16 are bound by the reads of
-// LDS (every wave reads all keys and values of a tile for its 32 rows) and the power limit: 8192 tokens, 32 heads of 128 on 8, causal: 520 us, 1.06 PFLOP/s of the 1.32 that a large
+// LDS (every wave reads all keys and values of a tile for its 32 rows) and the power limit: 8192 tokens, 32 heads of 128 on 8, causal: 511 us, 1.08 PFLOP/s of the 1.32 that a large
 // product of the vendor library reaches.  Twice the rows per wave halve the reads, but leave one wave per SIMD: 614 us.
 #include "attention_tile.h"
 
