@@ -6,7 +6,7 @@
 // shared heads need no sum afterwards).  Seven products instead of five, but no sum across workgroups whose order could change the bits of dq.
 //
 // Scores, dp, D and all sums are held in 32 bits; p and ds are rounded to the operands' type for the products that follow, as results are.  2 x 4096 tokens, 16 heads of 128 on 4, causal,
-// capped, bf16: dq 296 us (tanh and exp, two transcendental instructions each, beside three products), dk and dv 485 and 24 for the sum of their parts (four products; waits for the
+// capped, bf16: dq 300 us (tanh and exp, two transcendental instructions each, beside three products), dk and dv 485 and 24 for the sum of their parts (four products; waits for the
 // tiles); 2 x 1111, 8 heads of 80 with prefix and bias in fp32: 116 and 163.
 #include "attention_tile.h"
 
