@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(NT, DP <= 32 ? 2 : 1) attention_dkv_kernel(Att
   const T* qbase = (const T*)p.q + b * p.qs[0] + kh * p.G * p.qs[2];
   const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
   const float* st = stat + (long long)pair * 2 * p.R;
-  Chunks<T, DP, RT> qat, doat;
+  Chunks<T, DP, RT, true> qat, doat;
   if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole) {
     qat.set(tid, p.G, p.qs[1], p.qs[2], p.dim);
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
   const float* st = stat + (long long)pair * 2 * p.R;
   // Where the group divides 32, a tile's rows lie alike in every tile
-  Chunks<T, DP, RT> qat, doat;
+  Chunks<T, DP, RT, true> qat, doat;
   if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole) {
     qat.set(tid, p.G, p.qs[1], p.qs[2], p.dim);

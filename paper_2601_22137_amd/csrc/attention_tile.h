@@ -6,6 +6,7 @@
 // may run in any order, so the eight registers 8 s .. 8 s + 7 are taken as they lie, and the first operand is read to match.
 #pragma once
 #include "layer.h"
+#include "tile_rows.h"
 
 namespace prism {
 namespace {
@@ -114,24 +115,25 @@ template <int BYTES> __device__ inline void zero_tiles(char* lds, int tid) {
   __syncthreads();
 }
 
-// The same for whole tiles of rows.  The chunks of a thread lie a fixed number of rows apart: one offset and a uniform step where the swizzle repeats at that distance,
-// two offsets in turn for rows of 512 bytes (8 apart).
-template <typename T, int DP, int ROWS> struct Chunks {
+// The same for whole tiles of rows.  The chunks of a thread lie a fixed number of rows apart: one offset and uniform steps (tile_rows.h) where the swizzle repeats at that
+// distance, two offsets in turn for rows of 512 bytes (8 apart).  GROUPS: rows are heads of tokens; else every row is a token of its own.
+template <typename T, int DP, int ROWS, bool GROUPS = false> struct Chunks {
   static constexpr int APART = NT / Lds<T, DP>::CPR, N = ROWS / APART, KINDS = APART < 16 ? 2 : 1;
+  static_assert(N <= 4, "row_steps");
   unsigned at[KINDS];
-  long long step;
+  RowSteps steps;      // bytes
   bool any[KINDS];   // a chunk past the head's entries stays as zero_tiles has left it
   // row x is token x / G, head x % G (G divides 32) of the first row's token
   __device__ void set(int tid, int G, long long token, long long head, int dim) {
     using L = Lds<T, DP>;
-    const int r = tid / L::CPR, i = r / G;
+    const int r = tid / L::CPR;
 #pragma unroll
     for (int k = 0; k < KINDS; ++k) {
       const int c = (tid % L::CPR) ^ L::swizzle(r + k * APART);
       any[k] = c * L::EPC < dim;
-      at[k] = (unsigned)((i * (int)token + (r - i * G) * (int)head) * (int)sizeof(T)) + (c << 4);
+      at[k] = (unsigned)row_offset(r, G, token, head) * (unsigned)sizeof(T) + (c << 4);
     }
-    step = (G > APART ? APART * head : APART / G * token) * (long long)sizeof(T);
+    steps = row_steps(APART, G, token * (long long)sizeof(T), head * (long long)sizeof(T));
   }
   __device__ void load(char* lds, const char* base, int wave) const {
 #pragma unroll
@@ -141,7 +143,7 @@ template <typename T, int DP, int ROWS> struct Chunks {
       if (any[k])
 #pragma unroll
         for (int u = k; u < N; u += KINDS) {
-          const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(base + u * step);
+          const __attribute__((address_space(1))) char* from = (const __attribute__((address_space(1))) char*)(base + (GROUPS && N > 2 ? steps.to(u) : u * steps.one));
           __builtin_amdgcn_global_load_lds((gptr_t)(from + off), (lptr_t)(lds + (u * NW + wave) * 1024), 16, 0, 0);
         }
     }

@@ -517,3 +517,12 @@ def test_attention_refusals(prism):
     o.q.token = 256
     o.q_heads, o.batch, o.k_len = 4, 1 << 20, 1 << 20
     assert L.prism_attention(q.data_ptr(), k.data_ptr(), k.data_ptr(), q.data_ptr(), None, prism.F32, ctypes.byref(o), None) == prism.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("view", ["plain", "heads_first"])
+@pytest.mark.parametrize("group", [3, 5, 8, 16, 32, 64])
+@pytest.mark.parametrize("d", [64, 80, 128])
+def test_attention_groups_of_heads(prism, dtype, view, group, d):
+    """Groups on both sides of the rows of a tile and of the rows between a thread's chunks, two of them, several whole tiles and a part of one."""
+    _check_attention(prism, dtype, 2, 37, 45, 2 * group, 2, d, view=view, causal=True, seed=group)
