@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       s[kb] = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
-      scores<T>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
+      scores<true>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
       if (need) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -150,8 +150,8 @@ __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
 
 // The same for bf16, with the work of neighbouring tiles interleaved: while the matrix units take K Q^T of tile t + 1, the vector units take the exponentials of
 // tile t, and while those take V^T P^T of tile t, these the exponentials that are left and the maximum of tile t + 1.  The keys run one tile ahead of the
-// values in LDS.  MOD: scores with a cap or a bias.
-template <int DP, bool MOD>
+// values in LDS.  MOD: scores with a cap or a bias; SERIES: of a large cap.
+template <int DP, bool MOD, bool SERIES>
 __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Attn p) {
   typedef __bf16 T;
   using L = Lds<T, DP>;
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
     const int j0 = t * KT;
     if constexpr (MOD) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) scores<T>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
+      for (int kb = 0; kb < 2; ++kb) scores<SERIES>(p, s[kb], w, j0 + 32 * kb + 4 * h, cap, bias, in, out);
     }
     if (need) {
       const int hh = prism::here(h);
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
 // the keys are read into registers at once, which makes room for the next block's, the values lie in two blocks.  The waves' results are joined in LDS.
 // 8 tokens of 32 heads on 8 of 128, 4096 to 16384 keys, capped: 75 us and 5 for the join, 4.5 TB/s; with the kernel above 105.  One token of 8 heads on 2, 32768 keys: 13.9 and 20.2; 8 on
 // 2048 keys each: 21.9 and 19.5, where its join of four waves shows.
-template <int DP, bool MOD>
+template <int DP, bool MOD, bool SERIES>
 __global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {
   typedef __bf16 T;
   using L = Lds<T, DP>;
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {
 #pragma unroll
     for (int x = 0; x < STEPS; ++x) s = mma<T>(kf[x], qf[x], s);
     const int j0 = block * 32 + 4 * h;
-    if constexpr (MOD) scores<T>(p, s, w, j0, cap, bias, in, out);
+    if constexpr (MOD) scores<SERIES>(p, s, w, j0, cap, bias, in, out);
     if (block * 32 + 31 > lim.first) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = j0 + 8 * (e >> 2) + (e & 3) <= w.last ? s[e] : -INFINITY;
@@ -545,12 +545,12 @@ template <typename T, int DP> int launch(Attn& p, bool few, hipStream_t s) {
   if constexpr (sizeof(T) == 4) {
     kernel = attention_kernel<T, DP>;
   } else {
-    const bool mod = p.cap > 0.0f || p.slopes;
+    const bool mod = p.cap > 0.0f || p.slopes, series = p.cap > CAP_SERIES;
     if (few) {
-      kernel = mod ? attention_few_kernel<DP, true> : attention_few_kernel<DP, false>;
+      kernel = series ? attention_few_kernel<DP, true, true> : mod ? attention_few_kernel<DP, true, false> : attention_few_kernel<DP, false, false>;
       bytes = NW * 3 * 32 * Lds<T, DP>::RB;
     } else {
-      kernel = mod ? attention_bf16_kernel<DP, true> : attention_bf16_kernel<DP, false>;
+      kernel = series ? attention_bf16_kernel<DP, true, true> : mod ? attention_bf16_kernel<DP, true, false> : attention_bf16_kernel<DP, false, false>;
     }
   }
   const int rc = allow_dynamic_lds((const void*)kernel, bytes);

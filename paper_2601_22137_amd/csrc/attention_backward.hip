@@ -110,9 +110,9 @@ __global__ void __launch_bounds__(NT, DP <= 64 ? 2 : 1) attention_dq_kernel(Attn
     for (int kb = 0; kb < KB; ++kb) {
       f32x16 s = rows_by_rows<T, DP>(kt, 32 * kb, qf, lane);
       f32x16 ds = rows_by_rows<T, DP>(vt, 32 * kb, dof, lane);
-      if (cap) scores<T>(p, s, w, 0, true, false, in, out);
+      if (cap) scores<true>(p, s, w, 0, true, false, in, out);
       f32x16 f = s;                                          // capped, not yet biased
-      if (bias) scores<T>(p, s, w, j0 + 32 * kb + 4 * h, false, true, cap ? 1.0f : in, out);
+      if (bias) scores<true>(p, s, w, j0 + 32 * kb + 4 * h, false, true, cap ? 1.0f : in, out);
       if (need) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(NT, DP <= 64 ? 2 : 1) attention_dq_kernel(Attn
 // The same in bf16.  A tile of 64 keys is taken as two blocks: scores K Q^T and dp = V dO^T of the first, with its exponentials beside the latter; the scores of the second beside
 // ds of the first; dq; and so on.  D from the rounded `out` is off by 2^-9 of it, which shows where a row sees few keys (elsewhere in the mean over the keys it does not): a
 // workgroup that sees eight tiles at most takes D = sum p dp, in a walk of its own through them.  (Packed documents of 8 x 1024, 12 heads of 64: 45 us, in two launches 54.)
-template <int DP, bool CAP, bool BIAS>
+template <int DP, bool CAP, bool BIAS, bool SERIES>
 __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float* stat) {
   typedef __bf16 T;
   using L = Lds<T, DP>;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
         constexpr int kb = decltype(kbt)::value, e = decltype(et)::value;
         float a = s[kb][e] * in, t2 = 0.0f;
         if constexpr (CAP) {
-          t2 = tanh_of(a, false);
+          t2 = tanh_of<SERIES>(a);
           a = t2 * out;
         }
         if constexpr (BIAS) a -= w.slope * fabsf((float)(w.at - j0 - 4 * h) - (float)(32 * kb + 8 * (e >> 2) + (e & 3)));
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(NT, DP <= 32 ? 2 : 1) attention_dkv_kernel(Att
       if (cap) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[e] = out * tanh_of(s[e] * in, sizeof(T) == 4);
+          s[e] = out * tanh_of<true>(s[e] * in);
           f[e] = slope_of_cap(s[e], per_cap);
         }
       }
@@ -535,7 +535,7 @@ template <int STEPS, int NC, int AHEAD> constexpr int read_by(int x) {
 // dk and dv in bf16.  Per block of 32 rows: scores Q K^T, then dp = dO V^T while the exponentials are taken, then dv while ds is, then dk; the operands of every product are read from LDS a few products ahead.
 // Two waves per SIMD have 256 registers each: 128 of them are sums at DP = 128, so V stays in LDS there (its rows are read again for every block), and
 // tiles of 32 rows leave room for two workgroups per CU.
-template <int DP, bool CAP, bool BIAS>
+template <int DP, bool CAP, bool BIAS, bool SERIES>
 __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const float* stat) {
   typedef __bf16 T;
   using L = Lds<T, DP>;
@@ -706,7 +706,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
           }
           float a = s[e] * in, t2 = 0.0f;
           if constexpr (CAP) {
-            t2 = tanh_of(a, false);
+            t2 = tanh_of<SERIES>(a);
             a = t2 * out;
           }
           if constexpr (BIAS) a -= slope4[e & 3] * fabsf((float)((e & 3) == 0 ? place4.x - j : (e & 3) == 1 ? place4.y - j : (e & 3) == 2 ? place4.z - j : place4.w - j));
@@ -778,14 +778,15 @@ template <typename T, int DP> int launch(Attn& p, const AttnPlan& plan, float* s
     dq = attention_dq_kernel<T, DP>;
     dkv = attention_dkv_kernel<T, DP>;
   } else {
-    auto pick = [&](auto cap, auto bias) {
-      constexpr bool C = decltype(cap)::value, B = decltype(bias)::value;
-      dq = attention_dq_bf16_kernel<DP, C, B>;
-      dkv = attention_dkv_bf16_kernel<DP, C, B>;
+    auto pick = [&](auto cap, auto bias, auto series) {
+      constexpr bool C = decltype(cap)::value, B = decltype(bias)::value, S = decltype(series)::value;
+      dq = attention_dq_bf16_kernel<DP, C, B, S>;
+      dkv = attention_dkv_bf16_kernel<DP, C, B, S>;
     };
     std::true_type yes;
     std::false_type no;
-    p.cap > 0.0f ? (p.slopes ? pick(yes, yes) : pick(yes, no)) : (p.slopes ? pick(no, yes) : pick(no, no));
+    if (p.cap > CAP_SERIES) pick(yes, yes, yes);   // (without slopes they are 0)
+    else p.cap > 0.0f ? (p.slopes ? pick(yes, yes, no) : pick(yes, no, no)) : (p.slopes ? pick(no, yes, no) : pick(no, no, no));
     dkv_bytes = DP > 64 ? (4 * 32 + 128) * Lds<T, DP>::RB : 4 * 64 * Lds<T, DP>::RB;
   }
   int rc = allow_dynamic_lds((const void*)dq, bytes);

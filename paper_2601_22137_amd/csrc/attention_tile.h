@@ -266,10 +266,13 @@ __device__ inline float other_half(float x) {   // the value of lane l ^ 32
   return __shfl_xor(x, 32);
 }
 
-__device__ inline float tanh_of(float x, bool exact) {
-  // 1 - 2 / (1 + e^2x): absolute error of 1e-7, which the scores of bf16 operands do not see; near zero fp32 takes the odd series (to x^13: 2e-9 at 0.3)
+// 1 - 2 / (1 + e^2x): an absolute error of 1e-7, of a score the cap times that.  SERIES: near zero the odd series (to x^13: 2e-9 at 0.3), so that the error is some units of
+// the score itself whatever the cap: in fp32 always, in bf16 above caps of CAP_SERIES (up to it, 1e-7 of the cap is a sixteenth of the weights' own rounding at most).
+// bf16, 2 x 4096 tokens, 16 heads of 128 on 4, causal: forward 214 us without and 236 with the series, gradients 715 and 1552 (dk and dv then spill 228 bytes a work-item).
+constexpr float CAP_SERIES = 1024.0f;
+template <bool SERIES> __device__ inline float tanh_of(float x) {
   const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * LOG2E)));
-  if (!exact) return t;
+  if constexpr (!SERIES) return t;
   const float y = x * x;
   float s = 21844.0f / 6081075.0f;
   s = s * y - 1382.0f / 155925.0f;
@@ -457,11 +460,11 @@ template <int KT> __device__ inline bool tile_seen(const Attn& p, const Limits& 
 
 // Products q.k to what the exponent takes: without cap and bias they stay (the factor is applied with the exponent), else times log2(e), capped, biased.
 // Register r is key j + 8 (r / 4) + r % 4.
-template <typename T>
+template <bool SERIES>
 __device__ inline void scores(const Attn& p, f32x16& s, const Row& w, int j, bool cap, bool bias, float in, float out) {
   if (cap) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = out * tanh_of(s[e] * in, sizeof(T) == 4);
+    for (int e = 0; e < 16; ++e) s[e] = out * tanh_of<SERIES>(s[e] * in);
   } else if (bias) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] *= in;

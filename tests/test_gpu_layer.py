@@ -526,3 +526,39 @@ def test_attention_refusals(prism):
 def test_attention_groups_of_heads(prism, dtype, view, group, d):
     """Groups on both sides of the rows of a tile and of the rows between a thread's chunks, two of them, several whole tiles and a part of one."""
     _check_attention(prism, dtype, 2, 37, 45, 2 * group, 2, d, view=view, causal=True, seed=group)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("n,m,d", [(90, 90, 64), (70, 150, 80), (70, 150, 128), (3, 700, 128)])
+@pytest.mark.parametrize("softcap", [500.0, 3e4, 1e6, 1e9])
+def test_attention_caps_far_above_the_scores(prism, dtype, bias, n, m, d, softcap):
+    """A cap far above the scores leaves them almost as they are: their error is some units of themselves, whatever the cap."""
+    g = torch.Generator().manual_seed(21)
+    q, k, v, do = (_heads(g, 1, x, h, d, dtype, s, "plain") for x, h, s in ((n, 2, 3.0), (m, 1, 1.0), (m, 1, 1.0), (n, 2, 1.0)))
+    sl = _slopes(2) if bias else [0.0, 0.0]
+    opt = dict(causal=True, softcap=softcap, scale=d ** -0.5, slopes=torch.tensor(sl, device="cuda") if bias else None)
+    out, lse = prism.attention(q, k, v, **opt)
+    grads = prism.attention_backward(do, q, k, v, out, lse, **opt)
+    see, far = R.visible(n, m, True)
+    K, V, u = _f64(k)[0, :, 0], _f64(v)[0, :, 0], _u(dtype)
+    total = {x: 0.0 for x in ("dk", "dv", "lim_dk", "lim_dv")}
+    for h in range(2):
+        Q, G = _f64(q)[0, :, h], _f64(do)[0, :, h]
+        r = R.attention_head(Q, K, V, see, far, d ** -0.5, softcap, sl[h], G)
+        mag = d ** -0.5 * (np.abs(Q) @ np.abs(K).T)
+        # a score: a product of d terms, scaling, tanh, cap, bias and reference, some units of its size each, and the plain tanh's 2^-23 of a cap of 1024 at most
+        e = 2.0 ** -24 * ((d / 4 + 24) * (mag + sl[h] * far).max(where=see, initial=0.0) + np.sqrt(m) + 16) + (2.0 ** -23 * min(softcap, 1024.0))
+        p, rel = r["p"], (u if dtype == BF16 else 0.0) + 2 * e
+        lo = u * np.abs(r["out"]) + rel * (p @ np.abs(V))
+        adp, ago = np.abs(G) @ np.abs(V).T, np.sum(np.abs(G * r["out"]), 1, keepdims=True)
+        dD = np.sum(np.abs(G) * lo, 1, keepdims=True) + (d / 4 + 8) * 2.0 ** -24 * ago
+        eds = rel * np.abs(r["ds"]) + d ** -0.5 * p * (dD + (d / 4 + 8) * 2.0 ** -24 * adp + 2 * e * (adp + ago))
+        _close(out[0, :, h], r["out"], lo, "out")
+        assert np.max(np.abs(_f64(lse)[0, h] - r["lse"])) <= 2 * e + 2.0 ** -23 * np.abs(r["lse"]).max()
+        _close(grads[0][0, :, h], r["dq"], u * np.abs(r["dq"]) + eds @ np.abs(K), "dq")
+        for x, t, lim in (("dk", r["dk"], eds.T @ np.abs(Q)), ("dv", r["dv"], rel * (p.T @ np.abs(G)))):
+            total[x] = total[x] + t
+            total["lim_" + x] = total["lim_" + x] + lim
+    _close(grads[1][0, :, 0], total["dk"], u * np.abs(total["dk"]) + total["lim_dk"] + 1e-30, "dk")
+    _close(grads[2][0, :, 0], total["dv"], u * np.abs(total["dv"]) + total["lim_dv"] + 1e-30, "dv")
