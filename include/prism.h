@@ -358,7 +358,7 @@ int prism_norm_rope_workspace_bytes(prism_dtype dt, const prism_norm_rope_desc* 
 typedef struct {
   int32_t batch, q_len, k_len, q_heads, k_heads, head_dim; /* q_heads a multiple of k_heads: head h reads key head h / (q_heads / k_heads) */
   int32_t causal;          /* query i, whose place is i + keys - q_len, sees keys up to its place */
-  float scale;             /* > 0 */
+  float scale;             /* > 0; scale log2(e) has to be finite, scale / softcap and softcap log2(e) normal */
   float softcap;           /* scores become softcap * tanh(scale q.k / softcap); 0: as they are */
   const float* slopes;     /* [q_heads], or NULL: score -= slope |place - key| */
   const int32_t* prefix;   /* [batch], or NULL; causal only: keys below prefix are seen by every query */

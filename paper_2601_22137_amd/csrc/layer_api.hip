@@ -57,6 +57,10 @@ int check(const prism_attention_desc* d, int dt) {
   if (d->k_heads ? d->q_heads == 0 || d->q_heads % d->k_heads : d->q_heads) return refuse("q_heads has to be a multiple of k_heads");
   if (!(d->scale > 0.0f) || !std::isfinite(d->scale)) return refuse("scale has to be positive and finite");
   if (!(d->softcap >= 0.0f) || !std::isfinite(d->softcap)) return refuse("softcap has to be finite and not negative");
+  // the factors that scores are taken times: an infinite one would make NaN of a score of 0, a subnormal one of a cap loses digits
+  const float log2e = 1.4426950408889634f;
+  if (!std::isfinite(d->scale * log2e) || (d->softcap > 0.0f && !(std::isnormal(d->scale / d->softcap) && std::isnormal(d->softcap * log2e))))
+    return refuse("scale log2(e), scale / softcap or softcap log2(e) is out of the range of fp32");
   if (!d->q_doc != !d->k_doc) return refuse("q_doc and k_doc go together");
   if (d->prefix && !d->causal) return refuse("a prefix needs the causal mask");
   if (negative(d->q, d->k, d->v, d->out, d->dout, d->dq, d->dk, d->dv)) return refuse("a stride is negative");

@@ -122,3 +122,13 @@ def test_frequencies(prism):
     for bad in (dict(rot_dim=3), dict(rot_dim=0), dict(rot_dim=8, factor=0.0), dict(rot_dim=8, scaling="none"), dict(rot_dim=8, scaling="by_turns", factor=2.0)):
         with pytest.raises(prism.PrismError):
             prism.rope_frequencies(**bad)
+
+
+@pytest.mark.parametrize("kw", [dict(scale=3e38), dict(softcap=3e38), dict(softcap=1e-39), dict(softcap=1e-38, scale=10.0), dict(softcap=1e30, scale=1e-9)])
+def test_attention_refuses_factors_that_leave_fp32(prism, kw):
+    """Scores are taken times scale log2(e), or scale / softcap and softcap log2(e): an infinity there gives NaN for scores of 0, a subnormal loses digits."""
+    d = _attention(prism, **kw)
+    assert _bytes(prism, d, 0)[0] == prism.EINVAL and _bytes(prism, d, 1)[0] == prism.EINVAL
+    assert b"softcap" in prism.lib().prism_last_error()
+    for kw in (dict(scale=1e37), dict(scale=1e-40), dict(softcap=1e37), dict(softcap=1e-30)):
+        assert _bytes(prism, _attention(prism, **kw), 0)[0] == prism.OK
