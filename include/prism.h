@@ -373,7 +373,7 @@ typedef struct {
 
 /* out = softmax of the scores over the keys that a query sees, times v.  lse (fp32 [batch][q_heads][q_len], or NULL) receives the
  * logarithm of the sum of the exponentials, which the backward pass reads.  A query that sees no key gets out = 0 and
- * lse = -inf.  Keys and values past a sequence's length or of a negative document, and queries (and their dout) of a negative document, may
+ * lse = -inf, and gradient 0.  Keys and values past a sequence's length or of a negative document, and queries that see no key (and their dout), may
  * hold anything.  What some query sees has to be finite: where another does not see it, its weight is 0, and 0 times an infinity NaN.
  * bf16 rounds the weights to bf16 before their product with v. */
 int prism_attention(const void* q, const void* k, const void* v, void* out, float* lse, prism_dtype dt,

@@ -25,6 +25,18 @@ __device__ inline float lse2_of(const Attn& p, int b, int i, int head, int r) {
   return lse == -INFINITY ? INFINITY : lse * LOG2E;
 }
 
+// A row that sees nothing has no gradient whatever its query and its dout hold
+template <typename T, int DP> __device__ inline void clear_unseeing(Frag<T, DP>& f, float lse2) {
+#pragma unroll
+  for (int s = 0; s < Lds<T, DP>::STEPS; ++s)
+    if (lse2 == INFINITY) f[s] = (u32x4){0, 0, 0, 0};
+}
+
+// ... and its token's block of documents is marked as one with a query of none, for dk and dv (every workgroup that writes there writes the same)
+__device__ inline void mark_unseeing(const Attn& p, float lse2, int b, int i) {
+  if (p.qdoc && lse2 == INFINITY) ((int*)(p.qrange + (long long)b * ((p.n + 63) / 64) + i / 64))[2] = 1;
+}
+
 // A lane's share of the product of two rows
 template <typename T, int DP> __device__ inline float product_with_row(const Frag<T, DP>& f, const Attn& p, const T* row, int h) {
   using L = Lds<T, DP>;
@@ -70,8 +82,15 @@ __global__ void __launch_bounds__(NT, DP <= 64 ? 2 : 1) attention_dq_kernel(Attn
   const float lse2 = lse2_of(p, b, i, head, r);
   float delta = product_with_row<T, DP>(dof, p, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr, h);
   delta += other_half(delta);
-  if (split == 0 && h == 0 && r < p.R) { stat[r] = lse2; stat[p.R + r] = delta; }
+  if (lse2 == INFINITY) delta = 0.0f;
+  if (split == 0 && h == 0 && r < p.R) {
+    stat[r] = lse2;
+    stat[p.R + r] = delta;
+    mark_unseeing(p, lse2, b, i);
+  }
   load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
+  clear_unseeing<T, DP>(dof, lse2);
+  clear_unseeing<T, DP>(qf, lse2);
   const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
@@ -170,6 +189,8 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
   const bool exact = all1 - all0 <= 8;
   if (!exact) delta = product_with_row<T, DP>(dof, p, any ? (const T*)p.o + b * p.os[0] + i * p.os[1] + head * p.os[2] : nullptr, h);
   load_row<T, DP>(qf, p.direct, p.dim, h, any ? (const T*)p.q + b * p.qs[0] + i * p.qs[1] + head * p.qs[2] : nullptr);
+  clear_unseeing<T, DP>(dof, lse2);
+  clear_unseeing<T, DP>(qf, lse2);
   const T* kbase = (const T*)p.k + b * p.ks[0] + kh * p.ks[2];
   const T* vbase = (const T*)p.v + b * p.vs[0] + kh * p.vs[2];
   const int* kdoc = p.kdoc ? p.kdoc + (long long)b * p.m : nullptr;
@@ -312,7 +333,12 @@ __global__ void __launch_bounds__(NT, 2) attention_dq_bf16_kernel(Attn p, float*
     __syncthreads();   // the tiles are filled again
   }
   delta += other_half(delta);
-  if (split == 0 && h == 0 && r < p.R) { stat[r] = lse2; stat[p.R + r] = delta; }
+  if (lse2 == INFINITY) delta = 0.0f;
+  if (split == 0 && h == 0 && r < p.R) {
+    stat[r] = lse2;
+    stat[p.R + r] = delta;
+    mark_unseeing(p, lse2, b, i);
+  }
   walk(std::false_type{}, t0, t1);
   const int re = tile * 128 + wave * 32 + (here(lane) & 31), ie = re / p.G;   // (again, rather than kept)
   if (re >= p.R) return;
@@ -369,6 +395,11 @@ __device__ inline void row_range(const Attn& p, int b, int tile, int keys, int m
   const int first_tile = i0 * p.G / RT, end_tile = i0 < i1 ? (i1 * p.G + RT - 1) / RT : first_tile;
   t0 = __builtin_amdgcn_readfirstlane(first_tile);
   t1 = __builtin_amdgcn_readfirstlane(end_tile);
+}
+
+// Rows from the first one on that see nothing, of those without documents
+__device__ inline int unseeing_rows(const Attn& p, int b, int keys) {
+  return __builtin_amdgcn_readfirstlane(p.causal && !(p.prefix && min(p.prefix[b], keys) > 0) ? max(p.n - keys, 0) * p.G : 0);
 }
 
 // Key tile, part (of how many) and pair of a workgroup; the key tiles with the most rows come first
@@ -428,6 +459,7 @@ __global__ void __launch_bounds__(NT, DP <= 32 ? 2 : 1) attention_dkv_kernel(Att
   const T* qbase = (const T*)p.q + b * p.qs[0] + kh * p.G * p.qs[2];
   const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
   const float* st = stat + (long long)pair * 2 * p.R;
+  const int unseeing = unseeing_rows(p, b, keys);
   Chunks<T, DP, RT, true> qat, doat;
   if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
   if (p.whole) {
@@ -435,7 +467,7 @@ __global__ void __launch_bounds__(NT, DP <= 32 ? 2 : 1) attention_dkv_kernel(Att
     doat.set(tid, p.G, p.dos[1], p.dos[2], p.dim);
   }
   auto issue = [&](int t, int buf) {
-    if (p.whole && !kdoc && (t + 1) * RT <= p.R) {
+    if (p.whole && !kdoc && (t + 1) * RT <= p.R && t * RT >= unseeing) {
       const long long token = (long long)t * RT / p.G;
       qat.load(smem + buf * TB, (const char*)(qbase + token * p.qs[1]), wave);
       doat.load(smem + (2 + buf) * TB, (const char*)(dobase + token * p.dos[1]), wave);
@@ -569,6 +601,7 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   const T* qbase = (const T*)p.q + b * p.qs[0] + kh * p.G * p.qs[2];
   const T* dobase = (const T*)p.dout + b * p.dos[0] + kh * p.G * p.dos[2];
   const float* st = stat + (long long)pair * 2 * p.R;
+  const int unseeing = unseeing_rows(p, b, keys);
   // Where the group divides 32, a tile's rows lie alike in every tile
   Chunks<T, DP, RT, true> qat, doat;
   if (p.dim < DP) zero_tiles<4 * TB>(smem, tid);
@@ -586,14 +619,15 @@ __global__ void __launch_bounds__(NT, 2) attention_dkv_bf16_kernel(Attn p, const
   auto issue = [&](int t, int buf) __attribute__((always_inline)) {
     int4 dx = make_int4(0, 0, 0, 0), dy = dx;
     if (p.qdoc) docs_of(t, dx, dy);
-    if (p.whole && !dx.z && !dy.z && (t + 1) * RT <= p.R) {
+    const bool hidden = p.qdoc ? dx.z || dy.z : t * RT < unseeing;
+    if (p.whole && !hidden && (t + 1) * RT <= p.R) {
       const long long token = (long long)t * RT / p.G;
       qat.load(smem + buf * TB, (const char*)(qbase + token * p.qs[1]), wave);
       doat.load(smem + (2 + buf) * TB, (const char*)(dobase + token * p.dos[1]), wave);
     } else {
       auto at = [&](int x, const T* base, const long long (&s)[3]) -> const T* {
         const int r = t * RT + x, i = r / p.G, g = r - i * p.G;
-        return r < p.R && !(p.qdoc && p.qdoc[(long long)b * p.n + i] < 0) ? base + i * s[1] + g * s[2] : nullptr;
+        return r < p.R && !(hidden && st[r] == INFINITY) ? base + i * s[1] + g * s[2] : nullptr;
       };
       load_tile<T, DP, RT>(smem + buf * TB, p.direct, p.dim, tid, [&](int x) { return at(x, qbase, p.qs); });
       load_tile<T, DP, RT>(smem + (2 + buf) * TB, p.direct, p.dim, tid, [&](int x) { return at(x, dobase, p.dos); });

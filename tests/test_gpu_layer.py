@@ -562,3 +562,39 @@ def test_attention_caps_far_above_the_scores(prism, dtype, bias, n, m, d, softca
             total["lim_" + x] = total["lim_" + x] + lim
     _close(grads[1][0, :, 0], total["dk"], u * np.abs(total["dk"]) + total["lim_dk"] + 1e-30, "dk")
     _close(grads[2][0, :, 0], total["dv"], u * np.abs(total["dv"]) + total["lim_dv"] + 1e-30, "dv")
+
+
+def _queries_that_see_nothing(why, n, m):
+    """(mask arguments of three sequences, which queries see no key)."""
+    if why == "lengths":          # queries before the first key
+        lens = [m, n // 3, 0]
+        return dict(causal=True, k_lens=torch.tensor(lens, dtype=torch.int32).cuda()), [R.visible(n, m, True, keys=x)[0].any(1) for x in lens]
+    q = [[0] * (n // 2) + [5] * (n - n // 2), [7] * n, (_docs([n // 4] * 4) + [1] * n)[:n]]      # documents that have no key
+    k = [[0] * m, [2] * m, ([0] * (m // 2) + [3] * m)[:m]]
+    arr = lambda x: torch.tensor(x, dtype=torch.int32).cuda()   # noqa: E731
+    return dict(q_doc=arr(q), k_doc=arr(k)), [R.visible(n, m, q_doc=q[i], k_doc=k[i])[0].any(1) for i in range(3)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("why", ["lengths", "documents"])
+@pytest.mark.parametrize("softcap,bias", [(0.0, False), (20.0, True)])
+@pytest.mark.parametrize("n,m,hq,d", [(200, 200, 4, 64), (300, 300, 2, 128), (130, 1100, 6, 64), (9, 90, 2, 80), (40, 40, 32, 128)])
+def test_attention_queries_that_see_nothing_may_hold_anything(prism, dtype, why, softcap, bias, n, m, hq, d):
+    """The same bits, gradients too, whatever is in queries without a key and in their dout."""
+    g = torch.Generator().manual_seed(23)
+    mask, some = _queries_that_see_nothing(why, n, m)
+    q, k, v, do = (_heads(g, 3, x, h, d, dtype, 1.0, "plain") for x, h in ((n, hq), (m, 2), (m, 2), (n, hq)))
+    opt = dict(softcap=softcap, slopes=torch.tensor(_slopes(hq), device="cuda") if bias else None, **mask)
+    none = torch.from_numpy(~np.stack(some)).cuda()
+    assert bool(none.any()) and not bool(none.all())
+    results = []
+    for x in (0.0, float("nan"), float("inf")):
+        a, b = q.clone(), do.clone()
+        a[none], b[none] = x, x
+        out, lse = prism.attention(a, k, v, **opt)
+        results.append((out, lse) + prism.attention_backward(b, a, k, v, out, lse, **opt))
+    assert torch.all(results[0][0][none] == 0) and torch.all(results[0][2][none] == 0)
+    assert torch.all(torch.isneginf(results[0][1].transpose(1, 2)) == none[:, :, None])
+    for r in results[1:]:
+        for x, y, what in zip(results[0], r, ("out", "lse", "dq", "dk", "dv")):
+            assert torch.equal(x, y), what
