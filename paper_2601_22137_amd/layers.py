@@ -18,8 +18,8 @@ class _NormRope(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight = ctx.saved_tensors
-        # the gradient of a result that nothing reads is None
-        dq_out, dk_out = (torch.zeros_like(t) if g is None else _rows(g) for g, t in ((dq_out, q), (dk_out, k)))
+        # the gradient of a result that nothing reads is None, and so is that of one that there is not
+        dq_out, dk_out = (_rows(g) if g is not None else None if t is None else torch.zeros_like(t) for g, t in ((dq_out, q), (dk_out, k)))
         dq, dk, dqw, dkw = prism.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight=q_weight, k_weight=k_weight, **ctx.options)
         return dq, dk, dqw if q_weight is not None else None, dkw if k_weight is not None else None, None
 
@@ -56,7 +56,7 @@ def _rows(t):
 
 
 def norm_rope(q, k, q_weight=None, k_weight=None, **options):
-    """prism.qk_norm_rope of queries and keys with gradients for them and the weights; options: inv_freq, positions, start, norm, interleaved, scale, eps."""
+    """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights; options: inv_freq, positions, start, norm, interleaved, scale, eps."""
     return _NormRope.apply(q, k, q_weight, k_weight, options)
 
 

@@ -112,3 +112,18 @@ def test_example_learns(layers):
     assert np.all(np.isfinite(losses)) and np.mean(losses[-5:]) < 0.8 * losses[0]
     prompts = torch.randint(0, M.VOCABULARY, (3, 12), device="cuda")
     assert M.generate(model, prompts, 4).shape == (3, 16)
+
+
+def test_norm_rope_of_queries_or_keys_alone(layers):
+    q, k = (torch.randn(2, 9, h, 64, device="cuda", requires_grad=True) for h in (4, 2))
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    f = torch.rand(16, device="cuda")
+    g = [torch.randn_like(t) for t in (q, k)]
+    torch.autograd.backward(layers.norm_rope(q, k, w, w, inv_freq=f), g)
+    both = [t.grad for t in (q, k, w)]
+    q.grad = k.grad = w.grad = None
+    layers.norm_rope(q, None, w, inv_freq=f)[0].backward(g[0])
+    layers.norm_rope(None, k, None, w, inv_freq=f)[1].backward(g[1])
+    assert torch.equal(q.grad, both[0]) and torch.equal(k.grad, both[1])
+    # sums of 108 terms in fp32, of a gradient turned (1.5 of its largest entry) times an entry of a normed head (8 at most)
+    assert torch.allclose(w.grad, both[2], rtol=0, atol=2.0 ** -23 * 108 * 1.5 * 8 * max(float(x.abs().max()) for x in g))

@@ -1,0 +1,43 @@
+"""What layers.py does around the library's calls, with stand-ins for them that need no GPU: only how gradients, masks and caches are handed on is tested here."""
+import pytest
+import torch
+
+from paper_2601_22137_amd import layers, prism
+
+
+@pytest.fixture(autouse=True)
+def stand_ins(monkeypatch):
+    """Calls of the right shapes; results keep a trace of what they were made from."""
+    def qk_norm_rope(q, k, **kw):
+        return tuple(None if t is None else 2 * t for t in (q, k))
+
+    def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight=None, k_weight=None, **kw):
+        assert (dq_out is None) == (q is None) and (dk_out is None) == (k is None)
+        return tuple(None if t is None else 2 * t for t in (dq_out, dk_out)) + tuple(None if t is None else t.sum((0, 1, 2)) for t in (q, k))
+
+    def attention(q, k, v, **kw):
+        return q + v.mean(), torch.zeros(q.shape[0], q.shape[2], q.shape[1])
+
+    def attention_backward(dout, q, k, v, out, lse, **kw):
+        return dout.clone(), torch.zeros_like(k), torch.full_like(v, float(dout.sum()) / v.numel())
+
+    def dropout(x, p, seed, offset=0, residual=None, out=None):
+        y = x * float((seed + offset) % 7 + 1)
+        return y if residual is None else y + residual
+    for f in (qk_norm_rope, qk_norm_rope_backward, attention, attention_backward, dropout):
+        monkeypatch.setattr(prism, f.__name__, f)
+
+
+def _heads(*shape):
+    return torch.randn(*shape, requires_grad=True)
+
+
+def test_norm_rope_of_queries_or_keys_alone():
+    q, w = _heads(1, 3, 2, 8), torch.ones(8, requires_grad=True)
+    a, none = layers.norm_rope(q, None, w)
+    a.sum().backward()
+    assert none is None and torch.all(q.grad == 2) and w.grad.shape == (8,)
+    k = _heads(1, 3, 2, 8)
+    none, b = layers.norm_rope(None, k)
+    b.sum().backward()
+    assert none is None and torch.all(k.grad == 2)
