@@ -467,8 +467,7 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, inv_freq=None, positions=None, s
     q and k are the inputs of the forward call.  out: tensors for dq and dk."""
     dq, dk = (_new(q), _new(k)) if out is None else out
     some, dev, desc = _norm_rope_desc(q, k, (dq_out, dk_out), (dq, dk), inv_freq, positions, start, q_weight, k_weight, norm, interleaved, scale, eps, workspace)
-    dqw, dkw = [t.new_zeros(t.shape[3], dtype=torch.float32) if t.numel() == 0 else t.new_empty(t.shape[3], dtype=torch.float32)
-                if norm and t is not None else None for t in (q, k)]
+    dqw, dkw = [None if t is None or not norm else (t.new_empty if t.numel() else t.new_zeros)(t.shape[3], dtype=torch.float32) for t in (q, k)]
     _on(dev, lib().prism_qk_norm_rope_backward, _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(dq), _ptr(dk), _ptr(dqw), _ptr(dkw), _dtype_code(some), desc)
     return dq, dk, dqw, dkw
 

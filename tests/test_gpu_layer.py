@@ -598,3 +598,17 @@ def test_attention_queries_that_see_nothing_may_hold_anything(prism, dtype, why,
     for r in results[1:]:
         for x, y, what in zip(results[0], r, ("out", "lse", "dq", "dk", "dv")):
             assert torch.equal(x, y), what
+
+
+@pytest.mark.parametrize("norm", [True, False])
+def test_norm_rope_gradients_of_one_of_two(prism, norm):
+    q, k, gq, gk, pos, w, f = _norm_rope_case(F32, 2, 19, 4, 2, 64, 32, 1, "plain")
+    args = dict(inv_freq=f.cuda(), positions=pos.cuda(), norm=norm)
+    w = w if norm else (None, None)
+    both = prism.qk_norm_rope_backward(gq, gk, q, k, q_weight=w[0], k_weight=w[1], **args)
+    dq, dk, dqw, dkw = prism.qk_norm_rope_backward(gq, None, q, None, q_weight=w[0], **args)
+    assert torch.equal(dq, both[0]) and dk is None and dkw is None and (torch.equal(dqw, both[2]) if norm else dqw is None)
+    dq, dk, dqw, dkw = prism.qk_norm_rope_backward(None, gk, None, k, k_weight=w[1], **args)
+    assert torch.equal(dk, both[1]) and dq is None and dqw is None and (torch.equal(dkw, both[3]) if norm else dkw is None)
+    e = torch.empty(0, 4, 2, 64, device="cuda")
+    assert (prism.qk_norm_rope_backward(e, None, e, None, norm=norm)[2] is None) == (not norm)
