@@ -1,9 +1,10 @@
 """The layer operators for autograd, and the attention half of a transformer layer made of them: the part of a model whose 2-D weights
 optim.muon_orthogonalize updates.
 
-Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.
+Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.  Second derivatives of attention and of norm and rotation are an error.
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import prism
 
@@ -16,6 +17,7 @@ class _NormRope(torch.autograd.Function):
         return prism.qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, **options)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight = ctx.saved_tensors
         # the gradient of a result that nothing reads is None, and so is that of one that there is not
@@ -33,6 +35,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         return prism.attention_backward(_rows(dout), *ctx.saved_tensors, **ctx.options) + (None,)
 
@@ -45,8 +48,8 @@ class _Dropout(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        p, seed, offset = ctx.args
-        dx = prism.dropout(dy.contiguous(), p, seed, offset=offset) if ctx.needs_input_grad[0] else None
+        # the same call, so that derivatives of the gradient are right too
+        dx = _Dropout.apply(dy.contiguous(), None, *ctx.args) if ctx.needs_input_grad[0] else None
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
 
 

@@ -127,3 +127,18 @@ def test_norm_rope_of_queries_or_keys_alone(layers):
     assert torch.equal(q.grad, both[0]) and torch.equal(k.grad, both[1])
     # sums of 108 terms in fp32, of a gradient turned (1.5 of its largest entry) times an entry of a normed head (8 at most)
     assert torch.allclose(w.grad, both[2], rtol=0, atol=2.0 ** -23 * 108 * 1.5 * 8 * max(float(x.abs().max()) for x in g))
+
+
+def test_second_derivatives(layers):
+    """Those of dropout are right, those of the others an error."""
+    x, r = (torch.randn(1000, device="cuda", requires_grad=True) for _ in range(2))
+    y = layers.dropout(x, 0.25, 11, 3, residual=r)
+    (gx,) = torch.autograd.grad((y ** 2).sum(), x, create_graph=True)
+    gx.sum().backward()
+    kept = (layers.dropout(torch.ones_like(x), 0.25, 11, 3) != 0).float() * (65536 / 49152)
+    assert torch.allclose(x.grad, 2 * kept * kept) and torch.allclose(r.grad, 2 * kept)
+    q = torch.randn(1, 5, 2, 32, device="cuda", requires_grad=True)
+    for call in (lambda: layers.attention(q, q, q), lambda: layers.norm_rope(q, q)[0]):
+        (g,) = torch.autograd.grad((call() ** 2).sum(), q, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.sum().backward()

@@ -25,7 +25,7 @@ def stand_ins(monkeypatch):
         y = x * float((seed + offset) % 7 + 1)
         return y if residual is None else y + residual
     for f in (qk_norm_rope, qk_norm_rope_backward, attention, attention_backward, dropout):
-        monkeypatch.setattr(prism, f.__name__, f)
+        monkeypatch.setattr(prism, f.__name__, torch.no_grad()(f))       # like the library, which autograd does not see into
 
 
 def _heads(*shape):
@@ -41,3 +41,21 @@ def test_norm_rope_of_queries_or_keys_alone():
     none, b = layers.norm_rope(None, k)
     b.sum().backward()
     assert none is None and torch.all(k.grad == 2)
+
+
+@pytest.mark.parametrize("call", [lambda q, k: layers.norm_rope(q, k)[0], lambda q, k: layers.attention(q, k, k)])
+def test_second_derivatives_are_refused(call):
+    """They are not computed; without an error a penalty on a gradient would quietly lose its part through these calls."""
+    q, k = _heads(1, 3, 2, 8), _heads(1, 3, 2, 8)
+    (g,) = torch.autograd.grad((call(q, k) ** 2).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (g ** 2).sum().backward()
+
+
+def test_second_derivatives_of_dropout():
+    x, r = _heads(5), _heads(5)
+    y = layers.dropout(x, 0.5, 2, residual=r)        # the stand-in: 3 x + r
+    gx, gr = torch.autograd.grad((y ** 3).sum(), (x, r), create_graph=True)
+    (gx.sum() + gr.sum()).backward()
+    z = (3 * x + r).detach()
+    assert torch.allclose(x.grad, 3 * (3 + 1) * 6 * z) and torch.allclose(r.grad, (3 + 1) * 6 * z)
