@@ -58,14 +58,15 @@ def _rows(t):
     return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
 
 
-def norm_rope(q, k, q_weight=None, k_weight=None, **options):
-    """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights; options: inv_freq, positions, start, norm, interleaved, scale, eps."""
-    return _NormRope.apply(q, k, q_weight, k_weight, options)
+def norm_rope(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, start=0, norm=True, interleaved=False, scale=1.0, eps=1e-6):
+    """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights."""
+    return _NormRope.apply(q, k, q_weight, k_weight, dict(inv_freq=inv_freq, positions=positions, start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps))
 
 
-def attention(q, k, v, **options):
-    """prism.attention with gradients for q, k and v; options: scale, causal, softcap, slopes, prefix, k_lens, q_doc, k_doc."""
-    return _Attention.apply(q, k, v, options)
+def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, workspace=None):
+    """prism.attention with gradients for q, k and v.  A workspace has to be enough for the gradients too."""
+    return _Attention.apply(q, k, v, dict(scale=scale, causal=causal, softcap=softcap, slopes=slopes, prefix=prefix, k_lens=k_lens, q_doc=q_doc, k_doc=k_doc,
+                                          workspace=workspace))
 
 
 def dropout(x, p, seed, offset=0, residual=None):

@@ -59,3 +59,14 @@ def test_second_derivatives_of_dropout():
     (gx.sum() + gr.sum()).backward()
     z = (3 * x + r).detach()
     assert torch.allclose(x.grad, 3 * (3 + 1) * 6 * z) and torch.allclose(r.grad, (3 + 1) * 6 * z)
+
+
+def test_results_have_no_given_place():
+    """The backward pass would write its own results there."""
+    q, k = _heads(1, 3, 2, 8), _heads(1, 3, 2, 8)
+    with pytest.raises(TypeError, match="out"):
+        layers.norm_rope(q, k, out=(torch.empty(1, 3, 2, 8), torch.empty(1, 3, 2, 8)))
+    with pytest.raises(TypeError, match="out"):
+        layers.attention(q, k, k, out=torch.empty(1, 3, 2, 8))
+    with pytest.raises(TypeError):
+        layers.attention(q, k, k, soft_cap=1.0)
