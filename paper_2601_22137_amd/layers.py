@@ -9,35 +9,39 @@ from torch.autograd.function import once_differentiable
 from . import prism
 
 
+# Tensors of the masks and positions are arguments of their own: written to between the passes, they are an error as other saved tensors are.
+
 class _NormRope(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, q_weight, k_weight, options):
-        ctx.save_for_backward(q, k, q_weight, k_weight)
+    def forward(ctx, q, k, q_weight, k_weight, inv_freq, positions, options):
+        ctx.save_for_backward(q, k, q_weight, k_weight, inv_freq, positions)
         ctx.options = options
-        return prism.qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, **options)
+        return prism.qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, positions=positions, **options)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dq_out, dk_out):
-        q, k, q_weight, k_weight = ctx.saved_tensors
+        q, k, q_weight, k_weight, inv_freq, positions = ctx.saved_tensors
         # the gradient of a result that nothing reads is None, and so is that of one that there is not
         dq_out, dk_out = (_rows(g) if g is not None else None if t is None else torch.zeros_like(t) for g, t in ((dq_out, q), (dk_out, k)))
-        dq, dk, dqw, dkw = prism.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight=q_weight, k_weight=k_weight, **ctx.options)
-        return dq, dk, dqw if q_weight is not None else None, dkw if k_weight is not None else None, None
+        dq, dk, dqw, dkw = prism.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, positions=positions, **ctx.options)
+        return dq, dk, dqw if q_weight is not None else None, dkw if k_weight is not None else None, None, None, None
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, options):
-        out, lse = prism.attention(q, k, v, **options)
-        ctx.save_for_backward(q, k, v, out, lse)
+    def forward(ctx, q, k, v, slopes, prefix, k_lens, q_doc, k_doc, options):
+        masks = dict(slopes=slopes, prefix=prefix, k_lens=k_lens, q_doc=q_doc, k_doc=k_doc)
+        out, lse = prism.attention(q, k, v, **masks, **options)
+        ctx.save_for_backward(q, k, v, out, lse, *masks.values())
         ctx.options = options
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        return prism.attention_backward(_rows(dout), *ctx.saved_tensors, **ctx.options) + (None,)
+        q, k, v, out, lse, slopes, prefix, k_lens, q_doc, k_doc = ctx.saved_tensors
+        return prism.attention_backward(_rows(dout), q, k, v, out, lse, slopes=slopes, prefix=prefix, k_lens=k_lens, q_doc=q_doc, k_doc=k_doc, **ctx.options) + 6 * (None,)
 
 
 class _Dropout(torch.autograd.Function):
@@ -60,13 +64,12 @@ def _rows(t):
 
 def norm_rope(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, start=0, norm=True, interleaved=False, scale=1.0, eps=1e-6):
     """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights."""
-    return _NormRope.apply(q, k, q_weight, k_weight, dict(inv_freq=inv_freq, positions=positions, start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps))
+    return _NormRope.apply(q, k, q_weight, k_weight, inv_freq, positions, dict(start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps))
 
 
 def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, workspace=None):
     """prism.attention with gradients for q, k and v.  A workspace has to be enough for the gradients too."""
-    return _Attention.apply(q, k, v, dict(scale=scale, causal=causal, softcap=softcap, slopes=slopes, prefix=prefix, k_lens=k_lens, q_doc=q_doc, k_doc=k_doc,
-                                          workspace=workspace))
+    return _Attention.apply(q, k, v, slopes, prefix, k_lens, q_doc, k_doc, dict(scale=scale, causal=causal, softcap=softcap, workspace=workspace))
 
 
 def dropout(x, p, seed, offset=0, residual=None):

@@ -70,3 +70,32 @@ def test_results_have_no_given_place():
         layers.attention(q, k, k, out=torch.empty(1, 3, 2, 8))
     with pytest.raises(TypeError):
         layers.attention(q, k, k, soft_cap=1.0)
+
+
+@pytest.mark.parametrize("name", ["inv_freq", "positions", "q_weight"])
+def test_norm_rope_notices_what_was_written_before_backward(name):
+    q, k = _heads(1, 3, 2, 8), _heads(1, 3, 2, 8)
+    given = dict(inv_freq=torch.ones(4), positions=torch.zeros(1, 3, dtype=torch.int32), q_weight=torch.ones(8))
+    a, b = layers.norm_rope(q, k, **given)
+    given[name].add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (a.sum() + b.sum()).backward()
+
+
+@pytest.mark.parametrize("name", ["slopes", "prefix", "k_lens", "q_doc", "k_doc"])
+def test_attention_notices_what_was_written_before_backward(name):
+    q, k = _heads(2, 3, 2, 8), _heads(2, 3, 2, 8)
+    i32 = lambda *s: torch.ones(*s, dtype=torch.int32)   # noqa: E731
+    given = dict(slopes=torch.ones(2), prefix=i32(2), k_lens=i32(2), q_doc=i32(2, 3), k_doc=i32(2, 3))
+    y = layers.attention(q, k, k, causal=True, workspace=torch.empty(1), **given)
+    given[name].add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+def test_scratch_memory_is_no_input():
+    q, ws = _heads(1, 3, 2, 8), torch.zeros(4)
+    y = layers.attention(q, q, q, workspace=ws)
+    ws.add_(1)
+    y.sum().backward()
+    assert q.grad is not None
