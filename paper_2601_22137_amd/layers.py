@@ -62,13 +62,20 @@ def _rows(t):
     return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
 
 
+def _fixed(t, name):
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise prism.PrismError("%s: there is no gradient for it" % name)
+
+
 def norm_rope(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, start=0, norm=True, interleaved=False, scale=1.0, eps=1e-6):
     """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights."""
+    _fixed(inv_freq, "inv_freq")
     return _NormRope.apply(q, k, q_weight, k_weight, inv_freq, positions, dict(start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps))
 
 
 def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, workspace=None):
     """prism.attention with gradients for q, k and v.  A workspace has to be enough for the gradients too."""
+    _fixed(slopes, "slopes")
     return _Attention.apply(q, k, v, slopes, prefix, k_lens, q_doc, k_doc, dict(scale=scale, causal=causal, softcap=softcap, workspace=workspace))
 
 

@@ -99,3 +99,15 @@ def test_scratch_memory_is_no_input():
     ws.add_(1)
     y.sum().backward()
     assert q.grad is not None
+
+
+def test_learned_slopes_and_frequencies_are_refused():
+    q = _heads(1, 3, 2, 8)
+    learned = torch.ones(2, requires_grad=True)
+    with pytest.raises(prism.PrismError, match="slopes"):
+        layers.attention(q, q, q, slopes=learned)
+    with pytest.raises(prism.PrismError, match="inv_freq"):
+        layers.norm_rope(q, q, inv_freq=learned)
+    with torch.no_grad():
+        layers.attention(q, q, q, slopes=learned)
+        layers.norm_rope(q, q, inv_freq=learned)
