@@ -84,6 +84,34 @@ def dropout(x, p, seed, offset=0, residual=None):
     return _Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(), p, seed, offset)
 
 
+class Cache(tuple):
+    """(keys, values, lens): [batch, length, k_heads, dim] twice, and how many tokens there are of each sequence, int32 on the device.  How many the longest has is
+    also known on the host; it is read from the device only after lens was written to by others."""
+
+    def __new__(cls, keys, values, lens):
+        self = tuple.__new__(cls, (keys, values, lens))
+        self.longest, self.version = 0, None
+        return self
+
+    def _written(self):
+        """Changes with every write to lens (tensors of inference mode do not tell)."""
+        lens = self[2]
+        return 0 if lens.is_inference() else lens._version
+
+    def last_place(self):
+        """Index of the last token there is room for; an error, before anything is written, if it is taken."""
+        keys, _, lens = self
+        if self.version != self._written():
+            self.longest = int(lens.max()) if lens.numel() else 0
+        if self.longest >= keys.shape[1]:
+            raise prism.PrismError("the cache is full: it is made for %d tokens" % keys.shape[1])
+        return keys.shape[1] - 1
+
+    def took_one(self):
+        self.longest += 1
+        self.version = self._written()
+
+
 class SelfAttention(torch.nn.Module):
     """x + dropout(attention(x w_qkv) w_out): one projection for queries, keys and values, whose parts are used as views; norms of the heads of queries and
     keys, rotation by position, scores capped at will; queries in groups of heads / k_heads share a key head."""
@@ -117,16 +145,23 @@ class SelfAttention(torch.nn.Module):
     def new_cache(self, batch, length):
         """Keys and values of up to `length` tokens, and how many there are of each sequence."""
         make = lambda: torch.zeros(batch, length, self.k_heads, self.dim, dtype=self.w_qkv.dtype, device=self.w_qkv.device)   # noqa: E731
-        return make(), make(), torch.zeros(batch, dtype=torch.int32, device=self.w_qkv.device)
+        cache = Cache(make(), make(), torch.zeros(batch, dtype=torch.int32, device=self.w_qkv.device))
+        cache.version = cache._written()
+        return cache
 
     @torch.no_grad()
     def step(self, x, cache):
-        """One token of each sequence, x [batch, 1, width], behind the tokens in the cache, which takes it in."""
+        """One token of each sequence, x [batch, 1, width], behind the tokens in the cache, which takes it in.  (A step that is captured into a graph is counted once: how
+        often it is replayed is the caller's to count.  Tokens too many then replace the last one.)"""
+        if not isinstance(cache, Cache):
+            cache = Cache(*cache)
+        last = cache.last_place()
         keys, values, lens = cache
         b = x.shape[0]
         q, k, v = self._project(x, lens.view(b, 1))
-        at = torch.arange(b, device=x.device), lens.long()
+        at = torch.arange(b, device=x.device), lens.clamp(0, last).long()
         keys[at], values[at] = k[:, 0], v[:, 0]
         lens += 1
+        cache.took_one()
         out, _ = prism.attention(q, keys, values, softcap=self.softcap, k_lens=lens)
         return x + out.reshape(b, 1, -1) @ self.w_out.t()

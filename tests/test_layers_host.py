@@ -111,3 +111,42 @@ def test_learned_slopes_and_frequencies_are_refused():
     with torch.no_grad():
         layers.attention(q, q, q, slopes=learned)
         layers.norm_rope(q, q, inv_freq=learned)
+
+
+def _layer():
+    return layers.SelfAttention(16, 2, device="cpu", dtype=torch.float32)
+
+
+def test_a_full_cache_is_refused():
+    m, x = _layer(), torch.randn(3, 1, 16)
+    cache = m.new_cache(3, 4)
+    keys, values, lens = cache
+    for i in range(4):
+        assert lens.tolist() == [i] * 3
+        m.step(x, cache)
+    before = [t.clone() for t in cache]
+    with pytest.raises(prism.PrismError, match="4 tokens"):
+        m.step(x, cache)
+    assert all(torch.equal(a, b) for a, b in zip(before, cache))
+    lens.fill_(0)                         # emptied, or filled by hand
+    m.step(x, cache)
+    lens.copy_(torch.tensor([0, 4, 1]))
+    with pytest.raises(prism.PrismError, match="4 tokens"):
+        m.step(x, cache)
+    with pytest.raises(prism.PrismError, match="4 tokens"):
+        m.step(x, (keys, values, lens))   # a plain tuple of the three
+    lens.copy_(torch.tensor([0, 3, 1]))
+    m.step(x, (keys, values, lens))
+    assert lens.tolist() == [1, 4, 2]
+
+
+def test_a_cache_under_inference_mode():
+    with torch.inference_mode():
+        m, x = _layer(), torch.randn(3, 1, 16)
+        cache = m.new_cache(3, 2)
+        m.step(x, cache)
+        m.step(x, cache)
+        with pytest.raises(prism.PrismError, match="2 tokens"):
+            m.step(x, cache)
+        with pytest.raises(prism.PrismError, match="2 tokens"):
+            m.step(x, tuple(cache))
