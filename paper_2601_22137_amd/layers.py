@@ -135,12 +135,16 @@ class SelfAttention(torch.nn.Module):
         q, k = norm_rope(q, k, self.q_weight, self.k_weight, inv_freq=self.inv_freq, positions=positions, scale=self.rope_scale)
         return q, k, v
 
-    def forward(self, x, positions=None, doc=None, seed=0, offset=0):
-        """x [batch, token, width]; positions and documents int32 [batch, token] (a negative document is padding)."""
+    def forward(self, x, positions=None, doc=None, seed=None, offset=None):
+        """x [batch, token, width]; positions and documents int32 [batch, token] (a negative document is padding).  Seed and offset name the mask of the dropout; without
+        either, one is drawn from PyTorch's generator of the host."""
         b, n, _ = x.shape
         q, k, v = self._project(x, positions)
         y = attention(q, k, v, causal=True, softcap=self.softcap, q_doc=doc, k_doc=doc).reshape(b, n, -1) @ self.w_out.t()
-        return dropout(y, self.p if self.training else 0.0, seed, offset, residual=x)
+        p = self.p if self.training else 0.0
+        if p > 0.0 and seed is None and offset is None:
+            seed = int(torch.randint(2 ** 63 - 1, ()))
+        return dropout(y, p, seed or 0, offset or 0, residual=x)
 
     def new_cache(self, batch, length):
         """Keys and values of up to `length` tokens, and how many there are of each sequence."""

@@ -150,3 +150,33 @@ def test_a_cache_under_inference_mode():
             m.step(x, cache)
         with pytest.raises(prism.PrismError, match="2 tokens"):
             m.step(x, tuple(cache))
+
+
+def test_masks_of_dropout_differ_unless_asked_for(monkeypatch):
+    """In training every layer and step has a mask of its own; a seed or an offset names one; PyTorch's generator repeats them."""
+    seen = []
+
+    @torch.no_grad()
+    def dropout(x, p, seed, offset=0, residual=None, out=None):
+        seen.append((p, seed, offset))
+        return x + residual
+    monkeypatch.setattr(prism, "dropout", dropout)
+    x = torch.randn(1, 3, 16)
+    two = [layers.SelfAttention(16, 2, p=0.5, device="cpu", dtype=torch.float32) for _ in range(2)]
+
+    def run(*args, **kw):
+        del seen[:]
+        for _ in range(3):
+            for m in two:
+                m(x, *args, **kw)
+        return list(seen)
+    torch.manual_seed(5)
+    first = run()
+    assert len({s for _, s, _ in first}) == 6 and all(0 <= s < 2 ** 63 and o == 0 and p == 0.5 for p, s, o in first)
+    torch.manual_seed(5)
+    assert run() == first
+    assert set(run(seed=7, offset=3)) == {(0.5, 7, 3)} and set(run(seed=7)) == {(0.5, 7, 0)} and set(run(offset=3)) == {(0.5, 0, 3)} and set(run(seed=0)) == {(0.5, 0, 0)}
+    state = torch.get_rng_state()
+    for m in two:
+        m.eval()
+    assert {p for p, _, _ in run()} == {0.0} and torch.equal(state, torch.get_rng_state())
