@@ -143,7 +143,7 @@ class SelfAttention(torch.nn.Module):
         y = attention(q, k, v, causal=True, softcap=self.softcap, q_doc=doc, k_doc=doc).reshape(b, n, -1) @ self.w_out.t()
         p = self.p if self.training else 0.0
         if p > 0.0 and seed is None and offset is None:
-            seed = int(torch.randint(2 ** 63 - 1, ()))
+            seed = int(torch.randint(2 ** 63 - 1, (), device="cpu"))
         return dropout(y, p, seed or 0, offset or 0, residual=x)
 
     def new_cache(self, batch, length):

@@ -180,3 +180,9 @@ def test_masks_of_dropout_differ_unless_asked_for(monkeypatch):
     for m in two:
         m.eval()
     assert {p for p, _, _ in run()} == {0.0} and torch.equal(state, torch.get_rng_state())
+
+
+def test_drawn_seeds_are_of_the_host():
+    m, x = layers.SelfAttention(16, 2, p=0.5, device="cpu", dtype=torch.float32), torch.randn(1, 3, 16)
+    with torch.device("meta"):            # as a program does whose default device is the GPU
+        m(x)
