@@ -114,7 +114,7 @@ class Cache(tuple):
 
 class SelfAttention(torch.nn.Module):
     """x + dropout(attention(x w_qkv) w_out): one projection for queries, keys and values, whose parts are used as views; norms of the heads of queries and
-    keys, rotation by position, scores capped at will; queries in groups of heads / k_heads share a key head."""
+    keys, rotation by position (of their first rot_dim entries; None: all), scores capped at will; queries in groups of heads / k_heads share a key head."""
 
     def __init__(self, width, heads, k_heads=None, head_dim=None, rot_dim=None, softcap=0.0, p=0.0, base=10000.0, dtype=torch.bfloat16, device="cuda"):
         super().__init__()
@@ -125,7 +125,8 @@ class SelfAttention(torch.nn.Module):
         self.w_out = torch.nn.Parameter(torch.randn(width, self.heads * self.dim, dtype=dtype, device=device) * (self.heads * self.dim) ** -0.5)
         self.q_weight = torch.nn.Parameter(torch.ones(self.dim, device=device))
         self.k_weight = torch.nn.Parameter(torch.ones(self.dim, device=device))
-        inv_freq, self.rope_scale = prism.rope_frequencies(rot_dim or self.dim, base=base, device=device)
+        rot_dim = self.dim if rot_dim is None else rot_dim
+        inv_freq, self.rope_scale = prism.rope_frequencies(rot_dim, base=base, device=device) if rot_dim else (None, 1.0)
         self.register_buffer("inv_freq", inv_freq, persistent=False)
 
     def _project(self, x, positions):

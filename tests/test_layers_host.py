@@ -186,3 +186,13 @@ def test_drawn_seeds_are_of_the_host():
     m, x = layers.SelfAttention(16, 2, p=0.5, device="cpu", dtype=torch.float32), torch.randn(1, 3, 16)
     with torch.device("meta"):            # as a program does whose default device is the GPU
         m(x)
+
+
+def test_no_part_of_a_head_turns(monkeypatch):
+    seen = []
+    plain = prism.qk_norm_rope
+    monkeypatch.setattr(prism, "qk_norm_rope", lambda q, k, **kw: (seen.append(kw["inv_freq"]), plain(q, k, **kw))[1])
+    for rot, frequencies in ((0, 0), (4, 2), (None, 4)):
+        m = layers.SelfAttention(16, 2, rot_dim=rot, device="cpu", dtype=torch.float32)
+        m(torch.randn(1, 3, 16))
+        assert (0 if seen[-1] is None else seen[-1].numel()) == frequencies
