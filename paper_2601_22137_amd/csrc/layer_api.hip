@@ -8,6 +8,7 @@ namespace prism {
 namespace {
 
 constexpr long long MAX_ROWS = (1ll << 31) - 1;
+constexpr long long MAX_GROUPS = (1ll << 24) - 1;   // workgroups of 256 in a launch, which takes fewer than 2^32 work-items
 
 int refuse(const char* why, int rc = PRISM_EINVAL) {
   set_last_error(why);
@@ -67,9 +68,10 @@ int check(const prism_attention_desc* d, int dt) {
   if (d->head_dim > PRISM_MAX_ATTENTION_HEAD) return refuse("head_dim is over PRISM_MAX_ATTENTION_HEAD", PRISM_EUNSUPPORTED);
   if (!d->k_heads || !d->batch) return PRISM_OK;
   const long long G = d->q_heads / d->k_heads, R = G * d->q_len, pairs = (long long)d->batch * d->k_heads;
-  if (R > MAX_ROWS - 256 || d->k_len > MAX_ROWS - 256 || pairs * ((R + 127) / 128) > MAX_ROWS / 64 || pairs * (((long long)d->k_len + 127) / 128) > MAX_ROWS / 64 ||
-      pairs * R > MAX_ROWS / 4 || pairs * d->k_len > MAX_ROWS / 4)
+  if (R > MAX_ROWS - 256 || d->k_len > MAX_ROWS - 256 || pairs * R > MAX_ROWS / 4 || pairs * d->k_len > MAX_ROWS / 4)
     return refuse("the rows of a call and the keys of a call (their heads counted) may be 2^29 at most", PRISM_EUNSUPPORTED);
+  if (pairs * ((R + 127) / 128) > MAX_GROUPS || pairs * (((long long)d->k_len + 127) / 128) > MAX_GROUPS)
+    return refuse("more than 2^24 - 1 tiles of 128 rows or keys in a call", PRISM_EUNSUPPORTED);
   return PRISM_OK;
 }
 // no result at all (keys without queries have gradients: zero)

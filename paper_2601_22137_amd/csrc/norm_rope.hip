@@ -353,6 +353,10 @@ int launch_norm_rope(const void* q, const void* k, void* qo, void* ko, int dt, c
           (!d.k_heads || (whole_vectors(k, d.k, size) && whole_vectors(ko, d.k_out, size)));
   const int HS = vec ? heads_per_lane(d, L, 4) : 1;
   set_items(p, d, HS);
+  if (((unsigned long long)p.items[0] + p.items[1]) * L > 0xFFFFFF00ull) {
+    set_last_error("a launch takes fewer than 2^32 work-items, one for 16 entries of a head");
+    return PRISM_EUNSUPPORTED;
+  }
   by_type(p, dt, vec, L, HS, 0, false, s);
   return PRISM_OK;
 }

@@ -132,3 +132,16 @@ def test_attention_refuses_factors_that_leave_fp32(prism, kw):
     assert b"softcap" in prism.lib().prism_last_error()
     for kw in (dict(scale=1e37), dict(scale=1e-40), dict(softcap=1e37), dict(softcap=1e-30)):
         assert _bytes(prism, _attention(prism, **kw), 0)[0] == prism.OK
+
+
+def test_grids_that_no_launch_takes_are_refused_by_the_check(prism):
+    """A launch takes fewer than 2^32 work-items."""
+    most = dict(batch=(1 << 23) - 1, q_len=1, k_len=16, q_heads=2, k_heads=2)
+    for back in (0, 1):
+        assert _bytes(prism, _attention(prism, **most), back)[0] == prism.OK
+        assert _bytes(prism, _attention(prism, **dict(most, batch=1 << 23)), back)[0] == prism.EUNSUPPORTED
+    o = prism.NormRopeDesc()
+    o.batch, o.len, o.q_heads, o.head_dim, o.scale = 1 << 20, 1, 1030, 40, 1.0
+    o.q.batch, o.q.token, o.q.head = 1030 * 41, 1030 * 41, 41               # (rows of no whole vectors: a work-item for 16 entries)
+    o.q_out = o.q
+    assert prism.lib().prism_qk_norm_rope(ADDRESS, None, ADDRESS, None, prism.BF16, ctypes.byref(o), None) == prism.EUNSUPPORTED
