@@ -44,6 +44,7 @@ int check(const prism_norm_rope_desc* d, int dt) {
   if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 2) return refuse("rot_dim has to be even and at most head_dim");
   if (d->rot_dim > 0 && !d->inv_freq) return refuse("rot_dim without inv_freq");
   if (!std::isfinite(d->scale) || (d->norm && !(d->eps >= 0.0f && std::isfinite(d->eps)))) return refuse("scale or eps is not finite, or eps negative");
+  if (!d->positions && (long long)d->start + d->len - 1 > 0x7FFFFFFFll) return refuse("the last position is past 2^31 - 1");
   if (!d->norm && (d->q_weight || d->k_weight)) return refuse("weights without the norm");
   if (negative(d->q, d->k, d->q_out, d->k_out, d->dq, d->dk)) return refuse("a stride is negative");
   if (d->head_dim > PRISM_MAX_NORM_HEAD) return refuse("head_dim is over PRISM_MAX_NORM_HEAD", PRISM_EUNSUPPORTED);

@@ -145,3 +145,14 @@ def test_grids_that_no_launch_takes_are_refused_by_the_check(prism):
     o.q.batch, o.q.token, o.q.head = 1030 * 41, 1030 * 41, 41               # (rows of no whole vectors: a work-item for 16 entries)
     o.q_out = o.q
     assert prism.lib().prism_qk_norm_rope(ADDRESS, None, ADDRESS, None, prism.BF16, ctypes.byref(o), None) == prism.EUNSUPPORTED
+
+
+def test_positions_past_32_bits_are_refused(prism):
+    o = prism.NormRopeDesc()
+    o.batch, o.len, o.q_heads, o.head_dim, o.scale, o.start = 1, 3, 1, 8, 1.0, 2 ** 31 - 2
+    size = ctypes.c_size_t(0)
+    assert prism.lib().prism_norm_rope_workspace_bytes(prism.F32, ctypes.byref(o), ctypes.byref(size)) == prism.EINVAL
+    o.start -= 1
+    assert prism.lib().prism_norm_rope_workspace_bytes(prism.F32, ctypes.byref(o), ctypes.byref(size)) == prism.OK
+    o.start, o.positions = 2 ** 31 - 2, ADDRESS
+    assert prism.lib().prism_norm_rope_workspace_bytes(prism.F32, ctypes.byref(o), ctypes.byref(size)) == prism.OK
