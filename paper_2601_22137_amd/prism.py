@@ -331,6 +331,7 @@ def read_reports(infos):
 
 _NORM_ROPE = struct.Struct("@9i2f4P18qPN")
 _ATTENTION = struct.Struct("@7i2f5P24qPN")
+_NO_NUMBER = (struct.error, OverflowError)      # of pack: what a field does not hold
 _NO_STRIDES = (0, 0, 0)
 _NONE = (None, None)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -382,7 +383,7 @@ def _given(workspace, dev):
 
 def dropout(x, p, seed, offset=0, residual=None, out=None):
     """residual + dropout(x): every element is kept with probability 1 - p (rounded to 16 bits) and then divided by it.  The mask is a function
-    of (seed, offset, index) and is not stored: the gradient with respect to x is dropout(dy, p, seed, offset).  out may be x or residual."""
+    of (seed modulo 2^64, offset modulo 2^32, index) and is not stored: the gradient with respect to x is dropout(dy, p, seed, offset).  out may be x or residual."""
     y = torch.empty_like(x) if out is None else out
     dev = _device(x)
     for t in (x, y) if residual is None else (x, y, residual):
@@ -436,10 +437,13 @@ def _norm_rope_desc(q, k, results, grads, inv_freq, positions, start, q_weight, 
                 raise PrismError("%s: goes with its input" % names[x])
             strides += _NO_STRIDES if t is None else _heads(t, names[x], dtype, dev, (b, n, heads[x], d))
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    return some, dev, _NORM_ROPE.pack(
-        b, n, heads[0], heads[1], d, rot, 1 if norm else 0, 1 if interleaved else 0, start, eps, scale, _plain(positions, "positions", torch.int32, dev, (b, n)),
-        _plain(inv_freq, "inv_freq", torch.float32, dev, (rot // 2,)), _plain(q_weight, "q_weight", torch.float32, dev, (d,)),
-        _plain(k_weight, "k_weight", torch.float32, dev, (d,)), *strides, *_given(workspace, dev))
+    try:
+        return some, dev, _NORM_ROPE.pack(
+            b, n, heads[0], heads[1], d, rot, 1 if norm else 0, 1 if interleaved else 0, start, eps, scale, _plain(positions, "positions", torch.int32, dev, (b, n)),
+            _plain(inv_freq, "inv_freq", torch.float32, dev, (rot // 2,)), _plain(q_weight, "q_weight", torch.float32, dev, (d,)),
+            _plain(k_weight, "k_weight", torch.float32, dev, (d,)), *strides, *_given(workspace, dev))
+    except _NO_NUMBER as e:
+        raise PrismError("a number is out of range: %s" % e) from None
 
 
 def _ptr(t):
@@ -488,10 +492,13 @@ def _attention_desc(q, k, v, out, back, scale, causal, softcap, slopes, prefix, 
     else:
         strides += 4 * _NO_STRIDES
     i32 = torch.int32
-    return dev, _ATTENTION.pack(
-        b, n, m, hq, hk, d, 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap, _plain(slopes, "slopes", torch.float32, dev, (hq,)),
-        _plain(prefix, "prefix", i32, dev, (b,)), _plain(k_lens, "k_lens", i32, dev, (b,)), _plain(q_doc, "q_doc", i32, dev, (b, n)),
-        _plain(k_doc, "k_doc", i32, dev, (b, m)), *strides, *_given(workspace, dev))
+    try:
+        return dev, _ATTENTION.pack(
+            b, n, m, hq, hk, d, 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap, _plain(slopes, "slopes", torch.float32, dev, (hq,)),
+            _plain(prefix, "prefix", i32, dev, (b,)), _plain(k_lens, "k_lens", i32, dev, (b,)), _plain(q_doc, "q_doc", i32, dev, (b, n)),
+            _plain(k_doc, "k_doc", i32, dev, (b, m)), *strides, *_given(workspace, dev))
+    except _NO_NUMBER as e:
+        raise PrismError("a number is out of range: %s" % e) from None
 
 
 def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, out=None, workspace=None):

@@ -612,3 +612,14 @@ def test_norm_rope_gradients_of_one_of_two(prism, norm):
     assert torch.equal(dk, both[1]) and dq is None and dqw is None and (torch.equal(dkw, both[3]) if norm else dkw is None)
     e = torch.empty(0, 4, 2, 64, device="cuda")
     assert (prism.qk_norm_rope_backward(e, None, e, None, norm=norm)[2] is None) == (not norm)
+
+
+def test_numbers_that_no_description_holds(prism):
+    q, k, f = torch.randn(1, 3, 2, 64, device="cuda"), torch.randn(1, 5, 2, 64, device="cuda"), torch.ones(32, device="cuda")
+    for kw in (dict(start=2 ** 31), dict(start=2 ** 31 - 2), dict(scale=1e39), dict(eps=1e39)):
+        with pytest.raises(prism.PrismError):
+            prism.qk_norm_rope(q, None, f, **kw)
+    prism.qk_norm_rope(q, None, f, start=2 ** 31 - 3)
+    for kw in (dict(scale=1e39), dict(softcap=1e39)):
+        with pytest.raises(prism.PrismError):
+            prism.attention(q, k, k, **kw)
