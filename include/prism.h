@@ -314,7 +314,8 @@ int prism_run_grouped_from(prism_fn fn, const prism_group* groups, const void* c
  * heads are [batch][token][head][dim] with any strides (in elements, negative ones excepted) between batches, tokens and heads;
  * the entries of a head are contiguous.  PRISM_F32 or PRISM_BF16; sums, maxima and statistics are fp32 in either.  Pointers and
  * strides that are multiples of 16 bytes are read as whole vectors, others entry by entry.  Weights, statistics, positions and masks are
- * contiguous device arrays in 32 bits.  A call repeated gives the same bits.  Empty arrays are valid: nothing is enqueued or read. */
+ * contiguous device arrays in 32 bits.  A call repeated gives the same bits.  Empty arrays are valid: nothing is enqueued or read.  A stream's cached
+ * workspace that such a call has outgrown is followed by one of twice its size (outgrown ones stay until prism_release_workspaces()). */
 typedef struct { int64_t batch, token, head; } prism_strides;
 
 /* y = residual + x [u >= limit] / (1 - limit / 65536), limit = p * 65536 rounded (half to even), for `count` contiguous elements; residual may be NULL (0).

@@ -346,8 +346,8 @@ int make_plan(Plan& P, int fn, int batch, int m, int n, int dt, int degree, int 
 std::mutex g_mu;
 WorkspaceCache g_cache;
 
-// optional: the caller takes a plan that needs less if there is no such memory
-int get_workspace(size_t bytes, const void* owner, const prism_options* opt, char** out, bool optional = false) {
+// optional: the caller takes a plan that needs less if there is no such memory; doubled: see workspace_cache.h
+int get_workspace(size_t bytes, const void* owner, const prism_options* opt, char** out, bool optional = false, bool doubled = false) {
   if (opt && opt->workspace) {
     if (opt->workspace_bytes < bytes || ((uintptr_t)opt->workspace & 255)) return PRISM_ENOMEM;
     *out = (char*)opt->workspace;
@@ -361,7 +361,7 @@ int get_workspace(size_t bytes, const void* owner, const prism_options* opt, cha
     if (hipMalloc(&fresh, n) == hipSuccess) return fresh;
     (void)hipGetLastError();
     return nullptr;
-  });
+  }, doubled);
   if (!p) {
     if (!optional) set_last_error("hipMalloc of the workspace failed");
     return PRISM_ENOMEM;
@@ -376,7 +376,7 @@ int layer_workspace(size_t bytes, void* given, size_t given_bytes, hipStream_t s
   prism_options opt = {};
   opt.workspace = given;
   opt.workspace_bytes = given_bytes;
-  const int rc = get_workspace(bytes, s, &opt, out);
+  const int rc = get_workspace(bytes, s, &opt, out, false, true);
   if (rc == PRISM_ENOMEM && given) set_last_error("the workspace is too small or not aligned to 256 bytes");
   return rc;
 }

@@ -42,3 +42,41 @@ def test_a_refused_size_is_not_asked_for_again(tmp_path):
     subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Werror", "-I" + CSRC, str(src), "-o", str(exe)])
     got = [tuple(int(v) for v in line.split()) for line in subprocess.check_output([str(exe)], text=True).splitlines()]
     assert got == [(80, 2), (80, 2), (80, 2), (95, 3), (0, 5), (0, 6), (120, 7), (90, 7), (150, 8), (1,)]
+
+
+GROWING = r"""
+#include <cstdio>
+#include "workspace_cache.h"
+int main() {
+  prism::WorkspaceCache cache;
+  static char memory[64];
+  size_t asked = 0, held = 0, limit = ~(size_t)0;
+  auto alloc = [&](size_t n) -> void* {
+    if (n > limit) return nullptr;
+    held += n;
+    return memory + asked++;
+  };
+  int one, two;
+  // sequences that become longer from call to call
+  for (size_t n = 1000; n <= 1000000; n += 1000)
+    if (!cache.get(0, &one, n, false, alloc, true)) return 1;
+  std::printf("%zu %zu\n", asked, held / 1000);
+  // the first block is of the size asked for, and so is one where there is no room to spare
+  asked = held = 0;
+  limit = 1500;
+  for (size_t n : {1000, 1100, 1050, 1600}) std::printf("%d ", cache.get(0, &two, n, false, alloc, true) != nullptr);
+  std::printf("%zu %zu\n", asked, held);
+  return 0;
+}
+"""
+
+
+def test_blocks_that_are_outgrown_again_and_again(tmp_path):
+    """All blocks together stay within a few times the last, and are few."""
+    src, exe = tmp_path / "growing.cpp", tmp_path / "growing"
+    src.write_text(GROWING.replace("#include <cstdio>", "#include <cstdio>\n#include <initializer_list>"))
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Werror", "-I" + CSRC, str(src), "-o", str(exe)])
+    first, second = subprocess.check_output([str(exe)], text=True).splitlines()
+    blocks, held = (int(x) for x in first.split())
+    assert blocks == 11 and held == 2 ** 11 - 1          # 1, 2, 4 ... 1024 thousand
+    assert second.split() == ["1", "1", "1", "0", "2", "2100"]
