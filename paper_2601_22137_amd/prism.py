@@ -399,8 +399,8 @@ def rope_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_l
        "base"      a larger base, so that the lowest frequency is divided by factor and the highest kept
        "by_turns"  frequencies that turn less than `slow` times in original_len divided by factor, more than `fast` times kept, a ramp
                    between; the rotated part is scaled by 0.1 ln(factor) + 1."""
-    if rot_dim < 2 or rot_dim % 2 or not factor > 0:
-        raise PrismError("rot_dim has to be even and positive, factor positive")
+    if rot_dim < 2 or rot_dim % 2 or not 0 < factor < np.inf or not 0 < base < np.inf:
+        raise PrismError("rot_dim has to be even and positive, factor and base positive and finite")
     half = rot_dim // 2
     if scaling == "base":
         base = base * factor ** (rot_dim / (rot_dim - 2)) if rot_dim > 2 else base
@@ -409,8 +409,8 @@ def rope_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_l
     if scaling == "linear":
         f = f / factor
     elif scaling == "by_turns":
-        if not original_len:
-            raise PrismError("by_turns needs original_len")
+        if not original_len or original_len < 0 or not fast > slow:
+            raise PrismError("by_turns needs a positive original_len, and fast above slow")
         keep = np.clip((original_len * f / (2 * np.pi) - slow) / (fast - slow), 0.0, 1.0)
         f = f * keep + f / factor * (1.0 - keep)
         scale = 0.1 * np.log(factor) + 1.0 if factor > 1.0 else 1.0

@@ -156,3 +156,12 @@ def test_positions_past_32_bits_are_refused(prism):
     assert prism.lib().prism_norm_rope_workspace_bytes(prism.F32, ctypes.byref(o), ctypes.byref(size)) == prism.OK
     o.start, o.positions = 2 ** 31 - 2, ADDRESS
     assert prism.lib().prism_norm_rope_workspace_bytes(prism.F32, ctypes.byref(o), ctypes.byref(size)) == prism.OK
+
+
+@pytest.mark.parametrize("bad", [dict(fast=1.0), dict(fast=0.5), dict(factor=float("inf")), dict(original_len=-4096), dict(base=0.0), dict(base=-1.0)])
+def test_frequencies_that_would_not_be_numbers(prism, bad):
+    kw = dict(rot_dim=8, scaling="by_turns", factor=2.0, original_len=4096)
+    assert np.all(np.isfinite(prism.rope_frequencies(**kw)[0].numpy()))
+    kw.update(bad)
+    with pytest.raises(prism.PrismError):
+        prism.rope_frequencies(**kw)
