@@ -93,6 +93,9 @@ class Cache(tuple):
         self.longest, self.version = 0, None
         return self
 
+    def __getnewargs__(self):          # copies and pickles
+        return tuple(self)
+
     def _written(self):
         """Changes with every write to lens (tensors of inference mode do not tell)."""
         lens = self[2]

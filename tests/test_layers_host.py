@@ -196,3 +196,19 @@ def test_no_part_of_a_head_turns(monkeypatch):
         m = layers.SelfAttention(16, 2, rot_dim=rot, device="cpu", dtype=torch.float32)
         m(torch.randn(1, 3, 16))
         assert (0 if seen[-1] is None else seen[-1].numel()) == frequencies
+
+
+def test_caches_are_copied(tmp_path):
+    import copy
+    import pickle
+    m, x = _layer(), torch.randn(2, 1, 16)
+    cache = m.new_cache(2, 2)
+    m.step(x, cache)
+    for other in (copy.deepcopy(cache), pickle.loads(pickle.dumps(cache)), copy.copy(cache)):
+        assert all(torch.equal(a, b) for a, b in zip(cache, other))
+    other = copy.deepcopy(cache)
+    m.step(x, other)
+    assert cache[2].tolist() == [1, 1] and other[2].tolist() == [2, 2]
+    with pytest.raises(prism.PrismError, match="2 tokens"):
+        m.step(x, other)
+    m.step(x, cache)
