@@ -375,12 +375,13 @@ typedef struct {
 /* out = softmax of the scores over the keys that a query sees, times v.  lse (fp32 [batch][q_heads][q_len], or NULL) receives the
  * logarithm of the sum of the exponentials, which the backward pass reads.  A query that sees no key gets out = 0 and
  * lse = -inf, and gradient 0.  Keys and values past a sequence's length or of a negative document, and queries that see no key (and their dout), may
- * hold anything.  What some query sees has to be finite: where another does not see it, its weight is 0, and 0 times an infinity NaN.
- * bf16 rounds the weights to bf16 before their product with v. */
+ * hold anything.  All else has to be finite: where a query does not see a key, its weight is 0, and 0 times an infinity NaN.
+ * bf16 rounds the weights to bf16 before their product with v.  out may not overlap an input. */
 int prism_attention(const void* q, const void* k, const void* v, void* out, float* lse, prism_dtype dt,
                     const prism_attention_desc* desc, void* stream);
 /* Gradients with respect to q, k and v; out and lse are those of the forward pass.  Shared key heads receive the sum over their query
- * heads.  dq, dk and dv may not overlap any input. */
+ * heads.  dq, dk and dv may not overlap any input.  bf16 rounds the weights and the gradients of the scores to bf16 before their products (dv; dq and dk), and takes the row sums
+ * of dout out from the rounded out where a row's tile sees more than 512 keys: entries are off by some 2^-8 of what they are sums of. */
 int prism_attention_backward(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse,
                              void* dq, void* dk, void* dv, prism_dtype dt, const prism_attention_desc* desc, void* stream);
 int prism_attention_workspace_bytes(prism_dtype dt, const prism_attention_desc* desc, int backward, size_t* out_bytes);

@@ -6,9 +6,11 @@
 // flight.  Scores come out of the product K Q^T with a row per lane, so a row's maximum and sum are plain arithmetic in its own two lanes, and the
 // weights go from the registers straight into V^T P^T (attention_tile.h).
 //
-// Scores, maxima, sums and results are held in 32 bits; the weights are rounded to the type of the values for the second product.  Long prompts in bf16 are bound by the reads of
-// LDS (every wave reads all keys and values of a tile for its 32 rows) and the power limit: 8192 tokens, 32 heads of 128 on 8, causal: 511 us, 1.08 PFLOP/s of the 1.32 that a large
-// product of the vendor library reaches.  Twice the rows per wave halve the reads, but leave one wave per SIMD: 614 us.
+// Scores, maxima, sums and results are held in 32 bits; the weights are rounded to the type of the values for the second product.  Long prompts in bf16, 8192 tokens, 32 heads of 128
+// on 8, causal: 535 us, 1.03 PFLOP/s of the 1.32 that a large product of the vendor library reaches (555 to 660 in runs of these calls alone).  The matrix units are busy 59 % of
+// the cycles, the vector units 50, LDS 30 without conflicts; the waves wait for data or a barrier 28 % of theirs; and the clock is down to 1.6 GHz, the power limit.  Twice the rows per wave
+// halve the reads of LDS, but leave one wave per SIMD: 614 us against 518 when it was tried.  Capped scores (2 x 4096 tokens, 16 heads of 128 on 4: 245 us) are bound by the vector units, 68 % busy
+// beside matrix units at 31: three transcendental instructions a score (exp2 and rcp for the tanh, exp2 for the weight), the tanh with no product beside it.
 #include "attention_tile.h"
 
 namespace prism {
@@ -47,7 +49,7 @@ __device__ inline void finish(const Attn& p, const f32x16 (&acc)[DP / 32], float
   }
 }
 
-// (fp32) Bound by the matrix units' waits for its operands and, in short calls, by how evenly the parts fill the chip: 2 x 2048 x 8 heads of 128, causal: 199 us, 86 TFLOP/s of the
+// (fp32) Bound by the matrix units (2 x 1111 tokens, 8 heads of 80: busy 53 % of the cycles, the waves wait to issue half of theirs) and, in short calls, by how evenly the parts fill the chip: 2 x 2048 x 8 heads of 128, causal: 199 us, 86 TFLOP/s of the
 // pairs that are seen; 2 x 4096, all seen, 1094 us, 126 of 154.
 template <typename T, int DP>
 __global__ void __launch_bounds__(NT, 2) attention_kernel(Attn p) {
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(NT, DP > 64 ? 2 : 3) attention_bf16_kernel(Att
 // Few rows (32 of a pair at most, as when single tokens are generated for a group of heads): the time is that of reading the keys and values once.  Every wave
 // takes blocks of 32 keys of its own, with no barrier between them, through its own part of LDS (as an operand straight from memory every load of keys would touch 32 lines):
 // the keys are read into registers at once, which makes room for the next block's, the values lie in two blocks.  The waves' results are joined in LDS.
-// 8 tokens of 32 heads on 8 of 128, 4096 to 16384 keys, capped: 75 us and 5 for the join, 4.5 TB/s; with the kernel above 105.  One token of 8 heads on 2, 32768 keys: 13.9 and 20.2; 8 on
+// 8 tokens of 32 heads on 8 of 128, 4096 to 16384 keys, capped: 75 us and 5 for the join, 4.5 TB/s (waves wait for data 42 % of their cycles); with the kernel above 105.  One token of 8 heads on 2, 32768 keys: 13.9 and 20.2; 8 on
 // 2048 keys each: 21.9 and 19.5, where its join of four waves shows.
 template <int DP, bool MOD, bool SERIES>
 __global__ void __launch_bounds__(NT, 2) attention_few_kernel(Attn p) {

@@ -6,8 +6,9 @@
 // shared heads need no sum afterwards).  Seven products instead of five, but no sum across workgroups whose order could change the bits of dq.
 //
 // Scores, dp, D and all sums are held in 32 bits; p and ds are rounded to the operands' type for the products that follow, as results are.  2 x 4096 tokens, 16 heads of 128 on 4, causal,
-// capped, bf16: dq 300 us (tanh and exp, two transcendental instructions each, beside three products), dk and dv 485 and 24 for the sum of their parts (four products; waits for the
-// tiles); 2 x 1111, 8 heads of 80 with prefix and bias in fp32: 116 and 163.
+// capped, bf16: dq 310 us (three transcendental instructions a score, exp2 and rcp for the tanh, exp2 for the weight: vector units busy 76 % of the cycles, matrix units 37), dk and dv 480
+// and 25 for the sum of their parts (matrix units 33 %, vector units 53; the waves wait for data or a barrier 36 % of their cycles); 2 x 1111, 8 heads of 80 with prefix and bias in fp32:
+// 117 and 164 (matrix units 53 and 48 %, one wave per SIMD).
 #include "attention_tile.h"
 
 namespace prism {

@@ -8,7 +8,7 @@
 // turns in 64 bits (32 would lose 0.004 rad at position 10^5); a lane computes its eight sines and cosines once and uses them for HS heads of its token.
 //
 // Bound by memory: every entry is read and written once (gradients: two read, one written), sums and statistics are in 32 bits, results are rounded once.  4 x 4096 tokens,
-// 32 + 8 heads of 128, bf16: 80 us (335 MB, 4.2 TB/s) and gradients 109 + 6 us (503 MB, 4.6 TB/s); a large copy runs at 4.6 to 5.4.
+// 32 + 8 heads of 128, bf16: 78 us (335 MB, 4.3 TB/s) and gradients 104 + 7 us (503 MB, 4.8 TB/s; vector units 60 and 69 % busy); a large copy runs at 4.6 to 5.4.
 #include "layer.h"
 
 namespace prism {
