@@ -84,13 +84,17 @@ def dropout(x, p, seed, offset=0, residual=None):
     return _Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(), p, seed, offset)
 
 
+def _capturing(t):
+    return t.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
 class Cache(tuple):
     """(keys, values, lens): [batch, length, k_heads, dim] twice, and how many tokens there are of each sequence, int32 on the device.  How many the longest has is
-    also known on the host; it is read from the device only after lens was written to by others."""
+    also known on the host; it is read from the device only after lens was written to by others, or by a step that was captured into a graph."""
 
     def __new__(cls, keys, values, lens):
         self = tuple.__new__(cls, (keys, values, lens))
-        self.longest, self.version = 0, None
+        self.longest, self.version, self.captured = 0, None, False
         return self
 
     def __getnewargs__(self):          # copies and pickles
@@ -101,13 +105,20 @@ class Cache(tuple):
         lens = self[2]
         return 0 if lens.is_inference() else lens._version
 
+    def _read(self):
+        lens = self[2]
+        return int(lens.max()) if lens.numel() else 0
+
     def last_place(self):
         """Index of the last token there is room for; an error, before anything is written, if it is taken."""
         keys, _, lens = self
-        if self.version != self._written():
-            self.longest = int(lens.max()) if lens.numel() else 0
-        if self.longest >= keys.shape[1]:
-            raise prism.PrismError("the cache is full: it is made for %d tokens" % keys.shape[1])
+        if _capturing(lens):
+            self.captured = True
+        else:
+            if self.captured or self.version != self._written():
+                self.longest = self._read()
+            if self.longest >= keys.shape[1]:
+                raise prism.PrismError("the cache is full: it is made for %d tokens" % keys.shape[1])
         return keys.shape[1] - 1
 
     def took_one(self):
@@ -159,8 +170,8 @@ class SelfAttention(torch.nn.Module):
 
     @torch.no_grad()
     def step(self, x, cache):
-        """One token of each sequence, x [batch, 1, width], behind the tokens in the cache, which takes it in.  (A step that is captured into a graph is counted once: how
-        often it is replayed is the caller's to count.  Tokens too many then replace the last one.)"""
+        """One token of each sequence, x [batch, 1, width], behind the tokens in the cache, which takes it in.  (How often a step that is captured into a graph is
+        replayed is the caller's to count: tokens too many then replace the last one.)"""
         if not isinstance(cache, Cache):
             cache = Cache(*cache)
         last = cache.last_place()

@@ -142,3 +142,33 @@ def test_second_derivatives(layers):
         (g,) = torch.autograd.grad((call() ** 2).sum(), q, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             g.sum().backward()
+
+
+def test_step_in_a_graph(layers):
+    """Captured after the lengths were set by hand, replayed on new tokens with eager work between; the same tokens eagerly; then past the cache's end, which only loses tokens."""
+    torch.manual_seed(6)
+    m = layers.SelfAttention(64, 4, 2, head_dim=32, dtype=torch.float32)
+    m.eval()
+    tokens = torch.randn(7, 3, 1, 64, device="cuda")
+    x, cache, eager = tokens[0].clone(), m.new_cache(3, 5), m.new_cache(3, 5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.no_grad():
+        m.step(x, cache)
+        cache[2].zero_()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        y = m.step(x, cache)
+    for i in range(7):
+        x.copy_(tokens[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        if i < 5:
+            assert torch.equal(y, m.step(tokens[i], eager)) and torch.equal(cache[0], eager[0])
+        assert torch.isfinite(y).all()
+    for c in (cache, eager):
+        from paper_2601_22137_amd import prism
+        with pytest.raises(prism.PrismError, match="5 tokens"):
+            m.step(x, c)

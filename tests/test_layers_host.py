@@ -212,3 +212,23 @@ def test_caches_are_copied(tmp_path):
     with pytest.raises(prism.PrismError, match="2 tokens"):
         m.step(x, other)
     m.step(x, cache)
+
+
+def test_a_step_that_is_captured_reads_nothing(monkeypatch):
+    """While a stream is captured the lengths cannot be read; afterwards they change unseen, so they are read before every other step."""
+    m, x = _layer(), torch.randn(2, 1, 16)
+    cache = m.new_cache(2, 4)
+    m.step(x, cache)
+    cache[2].zero_()
+    reads, capturing = [], [True]
+    monkeypatch.setattr(layers, "_capturing", lambda t: capturing[0])
+    monkeypatch.setattr(layers.Cache, "_read", lambda self, plain=layers.Cache._read: (reads.append(1), plain(self))[1])
+    m.step(x, cache)
+    assert not reads
+    capturing[0] = False
+    with torch.no_grad():
+        cache[2].data.add_(2)             # replays, which no version tells of
+    m.step(x, cache)
+    assert len(reads) == 1 and cache[2].tolist() == [4, 4]
+    with pytest.raises(prism.PrismError, match="4 tokens"):
+        m.step(x, cache)
