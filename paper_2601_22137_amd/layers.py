@@ -70,7 +70,10 @@ def _fixed(t, name):
 def norm_rope(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, start=0, norm=True, interleaved=False, scale=1.0, eps=1e-6):
     """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights."""
     _fixed(inv_freq, "inv_freq")
-    return _NormRope.apply(q, k, q_weight, k_weight, inv_freq, positions, dict(start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps))
+    options = dict(start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps)
+    if not torch.is_grad_enabled():       # tokens one by one: the host's time counts
+        return prism.qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, positions=positions, **options)
+    return _NormRope.apply(q, k, q_weight, k_weight, inv_freq, positions, options)
 
 
 def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefix=None, k_lens=None, q_doc=None, k_doc=None, workspace=None):
@@ -95,6 +98,7 @@ class Cache(tuple):
     def __new__(cls, keys, values, lens):
         self = tuple.__new__(cls, (keys, values, lens))
         self.longest, self.version, self.captured = 0, None, False
+        self.rows = torch.arange(lens.shape[0], device=lens.device)
         return self
 
     def __getnewargs__(self):          # copies and pickles
@@ -178,7 +182,7 @@ class SelfAttention(torch.nn.Module):
         keys, values, lens = cache
         b = x.shape[0]
         q, k, v = self._project(x, lens.view(b, 1))
-        at = torch.arange(b, device=x.device), lens.clamp(0, last).long()
+        at = cache.rows, lens.clamp(0, last).long()
         keys[at], values[at] = k[:, 0], v[:, 0]
         lens += 1
         cache.took_one()
