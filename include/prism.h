@@ -386,6 +386,88 @@ int prism_attention_backward(const void* dout, const void* q, const void* k, con
                              void* dq, void* dk, void* dv, prism_dtype dt, const prism_attention_desc* desc, void* stream);
 int prism_attention_workspace_bytes(prism_dtype dt, const prism_attention_desc* desc, int backward, size_t* out_bytes);
 
+/* ---- operators at the ends of a model, around those of its layers ----
+ *
+ * The conventions of the operators of a layer.  Arrays of rows are [rows][width] with any stride (in elements, not negative) between rows; the entries of a row are
+ * contiguous, and rows may start at any element.  Tokens are a contiguous device array, int64_t where wide_tokens is set, int32_t where it is not.  Weights, statistics and
+ * whatever there is one of for a row are contiguous fp32. */
+
+typedef struct {
+  int64_t count, rows;       /* tokens (at most 2^30), rows of the table (at most 2^27) */
+  int32_t width;
+  int32_t wide_tokens;
+  float scale;
+  int64_t table_stride;      /* between rows of the table (backward: of its gradient) */
+  int64_t out_stride;        /* between rows of out (backward: of dout) */
+  void* workspace;           /* backward: device memory aligned to 256 bytes, or NULL for the stream's cached one */
+  size_t workspace_bytes;
+} prism_embedding_desc;
+
+/* out[i] = scale * table[tokens[i]] for `count` tokens, rounded once.  A token that is no row of the table (padding) gives a row of zeros. */
+int prism_embedding(const void* table, const void* tokens, void* out, prism_dtype dt, const prism_embedding_desc* desc, void* stream);
+/* dtable[v] = scale * the sum of dout[i] over the tokens i that name row v, in fp32 (runs of more than a tile of tokens: their parts in fp64), rounded once; every
+ * row is written, with zeros where no token names it.  Rows of dout whose token is no row of the table are not read. */
+int prism_embedding_backward(const void* dout, const void* tokens, void* dtable, prism_dtype dt, const prism_embedding_desc* desc, void* stream);
+int prism_embedding_workspace_bytes(prism_dtype dt, const prism_embedding_desc* desc, size_t* out_bytes);
+
+#define PRISM_MAX_NORM_WIDTH 16384   /* largest width of prism_layer_norm */
+
+typedef struct {
+  int64_t rows;
+  int32_t width;
+  int32_t center;            /* the mean is taken off; 0: root mean square only, mean = 0 */
+  float eps;
+  int64_t x, residual, total, y;   /* strides of the arrays of these names */
+  int64_t dy, dtotal, dx;          /* backward (with total) */
+  void* workspace;           /* backward: device memory aligned to 256 bytes, or NULL for the stream's cached one */
+  size_t workspace_bytes;
+} prism_layer_norm_desc;
+
+/* total = x + residual (rounded), y = (total - mean) (mean (total - mean)^2 + eps)^(-1/2) weight + bias, for every row.  residual may be NULL, and total then is: it is x.
+ * weight [width] may be NULL (ones), bias too (zeros).  stats [rows][2] (or NULL) receives mean and the root's inverse, which the backward pass reads.  total and y may each be x or
+ * the residual with the same stride, but not one another. */
+int prism_layer_norm(const void* x, const void* residual, const float* weight, const float* bias, void* y, void* total, float* stats, prism_dtype dt,
+                     const prism_layer_norm_desc* desc, void* stream);
+/* Gradients: dx (of x, and of the residual, which has the same), dweight and dbias [width] (NULL: not wanted), summed over the rows in a fixed order, from those of y and,
+ * where dtotal is not NULL, of total, which is added to dx.  dx may be dy or dtotal with the same stride. */
+int prism_layer_norm_backward(const void* dy, const void* total, const float* stats, const float* weight, const void* dtotal, void* dx, float* dweight, float* dbias,
+                              prism_dtype dt, const prism_layer_norm_desc* desc, void* stream);
+int prism_layer_norm_workspace_bytes(prism_dtype dt, const prism_layer_norm_desc* desc, size_t* out_bytes);
+
+typedef struct {
+  int64_t rows;
+  int32_t vocabulary;        /* logits of a row */
+  int32_t wide_tokens;
+  double scale;              /* > 0: logits are taken times it (one over the temperature) */
+  int64_t logits_stride, dlogits_stride;
+  /* prism_policy_loss only */
+  double clip_low, clip_high; /* the ratio is held between 1 - clip_low and 1 + clip_high */
+  double kl;                 /* factor of the divergence from the reference; 0: none */
+  const float* advantages;   /* [rows], or NULL: ones */
+  const float* old_logp;     /* [rows], or NULL: no ratio, the loss of a row is -advantage * logp */
+  const float* ref_logp;     /* [rows], or NULL where kl is 0 */
+  const float* weights;      /* [rows], or NULL: one over the number of rows that have a token */
+  void* workspace;           /* device memory aligned to 256 bytes, or NULL for the stream's cached one */
+  size_t workspace_bytes;
+} prism_logits_desc;
+
+/* logp[row] = scale * logits[row][token] - lse[row], lse = the logarithm of the sum of exp(scale * logits[row]), fp32 (either may be NULL).  A row whose token is not in 0 .. vocabulary - 1
+ * (padding) is not read: 0 in both.  Logits may be -inf (excluded: probability 0; logp -inf if it is the token's), but neither +inf nor NaN; scale times them has to stay
+ * in the range of fp32. */
+int prism_token_logprob(const void* logits, const void* tokens, float* logp, float* lse, prism_dtype dt, const prism_logits_desc* desc, void* stream);
+/* dlogits = scale * dlogp[row] * ([j is the token] - exp(scale * logits[row][j] - lse[row])), rounded once; zeros in rows without a token (whose dlogp is not read).  lse as the
+ * forward call gave it.  dlogits may be logits with the same stride. */
+int prism_token_logprob_backward(const float* dlogp, const void* logits, const void* tokens, const float* lse, void* dlogits, prism_dtype dt,
+                                 const prism_logits_desc* desc, void* stream);
+/* loss (fp32, one) = the sum over rows with a token of weight * l, in a fixed order,
+ *   l = -min(r A, clip(r) A) + kl (exp(f) - f - 1),  r = exp(logp - old_logp), f = ref_logp - logp, A = advantage
+ * (without old_logp: l = -A logp + ..., with neither that nor advantages the cross entropy), and its gradient with respect to the logits, in one pass over them.  Where r A = clip(r) A the
+ * gradient is that of r A.  Rows of weight 0 add nothing, whatever their ratio.  dlogp (the gradient with respect to logp), logp, lse and dlogits may each be NULL.  dlogits may be
+ * logits with the same stride. */
+int prism_policy_loss(const void* logits, const void* tokens, float* loss, float* logp, float* lse, float* dlogp, void* dlogits, prism_dtype dt,
+                      const prism_logits_desc* desc, void* stream);
+int prism_policy_loss_workspace_bytes(const prism_logits_desc* desc, size_t* out_bytes);
+
 /* ---- single steps of the path, exposed for unit tests and profiling ---- */
 
 /* S_k^T (Section 4.2: Gaussian sketch): out[n][sketch_dim] fp32 on the device,
@@ -446,9 +528,9 @@ int prism_gemm_bf16_nt(const uint16_t* A, const uint16_t* B, float* C, int batch
  * bracketed by a HIP event pair on the caller's stream.  prism_profile_enable(on) also discards
  * what was recorded so far.  prism_profile_collect waits for the recorded events and returns the
  * summed milliseconds and the launch counts per kernel kind (host arrays of PRISM_PROFILE_KINDS
- * entries; nkinds >= PRISM_PROFILE_KINDS, or 20 or 23: without the kinds that came after those).  Meant for a single benchmarking thread; calls from
+ * entries; nkinds >= PRISM_PROFILE_KINDS, or 20, 23 or 31: without the kinds that came after those).  Meant for a single benchmarking thread; calls from
  * other threads while it is enabled are recorded too (the record list is locked). */
-#define PRISM_PROFILE_KINDS 31
+#define PRISM_PROFILE_KINDS 40
 int prism_profile_enable(int on);
 int prism_profile_collect(double* ms_by_kind, long long* launches_by_kind, int nkinds);
 

@@ -396,6 +396,8 @@ enum ProfKind {
   PK_SMALL_ROOT,     // inverse roots of padded order 64, whole calls
   PK_DROPOUT, PK_NORM_ROPE, PK_NORM_ROPE_BACKWARD,
   PK_ATTENTION, PK_ATTENTION_JOIN, PK_ATTENTION_DOCS, PK_ATTENTION_DQ, PK_ATTENTION_DKV,
+  PK_EMBEDDING, PK_EMBEDDING_SORT, PK_EMBEDDING_BACKWARD, PK_LAYER_NORM, PK_LAYER_NORM_BACKWARD,
+  PK_LOGPROB, PK_LOGPROB_BACKWARD, PK_POLICY_LOSS, PK_LOSS_SUM,
   PK_COUNT
 };
 struct ProfScope {   // records an event pair around the launches made during its lifetime

@@ -1,4 +1,5 @@
-// Declarations shared by the operators of a transformer layer (dropout, norm and rotation of queries and keys, attention).
+// Declarations shared by the operators of a transformer layer (dropout, norm and rotation of queries and keys, attention) and of the ends
+// of a model around them (embedding, norm of the residual stream, log-probabilities and losses).
 #pragma once
 #include "common.h"
 
@@ -28,5 +29,26 @@ void launch_doc_ranges(const prism_attention_desc& d, int4* to, hipStream_t s);
 int launch_attention(const void* q, const void* k, const void* v, void* out, float* lse, int dt, const prism_attention_desc& d, char* ws, hipStream_t s);
 int launch_attention_backward(const void* dout, const void* q, const void* k, const void* v, const void* out, const float* lse, void* dq, void* dk,
                               void* dv, int dt, const prism_attention_desc& d, char* ws, hipStream_t s);
+
+int launch_embedding(const void* table, const void* tokens, void* out, int dt, const prism_embedding_desc& d, hipStream_t s);
+struct EmbeddingPlan {
+  int chunks, tile, tiles;              // 64 vectors of 16 bytes each in a row; sorted tokens of a tile; tiles
+  size_t o_sorted, o_part, total;       // bytes from the start of the workspace, where the starts of the rows' tokens lie
+};
+EmbeddingPlan embedding_plan(const prism_embedding_desc& d, int dt);
+int launch_embedding_backward(const void* dout, const void* tokens, void* dtable, int dt, const prism_embedding_desc& d, char* ws, hipStream_t s);
+
+int launch_layer_norm(const void* x, const void* residual, const float* weight, const float* bias, void* y, void* total, float* stats, int dt,
+                      const prism_layer_norm_desc& d, hipStream_t s);
+size_t layer_norm_backward_bytes(const prism_layer_norm_desc& d, int dt);
+// part: partial sums of the gradients of weight and bias, or null where neither is wanted
+int launch_layer_norm_backward(const void* dy, const void* total, const float* stats, const float* weight, const void* dtotal, void* dx, float* dweight,
+                               float* dbias, int dt, const prism_layer_norm_desc& d, float* part, hipStream_t s);
+
+int launch_logprob(const void* z, const void* tokens, float* logp, float* lse, int dt, const prism_logits_desc& d, hipStream_t s);
+int launch_logprob_backward(const float* dlogp, const void* z, const void* tokens, const float* lse, void* dz, int dt, const prism_logits_desc& d, hipStream_t s);
+size_t policy_loss_bytes(const prism_logits_desc& d);
+int launch_policy_loss(const void* z, const void* tokens, float* loss, float* logp, float* lse, float* dlogp, void* dz, int dt, const prism_logits_desc& d, char* ws,
+                       hipStream_t s);
 
 }  // namespace prism

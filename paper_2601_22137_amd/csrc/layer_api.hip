@@ -78,6 +78,47 @@ int check(const prism_attention_desc* d, int dt) {
 // no result at all (keys without queries have gradients: zero)
 bool empty(const prism_attention_desc& d, bool backward) { return d.batch == 0 || d.q_heads == 0 || (d.q_len == 0 && (!backward || d.k_len == 0)); }
 
+int size_of(int dt) { return dt == PRISM_F32 ? 4 : 2; }
+// negative, or so long that the rows end past 2^60 elements
+template <typename... S> bool bad_stride(long long rows, S... s) { return ((s < 0 || (s > 0 && rows > (1ll << 60) / s)) || ...); }
+
+// Rows of a result that lie over one another
+bool overlap(long long rows, long long width, long long stride) { return rows > 1 && stride < width; }
+constexpr const char* OVERLAP = "rows of a result lie over one another";
+
+int check(const prism_embedding_desc* d, int dt) {
+  if (!d || !is_type(dt)) return refuse("null description or unknown type");
+  if (d->count < 0 || d->rows < 0 || d->width < 1) return refuse("negative size, or rows without entries");
+  if (!std::isfinite(d->scale)) return refuse("scale is not finite");
+  if (bad_stride(d->rows, d->table_stride) || bad_stride(d->count, d->out_stride)) return refuse("a stride is negative, or an array ends past 2^60 elements");
+  if (d->count > (1ll << 30) || d->rows > (1ll << 27) || d->width > (1 << 24)) return refuse("more than 2^30 tokens, 2^27 rows or 2^24 entries of a row", PRISM_EUNSUPPORTED);
+  return PRISM_OK;
+}
+
+int check(const prism_layer_norm_desc* d, int dt) {
+  if (!d || !is_type(dt)) return refuse("null description or unknown type");
+  if (d->rows < 0 || d->width < 1) return refuse("negative size, or rows without entries");
+  if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return refuse("eps has to be finite and not negative");
+  if (bad_stride(d->rows, d->x, d->residual, d->total, d->y, d->dy, d->dtotal, d->dx)) return refuse("a stride is negative, or an array ends past 2^60 elements");
+  if (d->width > PRISM_MAX_NORM_WIDTH) return refuse("width is over PRISM_MAX_NORM_WIDTH", PRISM_EUNSUPPORTED);
+  if (d->rows > MAX_ROWS) return refuse("more than 2^31 - 1 rows", PRISM_EUNSUPPORTED);
+  return PRISM_OK;
+}
+
+int check(const prism_logits_desc* d, int dt, bool loss) {
+  if (!d || !is_type(dt)) return refuse("null description or unknown type");
+  if (d->rows < 0 || d->vocabulary < 1) return refuse("negative size, or rows without logits");
+  if (!(d->scale > 0.0) || !std::isnormal((float)d->scale) || !std::isfinite((float)(d->scale * 1.4426950408889634))) return refuse("scale and scale log2(e) have to be positive and in the range of fp32");
+  if (bad_stride(d->rows, d->logits_stride, d->dlogits_stride)) return refuse("a stride is negative, or an array ends past 2^60 elements");
+  if (loss) {
+    if (!(d->clip_low >= 0.0 && d->clip_low <= 1.0) || !(d->clip_high >= 0.0) || !std::isfinite(d->clip_high)) return refuse("clip_low has to be in 0 .. 1, clip_high finite and not negative");
+    if (!(d->kl >= 0.0) || !std::isfinite(d->kl)) return refuse("kl has to be finite and not negative");
+    if (d->kl > 0.0 && !d->ref_logp) return refuse("kl without ref_logp");
+  }
+  if (d->rows > MAX_ROWS || d->vocabulary > (1 << 30)) return refuse("more than 2^31 - 1 rows or 2^30 logits of a row", PRISM_EUNSUPPORTED);
+  return PRISM_OK;
+}
+
 }  // namespace
 }  // namespace prism
 
@@ -185,6 +226,147 @@ int prism_attention_workspace_bytes(prism_dtype dt, const prism_attention_desc* 
     if (!out_bytes) return refuse("null pointer");
     const int rc = check(d, (int)dt);
     if (rc == PRISM_OK) *out_bytes = empty(*d, backward != 0) ? 0 : attention_plan(*d, (int)dt, backward != 0).total;
+    return rc;
+  });
+}
+
+int prism_embedding(const void* table, const void* tokens, void* out, prism_dtype dt, const prism_embedding_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    const int rc = check(d, (int)dt);
+    if (rc != PRISM_OK || d->count == 0) return rc;
+    if (!tokens || !out || (d->rows && !table)) return refuse("null pointer");
+    if (overlap(d->count, d->width, d->out_stride)) return refuse(OVERLAP);
+    if (!aligned_to(table, size_of(dt)) || !aligned_to(out, size_of(dt)) || !aligned_to(tokens, d->wide_tokens ? 8 : 4)) return refuse("a pointer is not aligned to the element size");
+    launch_embedding(table, tokens, out, (int)dt, *d, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_embedding_backward(const void* dout, const void* tokens, void* dtable, prism_dtype dt, const prism_embedding_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    int rc = check(d, (int)dt);
+    if (rc != PRISM_OK || d->rows == 0) return rc;
+    if (!dtable || (d->count && (!tokens || !dout))) return refuse("null pointer");
+    if (overlap(d->rows, d->width, d->table_stride)) return refuse(OVERLAP);
+    if (!aligned_to(dtable, size_of(dt)) || !aligned_to(dout, size_of(dt)) || !aligned_to(tokens, d->wide_tokens ? 8 : 4)) return refuse("a pointer is not aligned to the element size");
+    char* ws = nullptr;
+    rc = layer_workspace(embedding_plan(*d, (int)dt).total, d->workspace, d->workspace_bytes, (hipStream_t)stream, &ws);
+    if (rc != PRISM_OK) return rc;
+    launch_embedding_backward(dout, tokens, dtable, (int)dt, *d, ws, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_embedding_workspace_bytes(prism_dtype dt, const prism_embedding_desc* d, size_t* out_bytes) {
+  return guarded([&]() -> int {
+    if (!out_bytes) return refuse("null pointer");
+    const int rc = check(d, (int)dt);
+    if (rc == PRISM_OK) *out_bytes = d->rows ? embedding_plan(*d, (int)dt).total : 0;
+    return rc;
+  });
+}
+
+int prism_layer_norm(const void* x, const void* residual, const float* weight, const float* bias, void* y, void* total, float* stats, prism_dtype dt,
+                     const prism_layer_norm_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    const int rc = check(d, (int)dt);
+    if (rc != PRISM_OK || d->rows == 0) return rc;
+    if (!x || !y) return refuse("null pointer");
+    if (!residual != !total) return refuse("residual and total go together");
+    if (y == total) return refuse("y and total are the same array");
+    if (overlap(d->rows, d->width, d->y) || (total && overlap(d->rows, d->width, d->total))) return refuse(OVERLAP);
+    for (const void* p : {x, residual, (const void*)y, (const void*)total})
+      if (!aligned_to(p, size_of(dt))) return refuse("a pointer is not aligned to the element size");
+    for (const void* p : {(const void*)weight, (const void*)bias})
+      if (!aligned_to(p, 4)) return refuse("a pointer is not aligned to the element size");
+    if (!aligned_to(stats, 8)) return refuse("stats are not aligned to 8 bytes");
+    launch_layer_norm(x, residual, weight, bias, y, total, stats, (int)dt, *d, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_layer_norm_backward(const void* dy, const void* total, const float* stats, const float* weight, const void* dtotal, void* dx, float* dweight, float* dbias,
+                              prism_dtype dt, const prism_layer_norm_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    int rc = check(d, (int)dt);
+    if (rc != PRISM_OK) return rc;
+    if (d->rows && (!dy || !total || !stats || !dx)) return refuse("null pointer");
+    if (overlap(d->rows, d->width, d->dx)) return refuse(OVERLAP);
+    for (const void* p : {dy, total, dtotal, (const void*)dx})
+      if (!aligned_to(p, size_of(dt))) return refuse("a pointer is not aligned to the element size");
+    for (const void* p : {(const void*)weight, (const void*)dweight, (const void*)dbias})
+      if (!aligned_to(p, 4)) return refuse("a pointer is not aligned to the element size");
+    if (!aligned_to(stats, 8)) return refuse("stats are not aligned to 8 bytes");
+    if (d->rows == 0 && !dweight && !dbias) return PRISM_OK;
+    char* ws = nullptr;
+    if (dweight || dbias) {      // (of no rows: zeros)
+      rc = layer_workspace(layer_norm_backward_bytes(*d, (int)dt) + 256, d->workspace, d->workspace_bytes, (hipStream_t)stream, &ws);
+      if (rc != PRISM_OK) return rc;
+    }
+    launch_layer_norm_backward(dy, total, stats, weight, dtotal, dx, dweight, dbias, (int)dt, *d, (float*)ws, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_layer_norm_workspace_bytes(prism_dtype dt, const prism_layer_norm_desc* d, size_t* out_bytes) {
+  return guarded([&]() -> int {
+    if (!out_bytes) return refuse("null pointer");
+    const int rc = check(d, (int)dt);
+    if (rc == PRISM_OK) *out_bytes = layer_norm_backward_bytes(*d, (int)dt) + 256;
+    return rc;
+  });
+}
+
+int prism_token_logprob(const void* logits, const void* tokens, float* logp, float* lse, prism_dtype dt, const prism_logits_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    const int rc = check(d, (int)dt, false);
+    if (rc != PRISM_OK || d->rows == 0) return rc;
+    if (!logits || !tokens) return refuse("null pointer");
+    if (!aligned_to(logits, size_of(dt)) || !aligned_to(tokens, d->wide_tokens ? 8 : 4) || !aligned_to(logp, 4) || !aligned_to(lse, 4))
+      return refuse("a pointer is not aligned to the element size");
+    launch_logprob(logits, tokens, logp, lse, (int)dt, *d, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_token_logprob_backward(const float* dlogp, const void* logits, const void* tokens, const float* lse, void* dlogits, prism_dtype dt,
+                                 const prism_logits_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    const int rc = check(d, (int)dt, false);
+    if (rc != PRISM_OK || d->rows == 0) return rc;
+    if (!dlogp || !logits || !tokens || !lse || !dlogits) return refuse("null pointer");
+    if (overlap(d->rows, d->vocabulary, d->dlogits_stride)) return refuse(OVERLAP);
+    if (!aligned_to(logits, size_of(dt)) || !aligned_to(dlogits, size_of(dt)) || !aligned_to(tokens, d->wide_tokens ? 8 : 4) || !aligned_to(dlogp, 4) || !aligned_to(lse, 4))
+      return refuse("a pointer is not aligned to the element size");
+    launch_logprob_backward(dlogp, logits, tokens, lse, dlogits, (int)dt, *d, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_policy_loss(const void* logits, const void* tokens, float* loss, float* logp, float* lse, float* dlogp, void* dlogits, prism_dtype dt,
+                      const prism_logits_desc* d, void* stream) {
+  return guarded([&]() -> int {
+    int rc = check(d, (int)dt, true);
+    if (rc != PRISM_OK) return rc;
+    if (!loss || (d->rows && (!logits || !tokens))) return refuse("null pointer");
+    if (dlogits && overlap(d->rows, d->vocabulary, d->dlogits_stride)) return refuse(OVERLAP);
+    if (!aligned_to(logits, size_of(dt)) || !aligned_to(dlogits, size_of(dt)) || !aligned_to(tokens, d->wide_tokens ? 8 : 4)) return refuse("a pointer is not aligned to the element size");
+    for (const void* p : {(const void*)loss, (const void*)logp, (const void*)lse, (const void*)dlogp, (const void*)d->advantages, (const void*)d->old_logp,
+                          (const void*)d->ref_logp, (const void*)d->weights})
+      if (!aligned_to(p, 4)) return refuse("a pointer is not aligned to the element size");
+    char* ws = nullptr;
+    rc = layer_workspace(policy_loss_bytes(*d), d->workspace, d->workspace_bytes, (hipStream_t)stream, &ws);
+    if (rc != PRISM_OK) return rc;
+    launch_policy_loss(logits, tokens, loss, logp, lse, dlogp, dlogits, (int)dt, *d, ws, (hipStream_t)stream);
+    return launched();
+  });
+}
+
+int prism_policy_loss_workspace_bytes(const prism_logits_desc* d, size_t* out_bytes) {
+  return guarded([&]() -> int {
+    if (!out_bytes) return refuse("null pointer");
+    const int rc = check(d, PRISM_F32, true);
+    if (rc == PRISM_OK) *out_bytes = policy_loss_bytes(*d);
     return rc;
   });
 }

@@ -1,0 +1,289 @@
+// What is computed from rows of logits and one token of each: its log-probability, losses of it, and the logits' gradients.
+//
+//   logp = s z_t - lse, lse = log sum_j exp(s z_j);   dz_j = s d ([j = t] - exp(s z_j - lse)), d = the derivative of the loss by logp
+//   loss = sum w l,  l = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(f) - f - 1),  r = exp(logp - old), f = ref - logp;  without old l = -A logp + ...
+//   dl / dlogp = -(r A where r A <= clip(r) A, else 0) + kl (1 - exp(f))
+//
+// A row is one workgroup's.  Its exponentials are taken in base 2 relative to a running maximum m (rounded c z, c = s log2 e: exp2(c z - m) is one fused product and one
+// instruction), every thread with its own, joined at the end.  Sums are in 32 bits a thread, what follows from the whole row in 64.
+#include "layer.h"
+#include "row_vector.h"
+
+namespace prism {
+namespace {
+
+struct Logits {
+  const void *z, *tokens;
+  void* dz;
+  float *logp, *lse, *dlogp;             // results (backward: lse and dlogp are given)
+  const float *advantages, *old, *ref, *weights;
+  double *losses, *mean;                 // weighted losses of the rows; one over the number of rows with a token, where weights are not given
+  long long rows, zs, ds;
+  int vocabulary;
+  float c, scale;
+  double low, high, kl;
+  double unit;                           // scale / c: what a power of two is worth, the rounding of c taken out
+  bool wide;
+};
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// sum_j 2^(c z_j) = s 2^m; no terms: m = -inf, s = 0
+struct Sum {
+  float m = -INFINITY, s = 0.0f;
+  __device__ float reference() const { return m == -INFINITY ? 0.0f : m; }
+  __device__ void raise(float to) {
+    if (to > m) {
+      s *= exp2_of(m - to);
+      m = to;
+    }
+  }
+  __device__ void join(float om, float os) {
+    const float to = fmaxf(m, om), by = to == -INFINITY ? 0.0f : to;
+    s = s * exp2_of(m - by) + os * exp2_of(om - by);
+    m = to;
+  }
+};
+
+template <typename T> __device__ inline void add(Sum& a, const typename Vec<T>::type& v, float c) {
+  constexpr int N = Vec<T>::N;
+  float top = (float)v[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) top = fmaxf(top, (float)v[e]);
+  a.raise(top * c);
+  const float m = a.reference();
+  float part[2] = {};
+#pragma unroll
+  for (int e = 0; e < N; ++e) part[e & 1] += exp2_of(fmaf((float)v[e], c, -m));
+  a.s += part[0] + part[1];
+}
+
+// The sum of the workgroup, in every thread
+template <int THREADS> __device__ inline Sum whole_row(Sum a, float2* memory) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) a.join(__shfl_xor(a.m, d), __shfl_xor(a.s, d));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) memory[threadIdx.x >> 6] = make_float2(a.m, a.s);
+  __syncthreads();
+  Sum b;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) b.join(memory[w].x, memory[w].y);
+  return b;
+}
+
+constexpr double LN2 = 0.69314718055994530942;
+
+__device__ inline int token_of(const Logits& p, long long row) {
+  const long long t = p.wide ? ((const long long*)p.tokens)[row] : (long long)((const int*)p.tokens)[row];
+  return t >= 0 && t < p.vocabulary ? (int)t : -1;
+}
+
+// What one thread computes of a row: its results, and the derivative of the loss by logp.  z: the logit of the token
+__device__ inline float finish_row(const Logits& p, long long row, const Sum& a, float z) {
+  const double log2s = log((double)a.s) * (1.0 / LN2);
+  const double lse = a.s > 0.0f ? (a.m + log2s) * p.unit : -INFINITY;
+  const double logp = z == -INFINITY ? -INFINITY : ((double)z * p.c - a.m - log2s) * p.unit;
+  if (p.logp) p.logp[row] = (float)logp;
+  if (p.lse) p.lse[row] = (float)lse;
+  if (!p.losses) return 0.0f;
+  const double w = p.weights ? (double)p.weights[row] : *p.mean;
+  double l = 0.0, d = 0.0;
+  if (w != 0.0) {
+    const double A = p.advantages ? (double)p.advantages[row] : 1.0;
+    if (p.old) {
+      const double r = exp(logp - p.old[row]), low = 1.0 - p.low, high = 1.0 + p.high, held = (r < low ? low : r > high ? high : r) * A, free = r * A;
+      if (free <= held) {
+        l = -free;
+        d = -free;
+      } else {
+        l = -held;
+      }
+    } else {
+      l = -A * logp;
+      d = -A;
+    }
+    if (p.kl != 0.0) {
+      const double f = p.ref[row] - logp, e = expm1(f);
+      l += p.kl * (e - f);
+      d -= p.kl * e;
+    }
+    l *= w;
+    d *= w;
+  }
+  p.losses[row] = l;
+  if (p.dlogp) p.dlogp[row] = (float)d;
+  return (float)d;
+}
+
+template <typename T> __device__ inline void clear_row(const Logits& p, long long row, int threads) {
+  T* dz = (T*)p.dz + row * p.ds;
+  for (int at = threadIdx.x * Vec<T>::N; at < p.vocabulary; at += threads * Vec<T>::N) store_vector(dz, at, p.vocabulary, typename Vec<T>::type{});
+}
+
+// A vector of the gradient: [j = t] d - exp2(c z - m) factor
+template <typename T> __device__ inline typename Vec<T>::type gradient(const typename Vec<T>::type& v, int at, int t, float c, float m, float d, float factor) {
+  typename Vec<T>::type o;
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e) {
+    const float g = -exp2_of(fmaf((float)v[e], c, -m)) * factor;
+    o[e] = (T)(at + e == t ? d + g : g);
+  }
+  return o;
+}
+
+template <typename T, int THREADS, bool GRAD>
+__global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
+  constexpr int N = Vec<T>::N;
+  __shared__ float2 memory[THREADS / 64];
+  __shared__ float result;
+  for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const int t = token_of(p, row);
+    if (t < 0) {
+      if (threadIdx.x == 0) {
+        if (p.logp) p.logp[row] = 0.0f;
+        if (p.lse) p.lse[row] = 0.0f;
+        if (p.dlogp) p.dlogp[row] = 0.0f;
+        if (p.losses) p.losses[row] = 0.0;
+      }
+      if constexpr (GRAD) clear_row<T>(p, row, THREADS);
+      continue;
+    }
+    const T* z = (const T*)p.z + row * p.zs;
+    const float zt = (float)z[t];
+    Sum a;
+#pragma unroll 4
+    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, load_vector(z, at, p.vocabulary, -INFINITY), p.c);
+    a = whole_row<THREADS>(a, memory);
+    if (threadIdx.x == 0) result = finish_row(p, row, a, zt);
+    if constexpr (GRAD) {
+      __syncthreads();
+      const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
+      T* dz = (T*)p.dz + row * p.ds;
+#pragma unroll 4
+      for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
+        store_vector(dz, at, p.vocabulary, gradient<T>(load_vector(z, at, p.vocabulary, -INFINITY), at, t, p.c, m, d, factor));
+      __syncthreads();
+    }
+  }
+}
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) logprob_backward_kernel(Logits p) {
+  constexpr int N = Vec<T>::N;
+  for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const int t = token_of(p, row);
+    if (t < 0) {
+      clear_row<T>(p, row, THREADS);
+      continue;
+    }
+    const T* z = (const T*)p.z + row * p.zs;
+    T* dz = (T*)p.dz + row * p.ds;
+    // the reference is lse in base 2, rounded; the factor makes up for its rounding
+    const float d = p.dlogp[row] * p.scale, lse = p.lse[row];
+    const double exact = (double)lse / p.unit;
+    const float m = lse == -INFINITY ? 0.0f : (float)exact;
+    const float factor = lse == -INFINITY ? 0.0f : d * exp2_of((float)(m - exact));
+#pragma unroll 4
+    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
+      store_vector(dz, at, p.vocabulary, gradient<T>(load_vector(z, at, p.vocabulary, -INFINITY), at, t, p.c, m, d, factor));
+  }
+}
+
+__device__ inline double block_sum(double v, double* memory) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) memory[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v += memory[w];
+  return v;
+}
+
+// One over the number of rows with a token
+__global__ void __launch_bounds__(1024) count_rows_kernel(Logits p) {
+  __shared__ double memory[16];
+  double n = 0.0;
+  for (long long row = threadIdx.x; row < p.rows; row += 1024) n += token_of(p, row) >= 0 ? 1.0 : 0.0;
+  n = block_sum(n, memory);
+  if (threadIdx.x == 0) *p.mean = n > 0.0 ? 1.0 / n : 0.0;
+}
+
+__global__ void __launch_bounds__(1024) loss_sum_kernel(Logits p, float* loss) {
+  __shared__ double memory[16];
+  double v = 0.0;
+  for (long long row = threadIdx.x; row < p.rows; row += 1024) v += p.losses[row];
+  v = block_sum(v, memory);
+  if (threadIdx.x == 0) *loss = (float)v;
+}
+
+constexpr long long MOST_BLOCKS = 1 << 20;
+
+Logits common(const void* z, const void* tokens, const prism_logits_desc& d) {
+  Logits p = {};
+  p.z = z; p.tokens = tokens;
+  p.rows = d.rows; p.zs = d.logits_stride; p.ds = d.dlogits_stride; p.vocabulary = d.vocabulary; p.wide = d.wide_tokens;
+  p.scale = (float)d.scale; p.c = (float)(d.scale / LN2); p.unit = d.scale / p.c;
+  return p;
+}
+
+int threads_of(int vocabulary, int dt) {
+  const int vectors = (vocabulary + 7) / 8;
+  return vectors <= 512 ? 64 : vectors <= 2048 ? 256 : 512;
+}
+
+template <typename T, int THREADS> void launch(const Logits& p, bool back, hipStream_t s) {
+  void (*kernel)(Logits) = back ? logprob_backward_kernel<T, THREADS> : p.dz ? logits_kernel<T, THREADS, true> : logits_kernel<T, THREADS, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.rows < MOST_BLOCKS ? p.rows : MOST_BLOCKS)), dim3(THREADS), 0, s, p);
+}
+template <typename T> void by_threads(const Logits& p, int threads, bool back, hipStream_t s) {
+  if (threads == 64) launch<T, 64>(p, back, s);
+  else if (threads == 256) launch<T, 256>(p, back, s);
+  else launch<T, 512>(p, back, s);
+}
+void by_type(const Logits& p, int dt, bool back, hipStream_t s) {
+  if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary, dt), back, s);
+  else by_threads<__bf16>(p, threads_of(p.vocabulary, dt), back, s);
+}
+
+}  // namespace
+
+int launch_logprob(const void* z, const void* tokens, float* logp, float* lse, int dt, const prism_logits_desc& d, hipStream_t s) {
+  ProfScope prof(PK_LOGPROB, s);
+  Logits p = common(z, tokens, d);
+  p.logp = logp; p.lse = lse;
+  by_type(p, dt, false, s);
+  return PRISM_OK;
+}
+
+int launch_logprob_backward(const float* dlogp, const void* z, const void* tokens, const float* lse, void* dz, int dt, const prism_logits_desc& d, hipStream_t s) {
+  ProfScope prof(PK_LOGPROB_BACKWARD, s);
+  Logits p = common(z, tokens, d);
+  p.dlogp = (float*)dlogp; p.lse = (float*)lse; p.dz = dz;
+  by_type(p, dt, true, s);
+  return PRISM_OK;
+}
+
+size_t policy_loss_bytes(const prism_logits_desc& d) { return (size_t)(d.rows + 1) * sizeof(double); }
+
+int launch_policy_loss(const void* z, const void* tokens, float* loss, float* logp, float* lse, float* dlogp, void* dz, int dt, const prism_logits_desc& d, char* ws,
+                       hipStream_t s) {
+  Logits p = common(z, tokens, d);
+  p.logp = logp; p.lse = lse; p.dlogp = dlogp; p.dz = dz;
+  p.advantages = d.advantages; p.old = d.old_logp; p.ref = d.ref_logp; p.weights = d.weights;
+  p.low = d.clip_low; p.high = d.clip_high; p.kl = d.kl;
+  p.mean = (double*)ws; p.losses = p.mean + 1;
+  {
+    ProfScope prof(PK_LOSS_SUM, s);
+    if (!p.weights) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, p);
+  }
+  if (p.rows) {
+    ProfScope prof(PK_POLICY_LOSS, s);
+    by_type(p, dt, false, s);
+  }
+  ProfScope prof(PK_LOSS_SUM, s);
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, s, p, loss);
+  return PRISM_OK;
+}
+
+}  // namespace prism

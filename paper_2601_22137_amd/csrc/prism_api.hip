@@ -1788,7 +1788,7 @@ int prism_profile_enable(int on) {
 }
 
 int prism_profile_collect(double* ms_by_kind, long long* launches_by_kind, int nkinds) {
-  if (!ms_by_kind || !launches_by_kind || (nkinds < PK_COUNT && nkinds != PK_FIT_SQUARE && nkinds != PK_DROPOUT)) return PRISM_EINVAL;   // (these: see prism.h)
+  if (!ms_by_kind || !launches_by_kind || (nkinds < PK_COUNT && nkinds != PK_FIT_SQUARE && nkinds != PK_DROPOUT && nkinds != PK_EMBEDDING)) return PRISM_EINVAL;   // (these: see prism.h)
   std::lock_guard<std::mutex> lock(g_prof_mu);
   for (int i = 0; i < nkinds; ++i) { ms_by_kind[i] = 0.0; launches_by_kind[i] = 0; }
   for (auto& r : g_prof) {

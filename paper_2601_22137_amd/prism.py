@@ -3,6 +3,7 @@ step of the path runs in the HIP kernels.  PyTorch supplies device memory and th
 
 The library must have been built (python -m paper_2601_22137_amd.build); there is no fallback.
 """
+import collections
 import ctypes
 import os
 import struct
@@ -30,6 +31,9 @@ EXPORTS = ("prism_workspace_bytes", "prism_release_workspaces", "prism_polar", "
            "prism_inv_root", "prism_inv_root_ex", "prism_sign", "prism_sign_ex", "prism_inverse", "prism_inverse_ex", "prism_sqrt_newton", "prism_sqrt_newton_ex", "prism_spd_inverse", "prism_run_grouped", "prism_run_grouped_from",
            "prism_dropout", "prism_qk_norm_rope", "prism_qk_norm_rope_backward", "prism_norm_rope_workspace_bytes",
            "prism_attention", "prism_attention_backward", "prism_attention_workspace_bytes",
+           "prism_embedding", "prism_embedding_backward", "prism_embedding_workspace_bytes",
+           "prism_layer_norm", "prism_layer_norm_backward", "prism_layer_norm_workspace_bytes",
+           "prism_token_logprob", "prism_token_logprob_backward", "prism_policy_loss", "prism_policy_loss_workspace_bytes",
            "prism_sketch", "prism_gauss_parts", "prism_chain_product", "prism_chain_product_bf16", "prism_gemm_f32", "prism_gemm_f32_planes",
            "prism_gemm_f64a", "prism_gemm_bf16_nt", "prism_profile_enable", "prism_profile_collect",
            "prism_last_error")
@@ -37,7 +41,8 @@ EXPORTS = ("prism_workspace_bytes", "prism_release_workspaces", "prism_polar", "
 PROFILE_KINDS = ("prep", "final", "sketch", "chain", "solve", "f32_resid", "f32_polyq", "f32_apply", "f32_store",
                  "f64_mnext", "make_t", "bf16_gram", "bf16_polyq", "bf16_apply", "bf16_store", "spd_inverse", "db_moments",
                  "db_update_m", "f32_small_polar", "moments", "fit_square", "flow", "small_root",
-                 "dropout", "norm_rope", "norm_rope_backward", "attention", "attention_join", "attention_docs", "attention_dq", "attention_dkv")
+                 "dropout", "norm_rope", "norm_rope_backward", "attention", "attention_join", "attention_docs", "attention_dq", "attention_dkv",
+                 "embedding", "embedding_sort", "embedding_backward", "layer_norm", "layer_norm_backward", "logprob", "logprob_backward", "policy_loss", "loss_sum")
 
 
 class Options(ctypes.Structure):
@@ -69,6 +74,24 @@ class AttentionDesc(ctypes.Structure):
                 + [(f, ctypes.c_void_p) for f in ("slopes", "prefix", "k_lens", "q_doc", "k_doc")]
                 + [(f, Strides) for f in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
                 + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
+
+
+class EmbeddingDesc(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("wide_tokens", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("table_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class LayerNormDesc(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("center", ctypes.c_int32), ("eps", ctypes.c_float)]
+                + [(f, ctypes.c_int64) for f in ("x", "residual", "total", "y", "dy", "dtotal", "dx")]
+                + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
+
+
+class LogitsDesc(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_int64), ("vocabulary", ctypes.c_int32), ("wide_tokens", ctypes.c_int32), ("scale", ctypes.c_double),
+                 ("logits_stride", ctypes.c_int64), ("dlogits_stride", ctypes.c_int64)]
+                + [(f, ctypes.c_double) for f in ("clip_low", "clip_high", "kl")]
+                + [(f, ctypes.c_void_p) for f in ("advantages", "old_logp", "ref_logp", "weights", "workspace")] + [("workspace_bytes", ctypes.c_size_t)])
 
 
 class PrismError(RuntimeError):
@@ -110,6 +133,15 @@ def lib():
         L.prism_attention.argtypes = [vp] * 5 + [i, vp, vp]
         L.prism_attention_backward.argtypes = [vp] * 9 + [i, vp, vp]
         L.prism_attention_workspace_bytes.argtypes = [i, vp, i, ctypes.POINTER(ctypes.c_size_t)]
+        size_p = ctypes.POINTER(ctypes.c_size_t)
+        L.prism_embedding.argtypes = L.prism_embedding_backward.argtypes = [vp, vp, vp, i, vp, vp]
+        L.prism_embedding_workspace_bytes.argtypes = L.prism_layer_norm_workspace_bytes.argtypes = [i, vp, size_p]
+        L.prism_layer_norm.argtypes = [vp] * 7 + [i, vp, vp]
+        L.prism_layer_norm_backward.argtypes = [vp] * 8 + [i, vp, vp]
+        L.prism_token_logprob.argtypes = [vp] * 4 + [i, vp, vp]
+        L.prism_token_logprob_backward.argtypes = [vp] * 5 + [i, vp, vp]
+        L.prism_policy_loss.argtypes = [vp] * 7 + [i, vp, vp]
+        L.prism_policy_loss_workspace_bytes.argtypes = [vp, size_p]
         L.prism_sketch.argtypes = [vp, i, i, u64, i, i, vp]
         L.prism_gauss_parts.argtypes = [ctypes.c_uint32, ctypes.c_uint32, vp, vp, vp, vp]
         L.prism_chain_product.argtypes = [vp, vp, vp, i, i, i, vp]
@@ -521,6 +553,178 @@ def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, softca
     _on(dev, lib().prism_attention_backward, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
         dv.data_ptr(), _dtype_code(q), desc)
     return dq, dk, dv
+
+
+# ---- operators at the ends of a model ----
+#
+# Arrays of rows are tensors [..., width] whose rows follow each other at one stride, their entries next to each other; tokens are contiguous int64 or int32 tensors.  Scratch
+# memory comes from PyTorch's allocator, for the stream (and graph) of the call.
+
+_EMBEDDING = struct.Struct("@2q2if2qPN")
+_LAYER_NORM = struct.Struct("@q2if7qPN")
+_LOGITS = struct.Struct("@q2id2q3d5PN")
+
+
+def _rows(t, name, dtype, dev, shape):
+    """The stride between the rows of an array of rows."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise PrismError("%s: expected shape %s, and the dtype and device of the other arrays" % (name, tuple(shape)))
+    if t.is_contiguous():
+        return shape[-1]
+    if t.dim() == 2 and t.stride(1) == 1:
+        return t.stride(0)
+    try:
+        flat = t.view(-1, shape[-1])
+    except RuntimeError:
+        flat = None
+    if flat is None or (flat.stride(1) != 1 and shape[-1] > 1):
+        raise PrismError("%s: expected rows at one stride, their entries next to each other" % name)
+    return flat.stride(0)
+
+
+def _tokens(t, dev, shape=None):
+    """Whether they are int64."""
+    if t.dtype is not torch.int64 and t.dtype is not torch.int32:
+        raise PrismError("tokens: expected int64 or int32")
+    if t.get_device() != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise PrismError("tokens: expected a contiguous tensor%s on the device of the others" % ("" if shape is None else " of shape %s" % (tuple(shape),)))
+    return 1 if t.dtype is torch.int64 else 0
+
+
+def _pack(layout, *fields):
+    try:
+        return layout.pack(*fields)
+    except _NO_NUMBER as e:
+        raise PrismError("a number is out of range: %s" % e) from None
+
+
+def _scratch(query, dev, workspace, layout, fields):
+    """(the packed description, the tensor of its workspace).  query: the library's size for a description."""
+    if workspace is None:
+        n = ctypes.c_size_t(0)
+        _check(query(_pack(layout, *fields, 0, 0), ctypes.byref(n)))
+        workspace = torch.empty(n.value, dtype=torch.uint8, device="cuda:%d" % dev)
+    return _pack(layout, *fields, *_given(workspace, dev)), workspace
+
+
+def embedding(tokens, table, scale=1.0, out=None):
+    """scale * table[tokens], [..., width]; a token that is no row of the table [rows, width] (padding) gives zeros."""
+    dev = _device(table)
+    if table.dim() != 2:
+        raise PrismError("table: expected [rows, width]")
+    wide, (rows, width) = _tokens(tokens, dev), table.shape
+    shape = tokens.shape + (width,)
+    y = table.new_empty(shape) if out is None else out
+    desc = _pack(_EMBEDDING, tokens.numel(), rows, width, wide, scale, _rows(table, "table", table.dtype, dev, table.shape), _rows(y, "out", table.dtype, dev, shape), 0, 0)
+    _on(dev, lib().prism_embedding, table.data_ptr(), tokens.data_ptr(), y.data_ptr(), _dtype_code(table), desc)
+    return y
+
+
+def embedding_backward(dout, tokens, rows, scale=1.0, out=None, workspace=None):
+    """The gradient of embedding() with respect to its table, [rows, width], whole: rows that no token names are zeros."""
+    dev, width, dtype = _device(dout), dout.shape[-1] if dout.dim() else 0, dout.dtype
+    if dout.dim() < 1 or rows < 0:
+        raise PrismError("expected dout [..., width] and a table's rows")
+    d = dout.new_empty((rows, width)) if out is None else out
+    fields = (tokens.numel(), rows, width, _tokens(tokens, dev, dout.shape[:-1]), scale, _rows(d, "out", dtype, dev, torch.Size((rows, width))),
+              _rows(dout, "dout", dtype, dev, dout.shape))
+    code = _dtype_code(dout)
+    desc, workspace = _scratch(lambda *a: lib().prism_embedding_workspace_bytes(code, *a), dev, workspace, _EMBEDDING, fields)
+    _on(dev, lib().prism_embedding_backward, dout.data_ptr(), tokens.data_ptr(), d.data_ptr(), code, desc)
+    return d
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, center=True, eps=1e-5, out=None):
+    """(y, total, stats): total = x + residual (x itself without one), y its rows [..., width] less their mean (center=False: as they are) over the root of their mean square
+    and eps, times weight, plus bias (fp32 [width]); stats [rows, 2] for the gradients.  out: the tensors for y and total (None without a residual)."""
+    dev, dtype, shape = _device(x), x.dtype, x.shape
+    if x.dim() < 1:
+        raise PrismError("expected [..., width]")
+    width = shape[-1]
+    y, total = (x.new_empty(shape), None if residual is None else x.new_empty(shape)) if out is None else out
+    if (total is None) != (residual is None):
+        raise PrismError("total: goes with residual")
+    rows = x.numel() // width if width else 0
+    stats = x.new_empty((rows, 2), dtype=torch.float32)
+    w, b = _plain(weight, "weight", torch.float32, dev, (width,)), _plain(bias, "bias", torch.float32, dev, (width,))
+    sx, sy = _rows(x, "x", dtype, dev, shape), _rows(y, "out", dtype, dev, shape)
+    sr, st = (0, 0) if residual is None else (_rows(residual, "residual", dtype, dev, shape), _rows(total, "total", dtype, dev, shape))
+    desc = _pack(_LAYER_NORM, rows, width, 1 if center else 0, eps, sx, sr, st, sy, 0, 0, 0, 0, 0)
+    _on(dev, lib().prism_layer_norm, x.data_ptr(), _ptr(residual), w, b, y.data_ptr(), _ptr(total), stats.data_ptr(), _dtype_code(x), desc)
+    return y, x if total is None else total, stats
+
+
+def layer_norm_backward(dy, total, stats, weight=None, dtotal=None, center=True, bias=True, out=None, workspace=None):
+    """(dx, dweight, dbias) of layer_norm() from the gradient of y and, where not None, of total; total and stats as it returned them.  dx is the gradient of x and of the
+    residual; dbias is None where bias is False."""
+    dev, dtype, shape = _device(total), total.dtype, total.shape
+    if total.dim() < 1:
+        raise PrismError("expected [..., width]")
+    width = shape[-1]
+    dx = total.new_empty(shape) if out is None else out
+    rows = total.numel() // width if width else 0
+    dw = total.new_empty((width,), dtype=torch.float32)
+    db = total.new_empty((width,), dtype=torch.float32) if bias else None
+    w, at = _plain(weight, "weight", torch.float32, dev, (width,)), _plain(stats, "stats", torch.float32, dev, (rows, 2))
+    fields = (rows, width, 1 if center else 0, 0.0, 0, 0, _rows(total, "total", dtype, dev, shape), 0, _rows(dy, "dy", dtype, dev, shape),
+              0 if dtotal is None else _rows(dtotal, "dtotal", dtype, dev, shape), _rows(dx, "out", dtype, dev, shape))
+    code = _dtype_code(total)
+    desc, workspace = _scratch(lambda *a: lib().prism_layer_norm_workspace_bytes(code, *a), dev, workspace, _LAYER_NORM, fields)
+    _on(dev, lib().prism_layer_norm_backward, dy.data_ptr(), total.data_ptr(), at, w, _ptr(dtotal), dx.data_ptr(), dw.data_ptr(), _ptr(db), code, desc)
+    return dx, dw, db
+
+
+def _logits(logits, tokens, scale, out, more=(0.0, 0.0, 0.0, 0, 0, 0, 0)):
+    """(device, dtype code, the description's fields before the workspace)."""
+    dev = _device(logits)
+    if logits.dim() < 1:
+        raise PrismError("expected logits [..., vocabulary]")
+    shape = logits.shape
+    return dev, _dtype_code(logits), (tokens.numel(), shape[-1], _tokens(tokens, dev, shape[:-1]), scale, _rows(logits, "logits", logits.dtype, dev, shape),
+                                      0 if out is None else _rows(out, "out", logits.dtype, dev, shape)) + more
+
+
+def token_logprob(logits, tokens, scale=1.0):
+    """(logp, lse), fp32 in the shape of tokens: the logarithm of the softmax of scale * logits [..., vocabulary] at each row's token, and of the sum of its exponentials.  A token
+    outside the vocabulary (padding) gives 0 in both."""
+    dev, code, fields = _logits(logits, tokens, scale, None)
+    logp, lse = logits.new_empty(tokens.shape, dtype=torch.float32), logits.new_empty(tokens.shape, dtype=torch.float32)
+    _on(dev, lib().prism_token_logprob, logits.data_ptr(), tokens.data_ptr(), logp.data_ptr(), lse.data_ptr(), code, _pack(_LOGITS, *fields, 0, 0))
+    return logp, lse
+
+
+def token_logprob_backward(dlogp, logits, tokens, lse, scale=1.0, out=None):
+    """The gradient with respect to the logits from that of logp; lse as token_logprob() (or policy_loss()) returned it.  out may be logits."""
+    d = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+    dev, code, fields = _logits(logits, tokens, scale, d)
+    given = [_plain(t, n, torch.float32, dev, tokens.shape) for t, n in ((dlogp, "dlogp"), (lse, "lse"))]
+    _on(dev, lib().prism_token_logprob_backward, given[0], logits.data_ptr(), tokens.data_ptr(), given[1], d.data_ptr(), code, _pack(_LOGITS, *fields, 0, 0))
+    return d
+
+
+PolicyLoss = collections.namedtuple("PolicyLoss", "loss logp lse dlogp dlogits")
+
+
+def policy_loss(logits, tokens, advantages=None, old_logp=None, ref_logp=None, weights=None, clip=(0.2, 0.2), kl=0.0, scale=1.0, gradient=True, out=None, workspace=None):
+    """The loss of a policy on the tokens it took, and its gradient, in one pass over the logits [..., vocabulary]:
+    the sum over rows of weight * (-min(r A, clip(r) A) + kl (exp(f) - f - 1)), r = exp(logp - old_logp) held between 1 - clip[0] and 1 + clip[1], f = ref_logp - logp.
+    Without old_logp -A logp takes the first part's place; without advantages A = 1 (with neither: cross entropy); weights None: the mean over the rows that have a token.
+    Everything given for a row is fp32 in the shape of tokens; a token outside the vocabulary (padding) is left out.
+    Returns (loss, logp, lse, dlogp, dlogits): dlogp the gradient with respect to logp, dlogits None with gradient=False; out: the tensor for dlogits (logits itself is allowed)."""
+    if gradient:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+    elif out is not None:
+        raise PrismError("out: goes with gradient")
+    low, high = clip
+    rows = tokens.shape
+    dev = _device(logits)
+    dev, code, fields = _logits(logits, tokens, scale, out, (low, high, kl) + tuple(
+        _plain(t, n, torch.float32, dev, rows) for t, n in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights"))))
+    loss = logits.new_empty((), dtype=torch.float32)
+    logp, lse, dlogp = (logits.new_empty(rows, dtype=torch.float32) for _ in range(3))
+    desc, workspace = _scratch(lib().prism_policy_loss_workspace_bytes, dev, workspace, _LOGITS, fields)
+    _on(dev, lib().prism_policy_loss, logits.data_ptr(), tokens.data_ptr(), loss.data_ptr(), logp.data_ptr(), lse.data_ptr(), dlogp.data_ptr(), _ptr(out), code, desc)
+    return PolicyLoss(loss, logp, lse, dlogp, out)
 
 
 # ---- single steps (unit tests, profiling) ----
