@@ -14,12 +14,24 @@
 namespace prism {
 namespace {
 
-constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, MAX_RANGE = 512;
+constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, MAX_RANGE = 512, LIST = 512, AHEAD = 8, SUM_AHEAD = 8;
 
-// Token i; -1: no row of the table
-template <typename I> __device__ inline int token_at(const void* tokens, long long i, long long rows) {
+// Token i as an unsigned number; what is no row of a table is 2^31 or more, or past its rows
+template <typename I> __device__ inline unsigned token_at(const void* tokens, long long i) {
   const I t = ((const I*)tokens)[i];
-  return t >= 0 && (long long)t < rows ? (int)t : -1;
+  return sizeof(I) == 8 && (unsigned long long)t >> 32 ? 0xFFFFFFFFu : (unsigned)t;
+}
+
+// Where lane vector c of a row begins.  The last one ends with the row and may repeat entries of the one before (the same values are then stored twice), so that every
+// vector is whole; WHOLE: the row has a vector's entries at least.
+template <typename T, bool WHOLE> __device__ inline int column(int c, int width) { return WHOLE && c > width - Vec<T>::N ? width - Vec<T>::N : c; }
+template <typename T, bool WHOLE> __device__ inline typename Vec<T>::type load_piece(const T* row, int c, int width) {
+  if constexpr (WHOLE) return *(const typename Vec<T>::type*)(row + c);
+  else return load_vector(row, c, width);
+}
+template <typename T, bool WHOLE> __device__ inline void store_piece(T* row, int c, int width, const typename Vec<T>::type& v) {
+  if constexpr (WHOLE) *(typename Vec<T>::type*)(row + c) = v;
+  else store_vector(row, c, width, v);
 }
 
 struct Lookup {
@@ -30,23 +42,27 @@ struct Lookup {
   float scale;
 };
 
-template <typename T, typename I> __global__ void __launch_bounds__(256) embedding_kernel(Lookup p) {
+template <typename T, typename I, bool WHOLE> __global__ void __launch_bounds__(256) embedding_kernel(Lookup p) {
   using V = typename Vec<T>::type;
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, NV = 4;
   const int lane = threadIdx.x & (p.lanes - 1), per = 256 / p.lanes;
   for (long long i = (long long)blockIdx.x * per + threadIdx.x / p.lanes; i < p.count; i += (long long)gridDim.x * per) {
-    const int t = token_at<I>(p.tokens, i, p.rows);
-    const T* row = (const T*)p.table + (t < 0 ? 0 : t) * p.ts;
+    const unsigned t = token_at<I>(p.tokens, i);
+    const bool there = t < p.rows;
+    const T* row = (const T*)p.table + (there ? t : 0) * p.ts;
     T* to = (T*)p.out + i * p.os;
-#pragma unroll 4
-    for (int c = lane * N; c < p.width; c += p.lanes * N) {
-      V v = {};
-      if (t >= 0) {
-        v = load_vector(row, c, p.width);
+    for (int first = 0; first < p.width; first += p.lanes * N * NV) {
+      V v[NV] = {};
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = (T)((float)v[e] * p.scale);
+      for (int j = 0; j < NV; ++j)
+        if (first + j * p.lanes * N < p.width && there) v[j] = load_piece<T, WHOLE>(row, column<T, WHOLE>(first + (j * p.lanes + lane) * N, p.width), p.width);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (first + j * p.lanes * N >= p.width) break;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[j][e] = there ? (T)((float)v[j][e] * p.scale) : (T)0.0f;
+        store_piece<T, WHOLE>(to, column<T, WHOLE>(first + (j * p.lanes + lane) * N, p.width), p.width, v[j]);
       }
-      store_vector(to, c, p.width, v);
     }
   }
 }
@@ -55,33 +71,53 @@ struct Sorted {
   const void* tokens;
   int* starts;                  // [rows + 1]: where a row's tokens begin
   int2* sorted;                 // (token, index), by token and then index
-  int count, range;
+  int count;
+  unsigned range;
   long long rows;
 };
 
 template <typename I> __global__ void __launch_bounds__(SORT_THREADS) embedding_sort_kernel(Sorted p) {
   __shared__ int places[MAX_RANGE * SORT_WAVES];        // [row of the range][wave]: counts, then where the wave's next one goes
+  __shared__ int2 lists[SORT_WAVES][LIST];              // the range's tokens among a wave's: (row of the range, index), in their order
   __shared__ int sums[SORT_WAVES];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long first = (long long)blockIdx.x * p.range;
-  const int range = (int)(p.rows - first < p.range ? p.rows - first : p.range), slots = range * SORT_WAVES;
+  const unsigned rows = (unsigned)p.rows, first = blockIdx.x * p.range, range = rows - first < p.range ? rows - first : p.range;
+  const int slots = range * SORT_WAVES;
   for (int i = threadIdx.x; i < slots; i += SORT_THREADS) places[i] = 0;
   __syncthreads();
   // a wave has a part of the tokens, in whole sixty-fours
   const int part = ((p.count + SORT_THREADS - 1) / SORT_THREADS) * 64;
   const int begin = (int)((long long)wave * part < p.count ? wave * part : p.count), end = p.count - begin < part ? p.count : begin + part;
-  int below = 0;
-#pragma unroll 8
-  for (int i = begin + lane; i < end; i += 64) {
-    const int t = token_at<I>(p.tokens, i, p.rows);
-    if (t < 0) continue;
-    const long long at = t - first;
-    if (at < 0) ++below;
-    else if (at < range) atomicAdd(&places[(int)at * SORT_WAVES + wave], 1);
+  auto load = [&](int i0, unsigned (&t)[AHEAD]) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int i = i0 + 64 * j + lane;
+      t[j] = token_at<I>(p.tokens, i < end ? i : end - 1);
+    }
+    if (i0 + 64 * AHEAD <= end) return;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (i0 + 64 * j + lane >= end) t[j] = 0xFFFFFFFFu;
+  };
+  int below = 0, listed = 0;                            // of the wave; listed: all of them, also those for which the list has no room
+  for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
+    unsigned t[AHEAD];
+    load(i0, t);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const unsigned at = t[j] - first;
+      below += __popcll(__ballot(t[j] < first));
+      const unsigned long long some = __ballot(at < range);
+      if (!some) continue;
+      if (at < range) {
+        atomicAdd(&places[at * SORT_WAVES + wave], 1);
+        const int place = listed + __popcll(some & ((1ull << lane) - 1));
+        if (place < LIST) lists[wave][place] = make_int2(at, i0 + 64 * j + lane);
+      }
+      listed += __popcll(some);
+    }
   }
   // all tokens before the range
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) below += __shfl_xor(below, d);
   if (lane == 0) sums[wave] = below;
   __syncthreads();
   int base = 0;
@@ -116,22 +152,36 @@ template <typename I> __global__ void __launch_bounds__(SORT_THREADS) embedding_
     }
     before += mine[j];
   }
-  if (threadIdx.x == SORT_THREADS - 1 && first + range == p.rows) p.starts[p.rows] = before;
+  if (threadIdx.x == SORT_THREADS - 1 && first + range == rows) p.starts[rows] = before;
   __syncthreads();
-#pragma unroll 4
-  for (int i0 = begin; i0 < end; i0 += 64) {
-    const int i = i0 + lane, t = i < end ? token_at<I>(p.tokens, i, p.rows) : -1;
-    const long long at = t - first;
-    const bool in = t >= 0 && at >= 0 && at < range;
-    unsigned long long left = __ballot(in);
-    while (left) {              // one turn for each row that a token of these 64 names
-      const int leader = __ffsll((long long)left) - 1, row = __shfl((int)at, leader);
-      const unsigned long long same = __ballot(in && (int)at == row);
-      int place = 0;
-      if (lane == leader) place = atomicAdd(&places[row * SORT_WAVES + wave], __popcll(same));
-      place = __shfl(place, leader);
-      if ((same >> lane) & 1) p.sorted[place + __popcll(same & ((1ull << lane) - 1))] = make_int2(t, i);
-      left &= ~same;
+  // 64 tokens into their places: lanes of the same row find each other by its bits, the first of them takes their places together
+  const int bits = range > 1 ? 32 - __clz((int)range - 1) : 0;
+  auto place = [&](bool in, int at, int i) {
+    unsigned long long same = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+      const unsigned long long set = __ballot((at >> b) & 1);
+      same &= (at >> b) & 1 ? set : ~set;
+    }
+    const int before = __popcll(same & ((1ull << lane) - 1)), leader = in ? __ffsll((long long)same) - 1 : lane;
+    int to = 0;
+    if (in && before == 0) to = atomicAdd(&places[at * SORT_WAVES + wave], __popcll(same));
+    to = __shfl(to, leader) + before;
+    if (in) p.sorted[to] = make_int2((int)first + at, i);
+  };
+  if (listed <= LIST) {
+    for (int k = 0; k < listed; k += 64) {
+      const int2 e = k + lane < listed ? lists[wave][k + lane] : make_int2(0, 0);
+      place(k + lane < listed, e.x, e.y);
+    }
+  } else {
+    for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
+      unsigned t[AHEAD];
+      load(i0, t);
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const unsigned at = t[j] - first;
+        if (__ballot(at < range)) place(at < range, (int)at, i0 + 64 * j + lane);
+      }
     }
   }
 }
@@ -141,106 +191,151 @@ struct Sums {
   void* dtable;
   const int* starts;
   const int2* sorted;
-  float* part;                  // [tile][run that came in, run that goes on][width]
+  float* part;                  // [tile][run that came in, run that goes on][chunks x 64 vectors]
   long long rows, ds, ts;
-  int width, tile, tiles, chunks, tile_waves;
+  int width, tile, chunks, tile_waves, clear;   // clear: rows that a wave looks at together to clear those without tokens
   float scale;
 };
 
-template <typename T> __device__ inline void put(const Sums& p, int token, int c, const float (&sum)[Vec<T>::N]) {
+template <typename T, bool WHOLE> __device__ inline void put(const Sums& p, int token, int c, const float (&sum)[Vec<T>::N]) {
   typename Vec<T>::type o;
 #pragma unroll
   for (int e = 0; e < Vec<T>::N; ++e) o[e] = (T)(sum[e] * p.scale);
-  store_vector((T*)p.dtable + token * p.ts, c, p.width, o);
+  store_piece<T, WHOLE>((T*)p.dtable + token * p.ts, column<T, WHOLE>(c, p.width), p.width, o);
 }
 
-template <typename T> __global__ void __launch_bounds__(256) embedding_sums_kernel(Sums p) {
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <typename T> __device__ inline f32x4* part_of(const Sums& p, int tile, int which, int c) {
+  return (f32x4*)(p.part + ((size_t)tile * 2 + which) * (p.chunks * 64 * Vec<T>::N) + c);
+}
+template <typename T> __device__ inline void keep(const Sums& p, int tile, int which, int c, const float (&sum)[Vec<T>::N]) {
+  f32x4* to = part_of<T>(p, tile, which, c);
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; e += 4) to[e / 4] = f32x4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+}
+
+template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) embedding_sums_kernel(Sums p) {
   using V = typename Vec<T>::type;
-  constexpr int N = Vec<T>::N, AHEAD = 8;
-  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63, count = p.starts[p.rows];
+  constexpr int N = Vec<T>::N;
+  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
   if (wave >= p.tile_waves) {
-    const int others = gridDim.x * 4 - p.tile_waves;
-    for (long long row = wave - p.tile_waves; row < p.rows; row += others) {
-      if (p.starts[row] != p.starts[row + 1]) continue;
-      for (int c = lane * N; c < p.width; c += 64 * N) store_vector((T*)p.dtable + row * p.ts, c, p.width, V{});
+    // some neighbouring rows at a time, each lane looks at one
+    const long long stride = (long long)(gridDim.x * 4 - p.tile_waves) * p.clear;
+    for (long long first = (long long)(wave - p.tile_waves) * p.clear; first < p.rows; first += stride) {
+      const long long row = first + lane;
+      const bool empty = lane < p.clear && row < p.rows && p.starts[row] == p.starts[row + 1];
+      for (unsigned long long left = __ballot(empty); left; left &= left - 1) {
+        T* to = (T*)p.dtable + (first + __ffsll((long long)left) - 1) * p.ts;
+        for (int c = lane * N; c < p.width; c += 64 * N) store_piece<T, WHOLE>(to, column<T, WHOLE>(c, p.width), p.width, V{});
+      }
     }
     return;
   }
-  const int tile = wave / p.chunks, c = ((wave - tile * p.chunks) * 64 + lane) * N, begin = tile * p.tile;
+  const int count = p.starts[p.rows], tile = wave / p.chunks, c = ((wave - tile * p.chunks) * 64 + lane) * N, from = column<T, WHOLE>(c, p.width);
+  const long long begin = (long long)tile * p.tile;
   if (begin >= count) return;
-  const int end = count - begin < p.tile ? count : begin + p.tile;
-  int token = p.sorted[begin].x;
-  bool inside = begin == 0 || p.sorted[begin - 1].x != token;      // the run began in this tile
+  const long long end = count - begin < p.tile ? count : begin + p.tile;
+  const int last = begin ? p.sorted[begin - 1].x : -1, next = end < count ? p.sorted[end].x : -1;     // tokens before and behind the tile
+  int token = -1;
+  bool inside = false;                      // the run began in this tile
   float sum[N] = {};
-  for (int i0 = begin; i0 < end; i0 += AHEAD) {
-    V v[AHEAD];
-    int2 at[AHEAD];
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      at[j] = p.sorted[i0 + j < end ? i0 + j : end - 1];
-      v[j] = load_vector((const T*)p.dout + at[j].y * p.ds, c, i0 + j < end ? p.width : 0);
+  for (long long b = begin; b < end; b += 64) {
+    const int here = (int)(end - b < 64 ? end - b : 64);
+    const int2 mine = p.sorted[b + (lane < here ? lane : here - 1)];
+    if (b == begin) {
+      token = __builtin_amdgcn_readfirstlane(mine.x);
+      inside = token != last;
     }
+    for (int j0 = 0; j0 < here; j0 += SUM_AHEAD) {
+      V v[SUM_AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      if (i0 + j >= end) break;
-      if (at[j].x != token) {
-        if (inside) put<T>(p, token, c, sum);
-        else {
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (c + e < p.width) p.part[(size_t)tile * 2 * p.width + c + e] = sum[e];
-        }
-#pragma unroll
-        for (int e = 0; e < N; ++e) sum[e] = 0.0f;
-        token = at[j].x;
-        inside = true;
+      for (int j = 0; j < SUM_AHEAD; ++j) {
+        const int at = __builtin_amdgcn_readlane(mine.y, j0 + j < here ? j0 + j : here - 1);
+        v[j] = load_piece<T, WHOLE>((const T*)p.dout + at * p.ds, from, p.width);
       }
 #pragma unroll
-      for (int e = 0; e < N; ++e) sum[e] += (float)v[j][e];
+      for (int j = 0; j < SUM_AHEAD; ++j) {
+        if (j0 + j >= here) break;
+        const int t = __builtin_amdgcn_readlane(mine.x, j0 + j);
+        if (t != token) {
+          if (inside) put<T, WHOLE>(p, token, c, sum);
+          else keep<T>(p, tile, 0, c, sum);
+#pragma unroll
+          for (int e = 0; e < N; ++e) sum[e] = 0.0f;
+          token = t;
+          inside = true;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += (float)v[j][e];
+      }
     }
   }
-  const bool goes_on = end < count && p.sorted[end].x == token;
-  if (inside && !goes_on) {
-    put<T>(p, token, c, sum);
-    return;
-  }
-  float* part = p.part + ((size_t)tile * 2 + (inside ? 1 : 0)) * p.width;
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (c + e < p.width) part[c + e] = sum[e];
+  if (inside && next != token) put<T, WHOLE>(p, token, c, sum);
+  else keep<T>(p, tile, inside ? 1 : 0, c, sum);
 }
 
-// A workgroup for each border between tiles and 64 vectors: the first border of a run adds it up, each of its waves a share of the tiles
-template <typename T> __global__ void __launch_bounds__(512) embedding_join_kernel(Sums p) {
-  constexpr int N = Vec<T>::N;
-  const int tile = blockIdx.x / p.chunks, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, border = (tile + 1) * p.tile, count = p.starts[p.rows];
-  if (border >= count) return;
-  const int token = p.sorted[border].x;
-  if (p.sorted[border - 1].x != token) return;
-  const int start = p.starts[token], stop = p.starts[token + 1];
-  if (start < tile * p.tile) return;                               // an earlier border's
-  const int c = ((blockIdx.x - tile * p.chunks) * 64 + lane) * N, last = (stop - 1) / p.tile, all = last - tile + 1, share = (all + 7) / 8;
-  const int from = tile + wave * share, to = from + share <= last + 1 ? from + share : last + 1;
-  double sum[N] = {};
+// Partial sums of the runs that cross borders between tiles.  A workgroup has BORDERS of them and 64 vectors of 16 bytes; its waves find those that are the
+// first of a run, and take the runs in turn, long ones together.
+constexpr int BORDERS = 16, JOIN_WAVES = 8, LONG_RUN = 24;
+
+template <typename T> __device__ inline void add_parts(const Sums& p, int tile, int from, int to, int c, double (&sum)[Vec<T>::N]) {
 #pragma unroll 4
   for (int t = from; t < to; ++t) {
-    const float* part = p.part + ((size_t)t * 2 + (t == tile ? 1 : 0)) * p.width;
+    const f32x4* part = part_of<T>(p, t, t == tile ? 1 : 0, c);
+    f32x4 v[Vec<T>::N / 4];
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e] += c + e < p.width ? part[c + e] : 0.0f;
+    for (int e = 0; e < Vec<T>::N / 4; ++e) v[e] = part[e];
+#pragma unroll
+    for (int e = 0; e < Vec<T>::N; ++e) sum[e] += v[e / 4][e % 4];
   }
-  __shared__ double sums[8][64 * N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) sums[wave][e * 64 + lane] = sum[e];
+}
+
+template <typename T, bool WHOLE> __global__ void __launch_bounds__(64 * JOIN_WAVES) embedding_join_kernel(Sums p) {
+  constexpr int N = Vec<T>::N;
+  __shared__ double sums[JOIN_WAVES][64 * N];
+  __shared__ int2 runs[BORDERS];                                   // (token, end of its last tile), or -1
+  const int group = blockIdx.x / p.chunks, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, count = p.starts[p.rows];
+  const int c = ((blockIdx.x - group * p.chunks) * 64 + lane) * N;
+  if (threadIdx.x < BORDERS) {
+    const int tile = group * BORDERS + threadIdx.x;
+    const long long border = (long long)(tile + 1) * p.tile;
+    int2 run = make_int2(-1, 0);
+    if (border < count) {
+      const int token = p.sorted[border].x;
+      if (p.sorted[border - 1].x == token && p.starts[token] >= tile * p.tile) run = make_int2(token, (p.starts[token + 1] - 1) / p.tile + 1);
+    }
+    runs[threadIdx.x] = run;
+  }
   __syncthreads();
-  if (wave) return;
-  float whole[N];
+  int turn = 0;
+  for (int i = 0; i < BORDERS; ++i) {
+    const int tile = group * BORDERS + i, token = runs[i].x, end = runs[i].y;
+    if (token < 0) continue;
+    double sum[N] = {};
+    float whole[N];
+    if (end - tile <= LONG_RUN) {
+      if (turn++ % JOIN_WAVES != wave) continue;
+      add_parts<T>(p, tile, tile, end, c, sum);
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    double v = 0.0;
-    for (int w = 0; w < 8; ++w) v += sums[w][e * 64 + lane];
-    whole[e] = (float)v;
+      for (int e = 0; e < N; ++e) whole[e] = (float)sum[e];
+      put<T, WHOLE>(p, token, c, whole);
+      continue;
+    }
+    const int share = (end - tile + JOIN_WAVES - 1) / JOIN_WAVES, from = tile + wave * share;
+    add_parts<T>(p, tile, from, from + share < end ? from + share : end, c, sum);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < N; ++e) sums[wave][e * 64 + lane] = sum[e];
+    __syncthreads();
+    if (wave) continue;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      double v = 0.0;
+      for (int w = 0; w < JOIN_WAVES; ++w) v += sums[w][e * 64 + lane];
+      whole[e] = (float)v;
+    }
+    put<T, WHOLE>(p, token, c, whole);
   }
-  put<T>(p, token, c, whole);
 }
 
 int range_of(long long rows) {
@@ -256,6 +351,19 @@ int tile_of(const prism_embedding_desc& d, int chunks) {
 }
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
+template <typename T, typename I> void lookup(const Lookup& p, dim3 grid, hipStream_t s) {
+  hipLaunchKernelGGL((p.width >= Vec<T>::N ? embedding_kernel<T, I, true> : embedding_kernel<T, I, false>), grid, dim3(256), 0, s, p);
+}
+template <typename T> void lookup(const Lookup& p, bool wide, dim3 grid, hipStream_t s) {
+  if (wide) lookup<T, int64_t>(p, grid, s);
+  else lookup<T, int>(p, grid, s);
+}
+template <typename T> void add_up(const Sums& p, dim3 sums, dim3 joins, hipStream_t s) {
+  const bool whole = p.width >= Vec<T>::N;
+  hipLaunchKernelGGL((whole ? embedding_sums_kernel<T, true> : embedding_sums_kernel<T, false>), sums, dim3(256), 0, s, p);
+  if (joins.x) hipLaunchKernelGGL((whole ? embedding_join_kernel<T, true> : embedding_join_kernel<T, false>), joins, dim3(64 * JOIN_WAVES), 0, s, p);
+}
+
 }  // namespace
 
 int launch_embedding(const void* table, const void* tokens, void* out, int dt, const prism_embedding_desc& d, hipStream_t s) {
@@ -268,13 +376,8 @@ int launch_embedding(const void* table, const void* tokens, void* out, int dt, c
   while (p.lanes > 1 && (p.lanes > vectors || (vectors + p.lanes - 1) / p.lanes * p.lanes > vectors + vectors / 8)) p.lanes /= 2;
   const long long need = (d.count + 256 / p.lanes - 1) / (256 / p.lanes);
   const dim3 grid((unsigned)(need < 16384 ? need : 16384));
-  if (dt == PRISM_F32) {
-    if (d.wide_tokens) hipLaunchKernelGGL((embedding_kernel<float, int64_t>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((embedding_kernel<float, int>), grid, dim3(256), 0, s, p);
-  } else {
-    if (d.wide_tokens) hipLaunchKernelGGL((embedding_kernel<__bf16, int64_t>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((embedding_kernel<__bf16, int>), grid, dim3(256), 0, s, p);
-  }
+  if (dt == PRISM_F32) lookup<float>(p, d.wide_tokens, grid, s);
+  else lookup<__bf16>(p, d.wide_tokens, grid, s);
   return PRISM_OK;
 }
 
@@ -286,7 +389,7 @@ EmbeddingPlan embedding_plan(const prism_embedding_desc& d, int dt) {
   P.tiles = (int)((d.count + P.tile - 1) / P.tile);
   P.o_sorted = up((size_t)(d.rows + 1) * sizeof(int));
   P.o_part = P.o_sorted + up((size_t)d.count * sizeof(int2));
-  P.total = P.o_part + up((size_t)P.tiles * 2 * d.width * sizeof(float));
+  P.total = P.o_part + up((size_t)P.tiles * 2 * P.chunks * 64 * n * sizeof(float));
   return P;
 }
 
@@ -305,17 +408,14 @@ int launch_embedding_backward(const void* dout, const void* tokens, void* dtable
   Sums p = {};
   p.dout = dout; p.dtable = dtable; p.starts = q.starts; p.sorted = q.sorted; p.part = (float*)(ws + P.o_part);
   p.rows = d.rows; p.ds = d.out_stride; p.ts = d.table_stride; p.width = d.width; p.scale = d.scale;
-  p.tile = P.tile; p.tiles = P.tiles; p.chunks = P.chunks; p.tile_waves = P.tiles * P.chunks;
-  // a wave clears rows until 2048 workgroups are at work
-  const long long clear = (d.rows + 3) / 4;
+  p.tile = P.tile; p.chunks = P.chunks; p.tile_waves = P.tiles * P.chunks;
+  // 2048 workgroups clear rows, if each wave has one
+  p.clear = (int)(d.rows <= 8192 ? 1 : d.rows < 64 * 8192 ? (d.rows + 8191) / 8192 : 64);
+  const long long clear = (d.rows + 4 * p.clear - 1) / (4 * p.clear);
   const dim3 grid((unsigned)((p.tile_waves + 3) / 4 + (clear < 2048 ? clear : 2048)));
-  if (dt == PRISM_F32) hipLaunchKernelGGL((embedding_sums_kernel<float>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((embedding_sums_kernel<__bf16>), grid, dim3(256), 0, s, p);
-  if (P.tiles > 1) {
-    const dim3 joins((unsigned)((P.tiles - 1) * P.chunks));
-    if (dt == PRISM_F32) hipLaunchKernelGGL((embedding_join_kernel<float>), joins, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((embedding_join_kernel<__bf16>), joins, dim3(512), 0, s, p);
-  }
+  const dim3 joins(P.tiles > 1 ? (unsigned)((P.tiles - 1 + BORDERS - 1) / BORDERS * P.chunks) : 0);
+  if (dt == PRISM_F32) add_up<float>(p, grid, joins, s);
+  else add_up<__bf16>(p, grid, joins, s);
   return PRISM_OK;
 }
 

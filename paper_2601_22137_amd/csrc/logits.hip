@@ -78,20 +78,34 @@ __device__ inline int token_of(const Logits& p, long long row) {
   return t >= 0 && t < p.vocabulary ? (int)t : -1;
 }
 
+// What is given for a row, read ahead
+struct Given {
+  int token;
+  float weight, advantage, old, ref;
+};
+__device__ inline Given given_for(const Logits& p, long long row) {
+  Given g = {token_of(p, row), 0.0f, 1.0f, 0.0f, 0.0f};
+  if (p.weights) g.weight = p.weights[row];
+  if (p.advantages) g.advantage = p.advantages[row];
+  if (p.old) g.old = p.old[row];
+  if (p.kl != 0.0) g.ref = p.ref[row];
+  return g;
+}
+
 // What one thread computes of a row: its results, and the derivative of the loss by logp.  z: the logit of the token
-__device__ inline float finish_row(const Logits& p, long long row, const Sum& a, float z) {
+__device__ inline float finish_row(const Logits& p, long long row, const Given& g, const Sum& a, float z) {
   const double log2s = log((double)a.s) * (1.0 / LN2);
   const double lse = a.s > 0.0f ? (a.m + log2s) * p.unit : -INFINITY;
   const double logp = z == -INFINITY ? -INFINITY : ((double)z * p.c - a.m - log2s) * p.unit;
   if (p.logp) p.logp[row] = (float)logp;
   if (p.lse) p.lse[row] = (float)lse;
   if (!p.losses) return 0.0f;
-  const double w = p.weights ? (double)p.weights[row] : *p.mean;
+  const double w = p.weights ? (double)g.weight : *p.mean;
   double l = 0.0, d = 0.0;
   if (w != 0.0) {
-    const double A = p.advantages ? (double)p.advantages[row] : 1.0;
+    const double A = g.advantage;
     if (p.old) {
-      const double r = exp(logp - p.old[row]), low = 1.0 - p.low, high = 1.0 + p.high, held = (r < low ? low : r > high ? high : r) * A, free = r * A;
+      const double r = exp(logp - g.old), low = 1.0 - p.low, high = 1.0 + p.high, held = (r < low ? low : r > high ? high : r) * A, free = r * A;
       if (free <= held) {
         l = -free;
         d = -free;
@@ -103,7 +117,7 @@ __device__ inline float finish_row(const Logits& p, long long row, const Sum& a,
       d = -A;
     }
     if (p.kl != 0.0) {
-      const double f = p.ref[row] - logp, e = expm1(f);
+      const double f = g.ref - logp, e = expm1(f);
       l += p.kl * (e - f);
       d -= p.kl * e;
     }
@@ -113,6 +127,14 @@ __device__ inline float finish_row(const Logits& p, long long row, const Sum& a,
   p.losses[row] = l;
   if (p.dlogp) p.dlogp[row] = (float)d;
   return (float)d;
+}
+
+// A row without a token
+__device__ inline void skip_row(const Logits& p, long long row) {
+  if (p.logp) p.logp[row] = 0.0f;
+  if (p.lse) p.lse[row] = 0.0f;
+  if (p.dlogp) p.dlogp[row] = 0.0f;
+  if (p.losses) p.losses[row] = 0.0;
 }
 
 template <typename T> __device__ inline void clear_row(const Logits& p, long long row, int threads) {
@@ -131,20 +153,16 @@ template <typename T> __device__ inline typename Vec<T>::type gradient(const typ
   return o;
 }
 
-template <typename T, int THREADS, bool GRAD>
+template <typename T, int THREADS, bool GRAD, bool PAST>
 __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
   constexpr int N = Vec<T>::N;
   __shared__ float2 memory[THREADS / 64];
   __shared__ float result;
   for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
-    const int t = token_of(p, row);
+    const Given g = given_for(p, row);
+    const int t = g.token;
     if (t < 0) {
-      if (threadIdx.x == 0) {
-        if (p.logp) p.logp[row] = 0.0f;
-        if (p.lse) p.lse[row] = 0.0f;
-        if (p.dlogp) p.dlogp[row] = 0.0f;
-        if (p.losses) p.losses[row] = 0.0;
-      }
+      if (threadIdx.x == 0) skip_row(p, row);
       if constexpr (GRAD) clear_row<T>(p, row, THREADS);
       continue;
     }
@@ -152,9 +170,9 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
     const float zt = (float)z[t];
     Sum a;
 #pragma unroll 4
-    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, load_vector(z, at, p.vocabulary, -INFINITY), p.c);
+    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, load_vector<T, PAST>(z, at, p.vocabulary, -INFINITY), p.c);
     a = whole_row<THREADS>(a, memory);
-    if (threadIdx.x == 0) result = finish_row(p, row, a, zt);
+    if (threadIdx.x == 0) result = finish_row(p, row, g, a, zt);
     if constexpr (GRAD) {
       __syncthreads();
       const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
@@ -164,6 +182,57 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
         store_vector(dz, at, p.vocabulary, gradient<T>(load_vector(z, at, p.vocabulary, -INFINITY), at, t, p.c, m, d, factor));
       __syncthreads();
     }
+  }
+}
+
+// The same with the row in registers, NV vectors a thread: loss and gradient read it once
+template <typename T, int THREADS, int NV, bool PAST>
+__global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
+  constexpr int N = Vec<T>::N;
+  using V = typename Vec<T>::type;
+  __shared__ float2 memory[THREADS / 64];
+  __shared__ float result;
+  const long long row = blockIdx.x;
+  const Given g = given_for(p, row);
+  const int t = g.token;
+  if (t < 0) {
+    if (threadIdx.x == 0) skip_row(p, row);
+    clear_row<T>(p, row, THREADS);
+    return;
+  }
+  const T* z = (const T*)p.z + row * p.zs;
+  const float zt = (float)z[t];
+  V v[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) v[j] = load_vector<T, PAST>(z, ((int)threadIdx.x + j * THREADS) * N, p.vocabulary, -INFINITY);
+  float top = -INFINITY, part[4] = {};
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = fmaxf(top, (float)v[j][e]);
+  Sum a;
+  a.m = top * p.c;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
+  const float own = a.reference();
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < N; ++e) part[e & 3] += exp2_of(fmaf((float)v[j][e], p.c, -own));
+  a.s = (part[0] + part[1]) + (part[2] + part[3]);
+  a = whole_row<THREADS>(a, memory);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
+  if (threadIdx.x == 0) result = finish_row(p, row, g, a, zt);
+  __syncthreads();
+  const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
+  T* dz = (T*)p.dz + row * p.ds;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = ((int)threadIdx.x + j * THREADS) * N;
+    const V o = gradient<T>(v[j], at, t, p.c, m, d, factor);
+    if constexpr (PAST) stream_vector_to(dz, at, p.vocabulary, o);
+    else store_vector(dz, at, p.vocabulary, o);
   }
 }
 
@@ -232,8 +301,12 @@ int threads_of(int vocabulary, int dt) {
   return vectors <= 512 ? 64 : vectors <= 2048 ? 256 : 512;
 }
 
+// Logits that do not fit the card's last cache are read past the caches where they are read once: 4096 x 131072 bf16, log-probabilities alone 165 us (177 through them)
+template <typename T> bool past(const Logits& p) { return p.rows * p.vocabulary * (long long)sizeof(T) > (256ll << 20); }
+
 template <typename T, int THREADS> void launch(const Logits& p, bool back, hipStream_t s) {
-  void (*kernel)(Logits) = back ? logprob_backward_kernel<T, THREADS> : p.dz ? logits_kernel<T, THREADS, true> : logits_kernel<T, THREADS, false>;
+  void (*kernel)(Logits) = back ? logprob_backward_kernel<T, THREADS> : p.dz ? logits_kernel<T, THREADS, true, false> : past<T>(p) ? logits_kernel<T, THREADS, false, true> :
+                                  logits_kernel<T, THREADS, false, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(p.rows < MOST_BLOCKS ? p.rows : MOST_BLOCKS)), dim3(THREADS), 0, s, p);
 }
 template <typename T> void by_threads(const Logits& p, int threads, bool back, hipStream_t s) {
@@ -241,7 +314,25 @@ template <typename T> void by_threads(const Logits& p, int threads, bool back, h
   else if (threads == 256) launch<T, 256>(p, back, s);
   else launch<T, 512>(p, back, s);
 }
+
+// The kernel that holds rows of that many vectors, or none
+template <typename T, bool PAST> void (*held_kernel(int vectors, int& threads))(Logits) {
+  if (vectors <= 64 * 8) return threads = 64, vectors <= 64 * 4 ? logits_held_kernel<T, 64, 4, PAST> : logits_held_kernel<T, 64, 8, PAST>;
+  if (vectors <= 256 * 8) return threads = 256, vectors <= 256 * 4 ? logits_held_kernel<T, 256, 4, PAST> : logits_held_kernel<T, 256, 8, PAST>;
+  if (vectors <= 512 * 8) return threads = 512, logits_held_kernel<T, 512, 8, PAST>;
+  if (vectors <= 1024 * 16) return threads = 1024, vectors <= 1024 * 8 ? logits_held_kernel<T, 1024, 8, PAST> : logits_held_kernel<T, 1024, 16, PAST>;
+  return nullptr;
+}
+template <typename T> bool held(const Logits& p, hipStream_t s) {
+  int threads = 0;
+  const int vectors = (p.vocabulary + Vec<T>::N - 1) / Vec<T>::N;
+  void (*kernel)(Logits) = p.rows > MOST_BLOCKS ? nullptr : past<T>(p) ? held_kernel<T, true>(vectors, threads) : held_kernel<T, false>(vectors, threads);
+  if (kernel) hipLaunchKernelGGL(kernel, dim3((unsigned)p.rows), dim3(threads), 0, s, p);
+  return kernel != nullptr;
+}
+
 void by_type(const Logits& p, int dt, bool back, hipStream_t s) {
+  if (!back && p.dz && (dt == PRISM_F32 ? held<float>(p, s) : held<__bf16>(p, s))) return;
   if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary, dt), back, s);
   else by_threads<__bf16>(p, threads_of(p.vocabulary, dt), back, s);
 }
