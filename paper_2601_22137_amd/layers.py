@@ -1,7 +1,7 @@
 """The layer operators for autograd, and the attention half of a transformer layer made of them: the part of a model whose 2-D weights
-optim.muon_orthogonalize updates.
+optim.muon_orthogonalize updates; and the operators at the ends of a model: embedding, norm of the residual stream, log-probabilities and losses.
 
-Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.  Second derivatives of attention and of norm and rotation are an error.
+Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.  Second derivatives are an error (those of dropout are computed).
 """
 import torch
 from torch.autograd.function import once_differentiable
@@ -57,6 +57,77 @@ class _Dropout(torch.autograd.Function):
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
 
 
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, table, scale):
+        ctx.save_for_backward(tokens)
+        ctx.rows, ctx.scale = table.shape[0], scale
+        return prism.embedding(tokens, table, scale=scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        tokens, = ctx.saved_tensors
+        return None, prism.embedding_backward(_width(dout), tokens, ctx.rows, scale=ctx.scale), None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, center, eps):
+        y, total, stats = prism.layer_norm(x, weight, bias, residual=residual, center=center, eps=eps)
+        ctx.save_for_backward(total, stats, weight)
+        ctx.center, ctx.bias = center, bias is not None
+        ctx.set_materialize_grads(False)
+        return y if residual is None else (y, total)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dtotal=None):
+        total, stats, weight = ctx.saved_tensors
+        if dy is None and dtotal is None:
+            return 6 * (None,)
+        dy = torch.zeros_like(total, memory_format=torch.contiguous_format) if dy is None else _width(dy)
+        dx, dw, db = prism.layer_norm_backward(dy, total, stats, weight, dtotal=None if dtotal is None else _width(dtotal), center=ctx.center, bias=ctx.bias)
+        need = ctx.needs_input_grad
+        return dx if need[0] else None, dx if need[1] else None, dw if weight is not None and need[2] else None, db, None, None
+
+
+class _TokenLogprob(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, scale):
+        logp, lse = prism.token_logprob(logits, tokens, scale=scale)
+        ctx.save_for_backward(logits, tokens, lse)
+        ctx.scale = scale
+        return logp
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp):
+        logits, tokens, lse = ctx.saved_tensors
+        return prism.token_logprob_backward(dlogp.contiguous(), logits, tokens, lse, scale=ctx.scale), None, None
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, advantages, old_logp, ref_logp, weights, options):
+        loss, logp, lse, dlogp, _ = prism.policy_loss(logits, tokens, advantages=advantages, old_logp=old_logp, ref_logp=ref_logp, weights=weights, gradient=False, **options)
+        ctx.save_for_backward(logits, tokens, lse, dlogp)
+        ctx.scale = options["scale"]
+        ctx.mark_non_differentiable(logp)
+        return loss, logp
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss, _):
+        logits, tokens, lse, dlogp = ctx.saved_tensors
+        return (prism.token_logprob_backward(dlogp * dloss, logits, tokens, lse, scale=ctx.scale),) + 6 * (None,)
+
+
+def _width(t):
+    """Rows at one stride, their entries next to each other (autograd hands out expanded gradients)."""
+    return t if t.is_contiguous() else t.contiguous()
+
+
 def _rows(t):
     """The entries of every head next to each other (autograd hands out expanded gradients)."""
     return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
@@ -85,6 +156,61 @@ def attention(q, k, v, scale=None, causal=False, softcap=0.0, slopes=None, prefi
 def dropout(x, p, seed, offset=0, residual=None):
     """prism.dropout with gradients for x and the residual."""
     return _Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(), p, seed, offset)
+
+
+def embedding(tokens, table, scale=1.0):
+    """prism.embedding with a gradient for the table [rows, width]."""
+    tokens = tokens.contiguous()
+    if not torch.is_grad_enabled():
+        return prism.embedding(tokens, table, scale=scale)
+    return _Embedding.apply(tokens, table, scale)
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, center=True, eps=1e-5):
+    """The norm of the rows of x, or, with a residual, (the norm of their sum, the sum): prism.layer_norm with gradients for x, the residual, weight and bias."""
+    if not torch.is_grad_enabled():
+        y, total, _ = prism.layer_norm(x, weight, bias, residual=residual, center=center, eps=eps)
+        return y if residual is None else (y, total)
+    return _LayerNorm.apply(x, residual, weight, bias, center, eps)
+
+
+def token_logprob(logits, tokens, scale=1.0):
+    """The log-probability of each row's token (prism.token_logprob) with a gradient for the logits."""
+    return _TokenLogprob.apply(logits, tokens.contiguous(), scale)
+
+
+def policy_loss(logits, tokens, advantages=None, old_logp=None, ref_logp=None, weights=None, clip=(0.2, 0.2), kl=0.0, scale=1.0):
+    """(loss, logp): prism.policy_loss with a gradient for the logits (cross entropy where only logits and tokens are given); logp has none.  The gradient is computed in the backward
+    pass, from the logits once more; where it can be used at once, prism.policy_loss gives it in the same pass as the loss: logits.backward(prism.policy_loss(...).dlogits)."""
+    for t, name in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights")):
+        _fixed(t, name)
+    tokens, advantages, old_logp, ref_logp, weights = (None if t is None else t.contiguous() for t in (tokens, advantages, old_logp, ref_logp, weights))
+    return _PolicyLoss.apply(logits, tokens, advantages, old_logp, ref_logp, weights, dict(clip=clip, kl=kl, scale=scale))
+
+
+class Embedding(torch.nn.Module):
+    """scale times the rows of a table, by token; a token that is no row gives zeros."""
+
+    def __init__(self, rows, width, scale=1.0, dtype=torch.bfloat16, device="cuda"):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.randn(rows, width, dtype=dtype, device=device))
+        self.scale = scale
+
+    def forward(self, tokens):
+        return embedding(tokens, self.weight, scale=self.scale)
+
+
+class LayerNorm(torch.nn.Module):
+    """The norm of the residual stream: x -> y, or (x, residual) -> (y, x + residual).  center=False: root mean square, without a bias."""
+
+    def __init__(self, width, center=True, eps=1e-5, device="cuda"):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(width, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(width, device=device)) if center else None
+        self.center, self.eps = center, eps
+
+    def forward(self, x, residual=None):
+        return layer_norm(x, self.weight, self.bias, residual=residual, center=self.center, eps=self.eps)
 
 
 def _capturing(t):
