@@ -17,7 +17,7 @@ struct Logits {
   void* dz;
   float *logp, *lse, *dlogp;             // results (backward: lse and dlogp are given)
   const float *advantages, *old, *ref, *weights;
-  double *losses, *mean;                 // weighted losses of the rows; one over the number of rows with a token, where weights are not given
+  double *losses, *mean;                 // weighted losses of the rows; one over the number of rows with a token (null: every workgroup counts them itself)
   long long rows, zs, ds;
   int vocabulary;
   float c, scale;
@@ -93,14 +93,14 @@ __device__ inline Given given_for(const Logits& p, long long row) {
 }
 
 // What one thread computes of a row: its results, and the derivative of the loss by logp.  z: the logit of the token
-__device__ inline float finish_row(const Logits& p, long long row, const Given& g, const Sum& a, float z) {
+__device__ inline float finish_row(const Logits& p, long long row, const Given& g, int count, const Sum& a, float z) {
   const double log2s = log((double)a.s) * (1.0 / LN2);
   const double lse = a.s > 0.0f ? (a.m + log2s) * p.unit : -INFINITY;
   const double logp = z == -INFINITY ? -INFINITY : ((double)z * p.c - a.m - log2s) * p.unit;
   if (p.logp) p.logp[row] = (float)logp;
   if (p.lse) p.lse[row] = (float)lse;
   if (!p.losses) return 0.0f;
-  const double w = p.weights ? (double)g.weight : *p.mean;
+  const double w = p.weights ? (double)g.weight : p.mean ? *p.mean : 1.0 / count;
   double l = 0.0, d = 0.0;
   if (w != 0.0) {
     const double A = g.advantage;
@@ -127,6 +127,14 @@ __device__ inline float finish_row(const Logits& p, long long row, const Given& 
   p.losses[row] = l;
   if (p.dlogp) p.dlogp[row] = (float)d;
   return (float)d;
+}
+
+// Rows with a token, by the whole workgroup
+template <int THREADS> __device__ inline int count_rows(const Logits& p) {
+  int n = 0;
+  if (p.losses && !p.weights && !p.mean)
+    for (long long first = 0; first < p.rows; first += THREADS) n += __syncthreads_count(first + threadIdx.x < p.rows && token_of(p, first + threadIdx.x) >= 0);
+  return n;
 }
 
 // A row without a token
@@ -158,6 +166,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
   constexpr int N = Vec<T>::N;
   __shared__ float2 memory[THREADS / 64];
   __shared__ float result;
+  const int count = count_rows<THREADS>(p);
   for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const Given g = given_for(p, row);
     const int t = g.token;
@@ -172,7 +181,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
 #pragma unroll 4
     for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, load_vector<T, PAST>(z, at, p.vocabulary, -INFINITY), p.c);
     a = whole_row<THREADS>(a, memory);
-    if (threadIdx.x == 0) result = finish_row(p, row, g, a, zt);
+    if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
     if constexpr (GRAD) {
       __syncthreads();
       const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
@@ -205,6 +214,7 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   V v[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) v[j] = load_vector<T, PAST>(z, ((int)threadIdx.x + j * THREADS) * N, p.vocabulary, -INFINITY);
+  const int count = count_rows<THREADS>(p);         // (while the row is under way)
   float top = -INFINITY, part[4] = {};
 #pragma unroll
   for (int j = 0; j < NV; ++j)
@@ -223,7 +233,7 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   a = whole_row<THREADS>(a, memory);
 #pragma unroll
   for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
-  if (threadIdx.x == 0) result = finish_row(p, row, g, a, zt);
+  if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
   __syncthreads();
   const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
   T* dz = (T*)p.dz + row * p.ds;
@@ -363,10 +373,12 @@ int launch_policy_loss(const void* z, const void* tokens, float* loss, float* lo
   p.logp = logp; p.lse = lse; p.dlogp = dlogp; p.dz = dz;
   p.advantages = d.advantages; p.old = d.old_logp; p.ref = d.ref_logp; p.weights = d.weights;
   p.low = d.clip_low; p.high = d.clip_high; p.kl = d.kl;
-  p.mean = (double*)ws; p.losses = p.mean + 1;
+  p.losses = (double*)ws + 1;
+  // a launch of its own counts the rows if there are many: a workgroup reads as many tokens as it has logits otherwise
+  if (!p.weights && (p.rows > 4096 || p.rows * 16 > p.vocabulary)) p.mean = (double*)ws;
   {
     ProfScope prof(PK_LOSS_SUM, s);
-    if (!p.weights) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, p);
+    if (p.mean) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, p);
   }
   if (p.rows) {
     ProfScope prof(PK_POLICY_LOSS, s);
