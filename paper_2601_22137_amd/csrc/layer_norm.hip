@@ -27,12 +27,16 @@ __global__ void __launch_bounds__(threads_of(THREADS)) layer_norm_kernel(LayerNo
       V r[NV];
 #pragma unroll
       for (int j = 0; j < NV; ++j) r[j] = R::load(res, j, width);
+      R::settle(v, width);
+      R::settle(r, width);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
 #pragma unroll
         for (int e = 0; e < N; ++e) v[j][e] = (T)((float)v[j][e] + (float)r[j][e]);
         R::store(total, j, width, v[j]);
       }
+    } else {
+      R::settle(v, width);
     }
     float mean = 0.0f;
     if (p.center) {

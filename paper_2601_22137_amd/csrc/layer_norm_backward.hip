@@ -31,6 +31,9 @@ __global__ void __launch_bounds__(threads_of(THREADS)) layer_norm_backward_kerne
     };
     if constexpr (TOTAL && THREADS < 1024) load_dtotal();
     const float2 stats = p.stats[at];
+    R::settle(d, width);
+    R::settle(h, width);
+    if constexpr (TOTAL && THREADS < 1024) R::settle(t, width);
     float sum = 0.0f, product = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -42,7 +45,10 @@ __global__ void __launch_bounds__(threads_of(THREADS)) layer_norm_backward_kerne
         dw[j * N + e] += dy * n;
         db[j * N + e] += dy;
       }
-    if constexpr (TOTAL && THREADS == 1024) load_dtotal();           // (registers)
+    if constexpr (TOTAL && THREADS == 1024) {                        // (registers)
+      load_dtotal();
+      R::settle(t, width);
+    }
     product = row_sum<THREADS>(product, memory, turn++) / (float)p.width;
     sum = p.center ? row_sum<THREADS>(sum, memory, turn++) / (float)p.width : 0.0f;
 #pragma unroll
@@ -119,7 +125,7 @@ template <typename T, int THREADS, int NV, int MODE> struct Backward {
 // Workgroups: as many as run at once.  More of them write more partial sums (16384 x 4096 bf16: 512 of them 109 us, 1024 137 us), fewer leave the chip idle.
 int backward_blocks(const Shape& h, const prism_layer_norm_desc& d, int dt) {
   const int entries = h.nv * (dt == PRISM_F32 ? 4 : 8);
-  return blocks_of(d.rows, h, h.threads == 1024 ? 256 : entries <= 8 || h.mode == ODD ? 1024 : 512);
+  return blocks_of(d.rows, h, h.threads == 1024 ? 256 : entries <= 8 ? 1024 : 512);
 }
 
 }  // namespace

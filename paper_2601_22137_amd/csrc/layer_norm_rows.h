@@ -25,23 +25,36 @@ struct LayerNorm {
 
 constexpr int threads_of(int THREADS) { return THREADS < 256 ? 256 : THREADS; }
 
-// How rows are read.  WHOLE: they end with a whole vector (no code for part of one, which costs registers); PAST: also past the caches.
-enum { ODD = 0, WHOLE = 1, PAST = 2 };
+// How rows are read.  WHOLE: they end with a whole vector (no code for part of one, which costs registers); ODD: they do not, TINY: they have not even one; ..PAST: past the caches.
+enum { TINY, ODD, ODD_PAST, WHOLE, WHOLE_PAST };
+constexpr bool whole_rows(int mode) { return mode >= WHOLE; }
 
 // Lane l of a row's THREADS has its vectors l, l + THREADS, ...: NV at most
 template <typename T, int THREADS, int NV, int MODE> struct Row {
   static constexpr int N = Vec<T>::N;
   using V = typename Vec<T>::type;
   static __device__ int at(int j) { return ((int)(threadIdx.x % THREADS) + j * THREADS) * N; }
-  static __device__ bool inside(int j, int e, int width) { return MODE == ODD ? at(j) + e < width : at(j) < width; }
+  static __device__ bool inside(int j, int e, int width) { return whole_rows(MODE) ? at(j) < width : at(j) + e < width; }
+  // A row's last vector is read so that it ends with the row, and put in its place by settle(): all the loads of a row first, as a wave waits for what it settles.  Entries past the
+  // end are 0 then.
   static __device__ V load(const T* row, int j, int width) {
-    if constexpr (MODE == ODD) return load_vector(row, at(j), width);
+    if constexpr (MODE == TINY) return load_vector(row, at(j), width);
     V v = {};
-    if (at(j) < width) v = MODE == PAST ? __builtin_nontemporal_load((const V*)(row + at(j))) : *(const V*)(row + at(j));
+    if (at(j) < width) {
+      const V* from = (const V*)(row + (whole_rows(MODE) || at(j) + N <= width ? at(j) : width - N));
+      v = MODE == ODD_PAST || MODE == WHOLE_PAST ? __builtin_nontemporal_load(from) : *from;
+    }
     return v;
   }
+  static __device__ void settle(V (&v)[NV], int width) {
+    if constexpr (MODE == ODD || MODE == ODD_PAST) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (at(j) < width && at(j) + N > width) v[j] = __builtin_bit_cast(V, __builtin_bit_cast(unsigned __int128, v[j]) >> ((at(j) + N - width) * (128 / N)));
+    }
+  }
   static __device__ void store(T* row, int j, int width, const V& v) {
-    if constexpr (MODE == ODD) return store_vector(row, at(j), width, v);
+    if constexpr (!whole_rows(MODE)) return store_vector(row, at(j), width, v);
     if (at(j) < width) *(V*)(row + at(j)) = v;
   }
 };
@@ -61,7 +74,7 @@ template <typename T, int THREADS, int NV, int MODE> struct Columns {
       for (int q = 0; q < N; q += 4) {
         Vec<float>::type v = {none, none, none, none};
         if (w) {
-          if constexpr (MODE != ODD) { if (R::at(j) < width) v = *(const Vec<float>::type*)(w + R::at(j) + q); }
+          if constexpr (whole_rows(MODE)) { if (R::at(j) < width) v = *(const Vec<float>::type*)(w + R::at(j) + q); }
           else v = load_vector(w, R::at(j) + q, width);
         }
 #pragma unroll
@@ -86,12 +99,14 @@ inline Shape shape_of(int width, int dt, long long rows, int arrays) {
   const int n = dt == PRISM_F32 ? 4 : 8, vectors = (width + n - 1) / n;
   constexpr Shape whole[] = {{16, 1}, {32, 1}, {32, 3}, {64, 2}, {64, 3}, {256, 1}, {256, 2}, {256, 3}, {1024, 1}, {1024, 2}, {1024, 4}};
   constexpr Shape odd[] = {{32, 1}, {32, 3}, {64, 2}, {64, 4}, {256, 2}, {256, 3}, {1024, 2}, {1024, 4}};
-  Shape r = {1024, 4, width % n ? ODD : rows * width * (16 / n) * arrays > (256ll << 20) ? PAST : WHOLE};
+  const bool past = rows * width * (16 / n) * arrays > (256ll << 20);
+  if (width < n) return {32, 1, TINY};
+  Shape r = {1024, 4, width % n ? past ? ODD_PAST : ODD : past ? WHOLE_PAST : WHOLE};
   auto find = [&](const Shape* all, int count) {
     for (int i = count - 1; i >= 0; --i)
       if (all[i].threads * all[i].nv >= vectors) { r.threads = all[i].threads; r.nv = all[i].nv; }
   };
-  if (r.mode == ODD) find(odd, 8);
+  if (!whole_rows(r.mode)) find(odd, 8);
   else find(whole, 11);
   return r;
 }
@@ -105,7 +120,9 @@ inline int blocks_of(long long rows, const Shape& s, int most) {
 template <typename T, template <typename, int, int, int> class L, int MODE, typename... A> void by_shape(const Shape& h, const A&... a) {
   constexpr int MOST = Vec<T>::N == 4 ? 4 : 2;      // four vectors of 1024 threads: rows over 8192 entries of fp32 only
   const int shape = h.threads * 8 + h.nv;
-  if constexpr (MODE == ODD) {
+  if constexpr (MODE == TINY) {
+    return L<T, 32, 1, MODE>::launch(a...);
+  } else if constexpr (!whole_rows(MODE)) {
     switch (shape) {
       case 32 * 8 + 1: return L<T, 32, 1, MODE>::launch(a...);
       case 32 * 8 + 3: return L<T, 32, 3, MODE>::launch(a...);
@@ -133,9 +150,11 @@ template <typename T, template <typename, int, int, int> class L, int MODE, type
   }
 }
 template <typename T, template <typename, int, int, int> class L, typename... A> void by_mode(const Shape& h, const A&... a) {
-  if (h.mode == ODD) by_shape<T, L, ODD>(h, a...);
+  if (h.mode == TINY) by_shape<T, L, TINY>(h, a...);
+  else if (h.mode == ODD) by_shape<T, L, ODD>(h, a...);
+  else if (h.mode == ODD_PAST) by_shape<T, L, ODD_PAST>(h, a...);
   else if (h.mode == WHOLE) by_shape<T, L, WHOLE>(h, a...);
-  else by_shape<T, L, PAST>(h, a...);
+  else by_shape<T, L, WHOLE_PAST>(h, a...);
 }
 template <template <typename, int, int, int> class L, typename... A> void by_type(int dt, const Shape& h, const A&... a) {
   if (dt == PRISM_F32) by_mode<float, L>(h, a...);
