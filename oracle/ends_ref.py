@@ -61,7 +61,7 @@ def logprob(z, tokens, scale):
         with np.errstate(divide="ignore"):
             lse[i] = top + np.log(total) if total else -np.inf
         p[i] = e / total if total else 0.0
-        logp[i] = -np.inf if np.isneginf(a[t]) else a[t] - lse[i]
+        logp[i] = -np.inf if np.isneginf(a[t]) else (a[t] - top) - np.log(total)         # (not from lse: next to a top of 1e38 the logarithm is lost)
     return logp, lse, p
 
 

@@ -4,8 +4,10 @@
 //   loss = sum w l,  l = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(f) - f - 1),  r = exp(logp - old), f = ref - logp;  without old l = -A logp + ...
 //   dl / dlogp = -(r A where r A <= clip(r) A, else 0) + kl (1 - exp(f))
 //
-// A row is one workgroup's.  Its exponentials are taken in base 2 relative to a running maximum m (rounded c z, c = s log2 e: exp2(c z - m) is one fused product and one
-// instruction), every thread with its own, joined at the end.  Sums are in 32 bits a thread, what follows from the whole row in 64.
+// A row is one workgroup's.  Its exponentials are taken in base 2 relative to a running maximum m, exp2(c (z - m)), c = s log2 e, every thread with its own, joined at the end: the difference
+// first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  Sums are in 32 bits a thread, what follows from the whole row in 64.
+#include <cmath>
+
 #include "layer.h"
 #include "row_vector.h"
 
@@ -20,54 +22,60 @@ struct Logits {
   double *losses, *mean;                 // weighted losses of the rows; one over the number of rows with a token (null: every workgroup counts them itself)
   long long rows, zs, ds;
   int vocabulary;
-  float c, scale;
-  double low, high, kl;
-  double unit;                           // scale / c: what a power of two is worth, the rounding of c taken out
+  float c, c_rest, scale;                // scale log2 e, rounded; fp32: rounded down and the rest, which is positive so that infinite differences keep their sign
+  double low, high, kl, exact_scale;
   bool wide;
 };
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// sum_j 2^(c z_j) = s 2^m; no terms: m = -inf, s = 0
+// c (z - m): fp32 with the rest of c, whose rounding would show there (of a difference of 20: 4e-7 of the exponential)
+template <typename T> __device__ inline float power(const Logits& p, float z, float m) {
+  const float d = z - m;
+  if constexpr (sizeof(T) == 4) return fmaf(d, p.c, d * p.c_rest);
+  else return d * p.c;
+}
+
+// sum_j 2^(c z_j) = s 2^(c m); no terms: m = -inf, s = 0
 struct Sum {
   float m = -INFINITY, s = 0.0f;
   __device__ float reference() const { return m == -INFINITY ? 0.0f : m; }
-  __device__ void raise(float to) {
+  template <typename T> __device__ void raise(const Logits& p, float to) {
     if (to > m) {
-      s *= exp2_of(m - to);
+      s *= exp2_of(power<T>(p, m, to));
       m = to;
     }
   }
-  __device__ void join(float om, float os) {
+  template <typename T> __device__ void join(const Logits& p, float om, float os) {
     const float to = fmaxf(m, om), by = to == -INFINITY ? 0.0f : to;
-    s = s * exp2_of(m - by) + os * exp2_of(om - by);
+    s = s * exp2_of(power<T>(p, m, by)) + os * exp2_of(power<T>(p, om, by));
     m = to;
   }
 };
 
-template <typename T> __device__ inline void add(Sum& a, const typename Vec<T>::type& v, float c) {
+template <typename T> __device__ inline void add(Sum& a, const Logits& p, const typename Vec<T>::type& v) {
   constexpr int N = Vec<T>::N;
   float top = (float)v[0];
 #pragma unroll
   for (int e = 1; e < N; ++e) top = fmaxf(top, (float)v[e]);
-  a.raise(top * c);
+  a.raise<T>(p, top);
   const float m = a.reference();
   float part[2] = {};
 #pragma unroll
-  for (int e = 0; e < N; ++e) part[e & 1] += exp2_of(fmaf((float)v[e], c, -m));
+  for (int e = 0; e < N; ++e) part[e & 1] += exp2_of(power<T>(p, (float)v[e], m));
   a.s += part[0] + part[1];
 }
 
 // The sum of the workgroup, in every thread
-template <int THREADS> __device__ inline Sum whole_row(Sum a, float2* memory) {
+template <typename T, int THREADS> __device__ inline Sum whole_row(const Logits& p, Sum a, float2* memory) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) a.join(__shfl_xor(a.m, d), __shfl_xor(a.s, d));
+  for (int d = 1; d < 64; d *= 2) a.join<T>(p, __shfl_xor(a.m, d), __shfl_xor(a.s, d));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) memory[threadIdx.x >> 6] = make_float2(a.m, a.s);
   __syncthreads();
   Sum b;
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) b.join(memory[w].x, memory[w].y);
+  for (int w = 0; w < THREADS / 64; ++w) b.join<T>(p, memory[w].x, memory[w].y);
   return b;
 }
 
@@ -94,9 +102,8 @@ __device__ inline Given given_for(const Logits& p, long long row) {
 
 // What one thread computes of a row: its results, and the derivative of the loss by logp.  z: the logit of the token
 __device__ inline float finish_row(const Logits& p, long long row, const Given& g, int count, const Sum& a, float z) {
-  const double log2s = log((double)a.s) * (1.0 / LN2);
-  const double lse = a.s > 0.0f ? (a.m + log2s) * p.unit : -INFINITY;
-  const double logp = z == -INFINITY ? -INFINITY : ((double)z * p.c - a.m - log2s) * p.unit;
+  const double logs = log((double)a.s), lse = a.m == -INFINITY ? -INFINITY : a.m * p.exact_scale + logs;
+  const double logp = z == -INFINITY ? -INFINITY : ((double)z - a.m) * p.exact_scale - logs;
   if (p.logp) p.logp[row] = (float)logp;
   if (p.lse) p.lse[row] = (float)lse;
   if (!p.losses) return 0.0f;
@@ -150,12 +157,12 @@ template <typename T> __device__ inline void clear_row(const Logits& p, long lon
   for (int at = threadIdx.x * Vec<T>::N; at < p.vocabulary; at += threads * Vec<T>::N) store_vector(dz, at, p.vocabulary, typename Vec<T>::type{});
 }
 
-// A vector of the gradient: [j = t] d - exp2(c z - m) factor
-template <typename T> __device__ inline typename Vec<T>::type gradient(const typename Vec<T>::type& v, int at, int t, float c, float m, float d, float factor) {
+// A vector of the gradient: [j = t] d - exp2(c (z - m)) factor
+template <typename T> __device__ inline typename Vec<T>::type gradient(const Logits& p, const typename Vec<T>::type& v, int at, int t, float m, float d, float factor) {
   typename Vec<T>::type o;
 #pragma unroll
   for (int e = 0; e < Vec<T>::N; ++e) {
-    const float g = -exp2_of(fmaf((float)v[e], c, -m)) * factor;
+    const float g = -exp2_of(power<T>(p, (float)v[e], m)) * factor;
     o[e] = (T)(at + e == t ? d + g : g);
   }
   return o;
@@ -179,8 +186,8 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
     const float zt = (float)z[t];
     Sum a;
 #pragma unroll 4
-    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, load_vector<T, PAST>(z, at, p.vocabulary, -INFINITY), p.c);
-    a = whole_row<THREADS>(a, memory);
+    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, p, load_vector<T, PAST>(z, at, p.vocabulary, -INFINITY));
+    a = whole_row<T, THREADS>(p, a, memory);
     if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
     if constexpr (GRAD) {
       __syncthreads();
@@ -188,7 +195,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
       T* dz = (T*)p.dz + row * p.ds;
 #pragma unroll 4
       for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
-        store_vector(dz, at, p.vocabulary, gradient<T>(load_vector(z, at, p.vocabulary, -INFINITY), at, t, p.c, m, d, factor));
+        store_vector(dz, at, p.vocabulary, gradient<T>(p, load_vector(z, at, p.vocabulary, -INFINITY), at, t, m, d, factor));
       __syncthreads();
     }
   }
@@ -221,16 +228,16 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
 #pragma unroll
     for (int e = 0; e < N; ++e) top = fmaxf(top, (float)v[j][e]);
   Sum a;
-  a.m = top * p.c;
+  a.m = top;
 #pragma unroll
   for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
   const float own = a.reference();
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int e = 0; e < N; ++e) part[e & 3] += exp2_of(fmaf((float)v[j][e], p.c, -own));
+    for (int e = 0; e < N; ++e) part[e & 3] += exp2_of(power<T>(p, (float)v[j][e], own));
   a.s = (part[0] + part[1]) + (part[2] + part[3]);
-  a = whole_row<THREADS>(a, memory);
+  a = whole_row<T, THREADS>(p, a, memory);
 #pragma unroll
   for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
   if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
@@ -240,15 +247,19 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int at = ((int)threadIdx.x + j * THREADS) * N;
-    const V o = gradient<T>(v[j], at, t, p.c, m, d, factor);
+    const V o = gradient<T>(p, v[j], at, t, m, d, factor);
     if constexpr (PAST) stream_vector_to(dz, at, p.vocabulary, o);
     else store_vector(dz, at, p.vocabulary, o);
   }
 }
 
+// lse up to which the gradient takes it as it was rounded: probabilities are off by 2^-24 |lse|, 4e-6 here
+constexpr float MOST_LSE = 64.0f;
+
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) logprob_backward_kernel(Logits p) {
   constexpr int N = Vec<T>::N;
+  __shared__ float2 memory[THREADS / 64];
   for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const int t = token_of(p, row);
     if (t < 0) {
@@ -257,14 +268,23 @@ __global__ void __launch_bounds__(THREADS) logprob_backward_kernel(Logits p) {
     }
     const T* z = (const T*)p.z + row * p.zs;
     T* dz = (T*)p.dz + row * p.ds;
-    // the reference is lse in base 2, rounded; the factor makes up for its rounding
     const float d = p.dlogp[row] * p.scale, lse = p.lse[row];
-    const double exact = (double)lse / p.unit;
-    const float m = lse == -INFINITY ? 0.0f : (float)exact;
-    const float factor = lse == -INFINITY ? 0.0f : d * exp2_of((float)(m - exact));
+    float m, factor;
+    if (fabsf(lse) <= MOST_LSE) {        // the reference is lse / s, rounded; the factor makes up for its rounding
+      const double exact = (double)lse / p.exact_scale;
+      m = (float)exact;
+      factor = d * exp2_of((float)((m - exact) * p.c));
+    } else {                             // lse itself is rounded by too much: its sum once more
+      Sum a;
+#pragma unroll 4
+      for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, p, load_vector(z, at, p.vocabulary, -INFINITY));
+      a = whole_row<T, THREADS>(p, a, memory);
+      m = a.reference();
+      factor = a.s > 0.0f ? d / a.s : 0.0f;
+    }
 #pragma unroll 4
     for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
-      store_vector(dz, at, p.vocabulary, gradient<T>(load_vector(z, at, p.vocabulary, -INFINITY), at, t, p.c, m, d, factor));
+      store_vector(dz, at, p.vocabulary, gradient<T>(p, load_vector(z, at, p.vocabulary, -INFINITY), at, t, m, d, factor));
   }
 }
 
@@ -298,11 +318,15 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(Logits p, float* loss) {
 
 constexpr long long MOST_BLOCKS = 1 << 20;
 
-Logits common(const void* z, const void* tokens, const prism_logits_desc& d) {
+Logits common(const void* z, const void* tokens, int dt, const prism_logits_desc& d) {
   Logits p = {};
   p.z = z; p.tokens = tokens;
   p.rows = d.rows; p.zs = d.logits_stride; p.ds = d.dlogits_stride; p.vocabulary = d.vocabulary; p.wide = d.wide_tokens;
-  p.scale = (float)d.scale; p.c = (float)(d.scale / LN2); p.unit = d.scale / p.c;
+  p.scale = (float)d.scale; p.exact_scale = d.scale;
+  const double c = d.scale / LN2;
+  p.c = (float)c;
+  if (dt == PRISM_F32 && p.c >= c) p.c = std::nextafterf(p.c, 0.0f);
+  p.c_rest = (float)(c - p.c);
   return p;
 }
 
@@ -351,7 +375,7 @@ void by_type(const Logits& p, int dt, bool back, hipStream_t s) {
 
 int launch_logprob(const void* z, const void* tokens, float* logp, float* lse, int dt, const prism_logits_desc& d, hipStream_t s) {
   ProfScope prof(PK_LOGPROB, s);
-  Logits p = common(z, tokens, d);
+  Logits p = common(z, tokens, dt, d);
   p.logp = logp; p.lse = lse;
   by_type(p, dt, false, s);
   return PRISM_OK;
@@ -359,7 +383,7 @@ int launch_logprob(const void* z, const void* tokens, float* logp, float* lse, i
 
 int launch_logprob_backward(const float* dlogp, const void* z, const void* tokens, const float* lse, void* dz, int dt, const prism_logits_desc& d, hipStream_t s) {
   ProfScope prof(PK_LOGPROB_BACKWARD, s);
-  Logits p = common(z, tokens, d);
+  Logits p = common(z, tokens, dt, d);
   p.dlogp = (float*)dlogp; p.lse = (float*)lse; p.dz = dz;
   by_type(p, dt, true, s);
   return PRISM_OK;
@@ -369,7 +393,7 @@ size_t policy_loss_bytes(const prism_logits_desc& d) { return (size_t)(d.rows + 
 
 int launch_policy_loss(const void* z, const void* tokens, float* loss, float* logp, float* lse, float* dlogp, void* dz, int dt, const prism_logits_desc& d, char* ws,
                        hipStream_t s) {
-  Logits p = common(z, tokens, d);
+  Logits p = common(z, tokens, dt, d);
   p.logp = logp; p.lse = lse; p.dlogp = dlogp; p.dz = dz;
   p.advantages = d.advantages; p.old = d.old_logp; p.ref = d.ref_logp; p.weights = d.weights;
   p.low = d.clip_low; p.high = d.clip_high; p.kl = d.kl;

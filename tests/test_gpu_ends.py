@@ -395,6 +395,35 @@ def test_logits_edges(prism):
     assert r.logp.shape == (2, 3) and r.dlogits.shape == (2, 3, 40)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("v", [5, 300, 5000, 33000, 140000])
+def test_logits_of_the_lowest_value(prism, dtype, v):
+    """Masks of the type's lowest value: like any other logit, also where a row has no others; and rows far from zero."""
+    low = torch.finfo(dtype).min
+    g = torch.Generator().manual_seed(v)
+    z = torch.randn(6, v, generator=g)
+    z[0], z[1, 1:] = low, low
+    z[2, ::2] = low
+    z[3] = low
+    z[3, 2:] = -float("inf")
+    z[4] += 3e4
+    z[5] = z[5].abs() * 1e37
+    z = z.to(dtype).cuda()
+    t = torch.tensor([v - 1, 0, 1, 1, 2, 3], device="cuda")
+    logp, lse = prism.token_logprob(z, t)
+    rlogp, rlse, p = R.logprob(_f64(z), t.tolist(), 1.0)
+    # differences of logits are rounded to fp32, and a thread's sum of v / 64 terms
+    off = E * np.where(p > 0, np.abs(np.where(p > 0, _f64(z), 0.0) - _f64(z).max(1, keepdims=True)) * p, 0.0).sum(1) * 3 + E * (v / 64 + 100)
+    _close(logp, rlogp, off + 2 * E * np.abs(rlogp), "logp")
+    _close(lse, rlse, off + E * np.abs(rlse), "lse")
+    d = prism.token_logprob_backward(torch.ones(6, device="cuda"), z, t, lse)
+    ref = R.logprob_gradient(np.ones(6), p, t.tolist(), 1.0)
+    bound = _u(dtype) * np.abs(ref) + (off + 80 * E)[:, None] * p + 3 * E * (p + (ref > 0))
+    _close(d, ref, bound, "dlogits")
+    r = prism.policy_loss(z, t, weights=torch.ones(6, device="cuda"))
+    _close(r.dlogits, -ref, bound, "dlogits in one pass")
+
+
 # ------------------------------------------------------------------------------------------------------- streams and graphs
 
 def _calls(prism, g, dtype):
