@@ -218,9 +218,10 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   }
   const T* z = (const T*)p.z + row * p.zs;
   const float zt = (float)z[t];
+  const int at = (int)threadIdx.x * N;       // in each of NV pieces of the row, whose beginnings all lanes share: one offset takes fewer registers than NV
   V v[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) v[j] = load_vector<T, PAST>(z, ((int)threadIdx.x + j * THREADS) * N, p.vocabulary, -INFINITY);
+  for (int j = 0; j < NV; ++j) v[j] = load_vector<T, PAST>(z + j * THREADS * N, at, p.vocabulary - j * THREADS * N, -INFINITY);
   const int count = count_rows<THREADS>(p);         // (while the row is under way)
   float top = -INFINITY, part[4] = {};
 #pragma unroll
@@ -246,10 +247,10 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   T* dz = (T*)p.dz + row * p.ds;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int at = ((int)threadIdx.x + j * THREADS) * N;
-    const V o = gradient<T>(p, v[j], at, t, m, d, factor);
-    if constexpr (PAST) stream_vector_to(dz, at, p.vocabulary, o);
-    else store_vector(dz, at, p.vocabulary, o);
+    const int width = p.vocabulary - j * THREADS * N;
+    const V o = gradient<T>(p, v[j], at, t - j * THREADS * N, m, d, factor);
+    if constexpr (PAST) stream_vector_to(dz + j * THREADS * N, at, width, o);
+    else store_vector(dz + j * THREADS * N, at, width, o);
   }
 }
 
