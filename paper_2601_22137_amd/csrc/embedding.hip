@@ -59,9 +59,10 @@ template <typename T, typename I, bool WHOLE> __global__ void __launch_bounds__(
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         if (first + j * p.lanes * N >= p.width) break;
+        float o[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[j][e] = there ? (T)((float)v[j][e] * p.scale) : (T)0.0f;
-        store_piece<T, WHOLE>(to, column<T, WHOLE>(first + (j * p.lanes + lane) * N, p.width), p.width, v[j]);
+        for (int e = 0; e < N; ++e) o[e] = there ? (float)v[j][e] * p.scale : 0.0f;
+        store_piece<T, WHOLE>(to, column<T, WHOLE>(first + (j * p.lanes + lane) * N, p.width), p.width, rounded<T>(o));
       }
     }
   }
@@ -198,10 +199,10 @@ struct Sums {
 };
 
 template <typename T, bool WHOLE> __device__ inline void put(const Sums& p, int token, int c, const float (&sum)[Vec<T>::N]) {
-  typename Vec<T>::type o;
+  float o[Vec<T>::N];
 #pragma unroll
-  for (int e = 0; e < Vec<T>::N; ++e) o[e] = (T)(sum[e] * p.scale);
-  store_piece<T, WHOLE>((T*)p.dtable + token * p.ts, column<T, WHOLE>(c, p.width), p.width, o);
+  for (int e = 0; e < Vec<T>::N; ++e) o[e] = sum[e] * p.scale;
+  store_piece<T, WHOLE>((T*)p.dtable + token * p.ts, column<T, WHOLE>(c, p.width), p.width, rounded<T>(o));
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));

@@ -31,8 +31,10 @@ __global__ void __launch_bounds__(threads_of(THREADS)) layer_norm_kernel(LayerNo
       R::settle(r, width);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
+        float o[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[j][e] = (T)((float)v[j][e] + (float)r[j][e]);
+        for (int e = 0; e < N; ++e) o[e] = (float)v[j][e] + (float)r[j][e];
+        v[j] = rounded<T>(o);
         R::store(total, j, width, v[j]);
       }
     } else {
@@ -64,10 +66,10 @@ __global__ void __launch_bounds__(threads_of(THREADS)) layer_norm_kernel(LayerNo
     T* y = (T*)p.y + (there ? row : 0) * p.ys;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      V o;
+      float o[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) o[e] = (T)(((float)v[j][e] - mean) * r * w.get(j, e) + b.get(j, e));
-      R::store(y, j, width, o);
+      for (int e = 0; e < N; ++e) o[e] = ((float)v[j][e] - mean) * r * w.get(j, e) + b.get(j, e);
+      R::store(y, j, width, rounded<T>(o));
     }
   }
 }

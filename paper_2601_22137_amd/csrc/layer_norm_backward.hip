@@ -55,15 +55,15 @@ __global__ void __launch_bounds__(threads_of(THREADS)) layer_norm_backward_kerne
     for (int j = 0; j < NV; ++j) {
       as_loaded<T>(d[j]);
       as_loaded<T>(h[j]);
-      V o;
+      float o[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float n = ((float)h[j][e] - stats.x) * stats.y;
         float dx = stats.y * ((float)d[j][e] * w.get(j, e) - sum - n * product);
         if constexpr (TOTAL) dx += (float)t[j][e];
-        o[e] = (T)dx;
+        o[e] = dx;
       }
-      R::store((T*)p.y + at * p.ys, j, width, o);
+      R::store((T*)p.y + at * p.ys, j, width, rounded<T>(o));
     }
   }
   if (!p.part) return;

@@ -36,6 +36,27 @@ template <typename T> __device__ inline float power(const Logits& p, float z, fl
   else return d * p.c;
 }
 
+// exp2(c (z - m)) of many z.  bf16 takes c z - (c m rounded) as one fused product and makes up for that rounding once, by the factor `rest`; not where c m is so large that its
+// rounding is no longer small, or overflows (masks of the lowest value).  One instruction in nine of an exponential less: the vector units bound these kernels as much as memory does.
+struct Reference {
+  float m, cm, rest;
+  bool fused;
+  __device__ Reference(const Logits& p, float m, bool bf16) : m(m), cm(m * p.c) {
+    fused = bf16 && fabsf(cm) < 1048576.0f;
+    rest = fused ? exp2_of(-fmaf(m, p.c, -cm)) : 1.0f;
+  }
+};
+template <typename T, bool FUSED> __device__ inline float exp_of(const Logits& p, const Reference& r, float z) {
+  return exp2_of(FUSED ? fmaf(z, p.c, -r.cm) : power<T>(p, z, r.m));
+}
+// f(whether fused), a constant
+template <typename T, typename F> __device__ inline void either(const Reference& r, F&& f) {
+  if constexpr (sizeof(T) == 2) {
+    if (r.fused) return f(std::true_type{});
+  }
+  f(std::false_type{});
+}
+
 // sum_j 2^(c z_j) = s 2^(c m); no terms: m = -inf, s = 0
 struct Sum {
   float m = -INFINITY, s = 0.0f;
@@ -53,17 +74,34 @@ struct Sum {
   }
 };
 
-template <typename T> __device__ inline void add(Sum& a, const Logits& p, const typename Vec<T>::type& v) {
-  constexpr int N = Vec<T>::N;
-  float top = (float)v[0];
+// The sum over a row that is read in pieces of K vectors a thread, all on their way before the first is used
+template <typename T, int THREADS, bool PAST> __device__ inline Sum own_sum(const Logits& p, const T* z) {
+  constexpr int N = Vec<T>::N, K = 4;
+  using V = typename Vec<T>::type;
+  Sum a;
+  for (int first = 0; first < p.vocabulary; first += K * THREADS * N) {
+    V v[K];
 #pragma unroll
-  for (int e = 1; e < N; ++e) top = fmaxf(top, (float)v[e]);
-  a.raise<T>(p, top);
-  const float m = a.reference();
-  float part[2] = {};
+    for (int j = 0; j < K; ++j) v[j] = load_vector<T, PAST>(z + first + j * THREADS * N, (int)threadIdx.x * N, p.vocabulary - first - j * THREADS * N, -INFINITY);
+    float top = -INFINITY;
 #pragma unroll
-  for (int e = 0; e < N; ++e) part[e & 1] += exp2_of(power<T>(p, (float)v[e], m));
-  a.s += part[0] + part[1];
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) top = fmaxf(top, (float)v[j][e]);
+    a.raise<T>(p, top);
+    const Reference r(p, a.reference(), sizeof(T) == 2);
+    float part[4] = {};
+    either<T>(r, [&](auto fused) {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        as_loaded<T>(v[j]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) part[e & 3] += exp_of<T, fused.value>(p, r, (float)v[j][e]);
+      }
+    });
+    a.s += ((part[0] + part[1]) + (part[2] + part[3])) * r.rest;
+  }
+  return a;
 }
 
 // The sum of the workgroup, in every thread
@@ -157,15 +195,18 @@ template <typename T> __device__ inline void clear_row(const Logits& p, long lon
   for (int at = threadIdx.x * Vec<T>::N; at < p.vocabulary; at += threads * Vec<T>::N) store_vector(dz, at, p.vocabulary, typename Vec<T>::type{});
 }
 
-// A vector of the gradient: [j = t] d - exp2(c (z - m)) factor
-template <typename T> __device__ inline typename Vec<T>::type gradient(const Logits& p, const typename Vec<T>::type& v, int at, int t, float m, float d, float factor) {
-  typename Vec<T>::type o;
+// A vector of the gradient: [j = t] d - exp2(c (z - m)) factor; factor has the reference's rest in it
+template <typename T, bool FUSED>
+__device__ inline typename Vec<T>::type gradient(const Logits& p, const Reference& r, const typename Vec<T>::type& v, int at, int t, float d, float factor) {
+  constexpr int N = Vec<T>::N;
+  float g[N];
 #pragma unroll
-  for (int e = 0; e < Vec<T>::N; ++e) {
-    const float g = -exp2_of(power<T>(p, (float)v[e], m)) * factor;
-    o[e] = (T)(at + e == t ? d + g : g);
+  for (int e = 0; e < N; ++e) g[e] = exp_of<T, FUSED>(p, r, (float)v[e]) * -factor;
+  if ((unsigned)(t - at) < (unsigned)N) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) g[e] += at + e == t ? d : 0.0f;
   }
-  return o;
+  return rounded<T>(g);
 }
 
 template <typename T, int THREADS, bool GRAD, bool PAST>
@@ -184,18 +225,18 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
     }
     const T* z = (const T*)p.z + row * p.zs;
     const float zt = (float)z[t];
-    Sum a;
-#pragma unroll 4
-    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, p, load_vector<T, PAST>(z, at, p.vocabulary, -INFINITY));
-    a = whole_row<T, THREADS>(p, a, memory);
+    const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, PAST>(p, z), memory);
     if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
     if constexpr (GRAD) {
       __syncthreads();
-      const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
+      const Reference r(p, a.reference(), sizeof(T) == 2);
+      const float d = result * p.scale, factor = a.s > 0.0f ? d / a.s * r.rest : 0.0f;
       T* dz = (T*)p.dz + row * p.ds;
+      either<T>(r, [&](auto fused) {
 #pragma unroll 4
-      for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
-        store_vector(dz, at, p.vocabulary, gradient<T>(p, load_vector(z, at, p.vocabulary, -INFINITY), at, t, m, d, factor));
+        for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
+          store_vector(dz, at, p.vocabulary, gradient<T, fused.value>(p, r, load_vector(z, at, p.vocabulary, -INFINITY), at, t, d, factor));
+      });
       __syncthreads();
     }
   }
@@ -230,28 +271,32 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
     for (int e = 0; e < N; ++e) top = fmaxf(top, (float)v[j][e]);
   Sum a;
   a.m = top;
+  const Reference own(p, a.reference(), sizeof(T) == 2);
+  either<T>(own, [&](auto fused) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
-  const float own = a.reference();
+    for (int j = 0; j < NV; ++j) {
+      as_loaded<T>(v[j]);
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int e = 0; e < N; ++e) part[e & 3] += exp2_of(power<T>(p, (float)v[j][e], own));
-  a.s = (part[0] + part[1]) + (part[2] + part[3]);
+      for (int e = 0; e < N; ++e) part[e & 3] += exp_of<T, fused.value>(p, own, (float)v[j][e]);
+    }
+  });
+  a.s = ((part[0] + part[1]) + (part[2] + part[3])) * own.rest;
   a = whole_row<T, THREADS>(p, a, memory);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) as_loaded<T>(v[j]);
   if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
   __syncthreads();
-  const float d = result * p.scale, m = a.reference(), factor = a.s > 0.0f ? d / a.s : 0.0f;
+  const Reference r(p, a.reference(), sizeof(T) == 2);
+  const float d = result * p.scale, factor = a.s > 0.0f ? d / a.s * r.rest : 0.0f;
   T* dz = (T*)p.dz + row * p.ds;
+  either<T>(r, [&](auto fused) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int width = p.vocabulary - j * THREADS * N;
-    const V o = gradient<T>(p, v[j], at, t - j * THREADS * N, m, d, factor);
-    if constexpr (PAST) stream_vector_to(dz + j * THREADS * N, at, width, o);
-    else store_vector(dz + j * THREADS * N, at, width, o);
-  }
+    for (int j = 0; j < NV; ++j) {
+      as_loaded<T>(v[j]);
+      const int width = p.vocabulary - j * THREADS * N;
+      const V o = gradient<T, fused.value>(p, r, v[j], at, t - j * THREADS * N, d, factor);
+      if constexpr (PAST) stream_vector_to(dz + j * THREADS * N, at, width, o);
+      else store_vector(dz + j * THREADS * N, at, width, o);
+    }
+  });
 }
 
 // lse up to which the gradient takes it as it was rounded: probabilities are off by 2^-24 |lse|, 4e-6 here
@@ -276,16 +321,17 @@ __global__ void __launch_bounds__(THREADS) logprob_backward_kernel(Logits p) {
       m = (float)exact;
       factor = d * exp2_of((float)((m - exact) * p.c));
     } else {                             // lse itself is rounded by too much: its sum once more
-      Sum a;
-#pragma unroll 4
-      for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N) add<T>(a, p, load_vector(z, at, p.vocabulary, -INFINITY));
-      a = whole_row<T, THREADS>(p, a, memory);
+      const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, false>(p, z), memory);
       m = a.reference();
       factor = a.s > 0.0f ? d / a.s : 0.0f;
     }
+    const Reference r(p, m, sizeof(T) == 2);
+    factor *= r.rest;
+    either<T>(r, [&](auto fused) {
 #pragma unroll 4
-    for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
-      store_vector(dz, at, p.vocabulary, gradient<T>(p, load_vector(z, at, p.vocabulary, -INFINITY), at, t, m, d, factor));
+      for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
+        store_vector(dz, at, p.vocabulary, gradient<T, fused.value>(p, r, load_vector(z, at, p.vocabulary, -INFINITY), at, t, d, factor));
+    });
   }
 }
 

@@ -16,6 +16,15 @@ template <> struct Vec<__bf16> {
   typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2)));
 };
 
+// Rounded, two at a time where the type has an instruction for it
+template <typename T> __device__ inline typename Vec<T>::type rounded(const float (&f)[Vec<T>::N]) {
+  typedef float floats __attribute__((ext_vector_type(Vec<T>::N)));
+  floats x;
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e) x[e] = f[e];
+  return __builtin_convertvector(x, typename Vec<T>::type);
+}
+
 // Keeps the compiler from holding what was computed from a vector before (its entries in 32 bits, twice the registers) until it is used again
 template <typename T> __device__ inline void as_loaded(typename Vec<T>::type& v) {
   typedef unsigned words __attribute__((ext_vector_type(4)));

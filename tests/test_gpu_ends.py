@@ -424,6 +424,46 @@ def test_logits_of_the_lowest_value(prism, dtype, v):
     _close(r.dlogits, -ref, bound, "dlogits in one pass")
 
 
+def test_offsets_past_32_bits(prism):
+    """Rows that lie more than 2^31 elements behind the first."""
+    n, width, stride = 40, 264, 1 << 26
+    whole = torch.empty(n * stride, device="cuda", dtype=BF16).view(n, stride)          # 5 GB, the rows' beginnings only are touched
+    out = torch.empty(n * stride, device="cuda", dtype=BF16).view(n, stride)[:, :width]
+    x = whole[:, :width]
+    x.copy_(torch.randn(n, width, generator=torch.Generator().manual_seed(1)))
+    near, t = x.contiguous(), torch.arange(n - 1, -1, -1, device="cuda")
+    assert torch.equal(prism.embedding(t, x, out=out), near[t])
+    assert torch.equal(prism.embedding_backward(x, t, n, out=out), near[t])
+    w = torch.ones(width, device="cuda")
+    y, total, stats = prism.layer_norm(near, w, residual=near)
+    got = prism.layer_norm(x, w, residual=x, out=(out, torch.empty_like(near)))
+    assert torch.equal(got[0], y) and torch.equal(got[1], total) and torch.equal(got[2], stats)
+    for a, b in zip(prism.layer_norm_backward(x, x, stats, w, dtotal=x, out=out), prism.layer_norm_backward(near, near, stats, w, dtotal=near)):
+        assert torch.equal(a, b)
+    logp, lse = prism.token_logprob(near, t)
+    assert all(torch.equal(a, b) for a, b in zip(prism.token_logprob(x, t), (logp, lse)))
+    assert torch.equal(prism.token_logprob_backward(logp, x, t, lse, out=out), prism.token_logprob_backward(logp, near, t, lse))
+    assert all(torch.equal(a, b) for a, b in zip(prism.policy_loss(x, t, out=out), prism.policy_loss(near, t)))
+
+
+def test_many_rows(prism):
+    """More rows than one launch has workgroups for, and more tokens of one row than an unsigned count of 16 bits."""
+    rows = (1 << 20) + 77
+    z, t = torch.zeros(rows, 3, device="cuda"), torch.full((rows,), -1, device="cuda")
+    z[-5:, 1], t[-5:] = 2.0, 1
+    t[0] = 0
+    logp, lse = prism.token_logprob(z, t)
+    one = float(logp[-1])
+    assert np.isclose(float(logp[0]), -np.log(3)) and np.isclose(one, 2 - np.log(2 + np.exp(2))) and bool((logp[1:-5] == 0).all()) and bool((logp[-5:] == one).all())
+    r = prism.policy_loss(z, t)
+    assert np.isclose(float(r.loss), -(float(logp[0]) + 5 * one) / 6) and not bool(r.dlogits[1:-5].any())
+    assert torch.equal(r.logp, logp)
+    y, _, _ = prism.layer_norm(z, eps=1.0)
+    assert bool((y[:-5] == 0).all()) and bool((y[-5:] == y[-1]).all())
+    d = prism.embedding_backward(torch.ones(rows, 2, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda"), 2)
+    assert d.tolist() == [[rows, rows], [0, 0]]
+
+
 # ------------------------------------------------------------------------------------------------------- streams and graphs
 
 def _calls(prism, g, dtype):
