@@ -98,7 +98,7 @@ struct Shape { int threads, nv, mode; };
 inline Shape shape_of(int width, int dt, long long rows, int arrays) {
   const int n = dt == PRISM_F32 ? 4 : 8, vectors = (width + n - 1) / n;
   constexpr Shape whole[] = {{16, 1}, {32, 1}, {32, 3}, {64, 2}, {64, 3}, {256, 1}, {256, 2}, {256, 3}, {1024, 1}, {1024, 2}, {1024, 4}};
-  constexpr Shape odd[] = {{32, 1}, {32, 3}, {64, 2}, {64, 4}, {256, 2}, {256, 3}, {1024, 2}, {1024, 4}};
+  constexpr Shape odd[] = {{32, 1}, {32, 3}, {64, 2}, {64, 3}, {256, 1}, {256, 2}, {256, 3}, {1024, 2}, {1024, 4}};
   const bool past = rows * width * (16 / n) * arrays > (256ll << 20);
   if (width < n) return {32, 1, TINY};
   Shape r = {1024, 4, width % n ? past ? ODD_PAST : ODD : past ? WHOLE_PAST : WHOLE};
@@ -106,7 +106,7 @@ inline Shape shape_of(int width, int dt, long long rows, int arrays) {
     for (int i = count - 1; i >= 0; --i)
       if (all[i].threads * all[i].nv >= vectors) { r.threads = all[i].threads; r.nv = all[i].nv; }
   };
-  if (!whole_rows(r.mode)) find(odd, 8);
+  if (!whole_rows(r.mode)) find(odd, 9);
   else find(whole, 11);
   return r;
 }
@@ -127,7 +127,8 @@ template <typename T, template <typename, int, int, int> class L, int MODE, type
       case 32 * 8 + 1: return L<T, 32, 1, MODE>::launch(a...);
       case 32 * 8 + 3: return L<T, 32, 3, MODE>::launch(a...);
       case 64 * 8 + 2: return L<T, 64, 2, MODE>::launch(a...);
-      case 64 * 8 + 4: return L<T, 64, 4, MODE>::launch(a...);
+      case 64 * 8 + 3: return L<T, 64, 3, MODE>::launch(a...);
+      case 256 * 8 + 1: return L<T, 256, 1, MODE>::launch(a...);
       case 256 * 8 + 2: return L<T, 256, 2, MODE>::launch(a...);
       case 256 * 8 + 3: return L<T, 256, 3, MODE>::launch(a...);
       case 1024 * 8 + 2: return L<T, 1024, 2, MODE>::launch(a...);
