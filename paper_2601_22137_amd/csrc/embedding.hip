@@ -3,11 +3,14 @@
 //   out[i] = scale table[token[i]], 0 for a token that is no row;   dtable[v] = scale sum over i with token[i] = v of dout[i], 0 for a row without a token
 //
 // The gradient is a sum over sorted tokens, so that the same call gives the same bits whatever the order in which workgroups run:
-//   sort   a workgroup has a range of the table's rows; it goes through all tokens twice, counting those of each of its rows and those before its range, then
-//          putting each (in its order) in its place.  Nothing passes between workgroups.
-//   sums   the sorted tokens are cut into tiles of equal length; a wave adds up the rows of dout of a tile, 64 vectors of 16 bytes wide, in 32 bits.  A run of
-//          equal tokens that lies in one tile goes straight to the table; what crosses a border is kept as partial sums.  Other waves clear the rows without tokens.
-//   join   partial sums of a run in their order, in 64 bits.
+//   sort   a workgroup has a range of the table's rows, about a 256th; it goes through all tokens, counts those of each of its rows and those before its range, keeps its own in LDS and puts
+//          them, 64 at a time, in their places.  Nothing passes between workgroups.  65536 tokens, 32768 rows: 17.6 us, vector units 59 % busy (every workgroup looks at every token); 16384
+//          tokens: 9.
+//   sums   the sorted tokens are cut into tiles of equal length; a wave adds up the rows of dout of a tile, 64 vectors of 16 bytes wide, eight rows under way, in 32 bits.  A run of equal
+//          tokens that lies in one tile goes straight to the table; what crosses a border is kept as partial sums.  Other waves clear the rows without tokens.  Memory: 65536 x 768
+//          bf16 into 32768 rows 30 us, 161 MB; 16384 x 4096 into 131072 rows 216 us, 1216 MB, most of them zeros (a fill alone runs at 6.8 TB/s).
+//   join   partial sums of a run in their order, in 64 bits, long runs by eight waves together: 8 to 9 us, a chain of five dependent reads.
+// The lookup: 65536 x 768 from 32768 rows 26 us (154 MB), 16384 x 4096 from 131072 rows 54 us (236 MB, rows at random); a few tokens: 3 us, and the host's call.
 #include "layer.h"
 #include "row_vector.h"
 

@@ -1,5 +1,6 @@
 // Gradients of the norm of rows (layer_norm_rows.h has the formulas).  A workgroup goes through many rows and keeps its share of dw and db in registers; the shares are joined by a
-// second launch in a fixed order.
+// second launch in a fixed order.  The sums of 24 columns a lane, their weights and three rows leave room for two waves a SIMD (65536 x 768 bf16: 67 us, memory); rows of 16384 entries spill a
+// few registers (4096 of them 169 us, 3.2 TB/s).
 #include "layer_norm_rows.h"
 
 namespace prism {

@@ -3,7 +3,8 @@
 //   h = x + residual, mean = sum h / width (0 where it is not taken off), r = (mean (h - mean)^2 + eps)^(-1/2), y = (h - mean) r w + b
 //   g = dy w, n = (h - mean) r:  dx = r (g - mean g - n mean (g n)) + dtotal (without mean g where the mean is not taken off), dw = sum dy n, db = sum dy
 //
-// THREADS threads share a row, NV vectors of 16 bytes each: one pass over memory.  Statistics are of h as it is stored (rounded), so that the gradients meet the same numbers.
+// THREADS threads share a row, NV vectors of 16 bytes each: one pass over memory, at the rate of a large copy and above: 65536 x 768 bf16 with a residual 63 us (403 MB, 6.4 TB/s), gradients
+// 67 + 5 us; 16384 x 4096 88 and 97; 65536 x 771 80 and 93 (part of a vector in every row).  Statistics are of h as it is stored (rounded), so that the gradients meet the same numbers.
 #pragma once
 #include "layer.h"
 #include "row_vector.h"
@@ -92,8 +93,9 @@ template <typename T, int THREADS, int NV, int MODE> struct Columns {
   }
 };
 
-// Rows of `width` entries: the fewest threads that hold one in a few vectors each.  past: the call's `arrays` do not fit the card's last cache; 65536 x 768 bf16 with a residual then takes
-// 138 us with its gradients, 160 through the caches, while 8192 x 768 takes 9.2 us (10.9 past them).
+// Rows of `width` entries: the fewest threads that hold one in a few vectors each.  past: the call's `arrays` do not fit the card's last cache (256 MB); 65536 x 768 bf16 with a residual then
+// takes 138 us with its gradients, 160 through the caches, while 8192 x 768 takes 9.2 us (10.9 past them).  More than three vectors a lane cost the gradients a wave of each SIMD: 65536
+// x 1111 bf16 120 us in three, 250 in four.
 struct Shape { int threads, nv, mode; };
 inline Shape shape_of(int width, int dt, long long rows, int arrays) {
   const int n = dt == PRISM_F32 ? 4 : 8, vectors = (width + n - 1) / n;

@@ -4,8 +4,13 @@
 //   loss = sum w l,  l = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(f) - f - 1),  r = exp(logp - old), f = ref - logp;  without old l = -A logp + ...
 //   dl / dlogp = -(r A where r A <= clip(r) A, else 0) + kl (1 - exp(f))
 //
-// A row is one workgroup's.  Its exponentials are taken in base 2 relative to a running maximum m, exp2(c (z - m)), c = s log2 e, every thread with its own, joined at the end: the difference
-// first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  Sums are in 32 bits a thread, what follows from the whole row in 64.
+// A row is one workgroup's (or one wave's, to 4096 logits of bf16).  Its exponentials are taken in base 2 relative to a running maximum m, exp2(c (z - m)), c = s log2 e, every thread with its own, joined
+// at the end: the difference first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  Sums are in 32 bits a thread, what follows from the whole
+// row in 64: a ratio next to where it is cut off decides about a row's gradient.
+//
+// Loss and gradient in one pass hold the row in registers, up to 16384 vectors of 16 bytes, so that it is read once and written once: 8192 x 32768 bf16 172 us (1013 MB, 5.9 TB/s, vector units 72 % busy),
+// 2048 x 131072 203 us (5.0 TB/s: the registers of a CU hold one such row, and nothing reads while it is computed).  Read twice, the second time from the caches: 249 and 266.  Log-probabilities
+// alone, 4096 x 131072: 167 us, 6.4 TB/s.  Two transcendental instructions a logit, four cycles each, are half of what the vector units do.
 #include <cmath>
 
 #include "layer.h"

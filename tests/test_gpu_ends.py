@@ -464,6 +464,53 @@ def test_many_rows(prism):
     assert d.tolist() == [[rows, rows], [0, 0]]
 
 
+def test_arrays_larger_than_the_caches(prism):
+    """Their kernels read past the caches; rows (or columns) are the same bits as in calls of a part of them."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=BF16)   # noqa: E731
+    for v in (32768, 65536, 131072, 66001):
+        rows = (300 << 20) // (2 * v)
+        z, t = make(rows, v), torch.randint(-1, v, (rows,), generator=g, device="cuda")
+        w, old = torch.rand(rows, generator=g, device="cuda"), torch.full((rows,), -12.0, device="cuda")
+        logp, lse = prism.token_logprob(z, t)
+        r = prism.policy_loss(z, t, old_logp=old, weights=w)
+        for a in (0, rows // 2, rows - 70):
+            part = slice(a, a + 70)
+            b = prism.policy_loss(z[part], t[part], old_logp=old[part], weights=w[part])
+            assert torch.equal(r.dlogits[part], b.dlogits) and torch.equal(r.logp[part], b.logp)
+            c = prism.token_logprob(z[part], t[part])
+            assert torch.equal(logp[part], c[0]) and torch.equal(lse[part], c[1])
+    for width in (768, 771, 4096, 4099, 8192):
+        rows = (200 << 20) // (2 * width)
+        x, res = make(rows, width), make(rows, width)
+        weight = torch.rand(width, generator=g, device="cuda")
+        y, total, stats = prism.layer_norm(x, weight, residual=res)
+        dx, dw, db = prism.layer_norm_backward(y, total, stats, weight, dtotal=res)
+        for a in (0, rows // 2, rows - 300):
+            part = slice(a, a + 300)
+            b = prism.layer_norm(x[part], weight, residual=res[part])
+            assert all(torch.equal(p, q) for p, q in zip(b, (y[part], total[part], stats[part])))
+            assert torch.equal(dx[part], prism.layer_norm_backward(y[part], total[part], stats[part], weight, dtotal=res[part])[0])
+        n = (total.double() - stats[:, :1].double()) * stats[:, 1:].double()
+        for got, terms in ((dw, y.double() * n), (db, y.double())):
+            # a thread adds rows / 512 terms at most
+            assert bool(((got.double() - terms.sum(0)).abs() <= (rows // 512 + 40) * E * terms.abs().sum(0)).all())
+    n, rows, width = 70000, 20000, 1000
+    dout, t = make(n, width), torch.randint(-1, rows, (n,), generator=g, device="cuda")
+    d = prism.embedding_backward(dout, t, rows)
+    assert torch.equal(d[:, :520], prism.embedding_backward(dout[:, :520], t, rows))          # (two pieces of 512 columns: tiles of the same length, the same sums)
+
+
+def test_embedding_gradient_of_very_many_pieces(prism):
+    """Tiles of more than 64 tokens: sums of ones are exact."""
+    n, width = 600001, 65536
+    t = (torch.rand(n, generator=torch.Generator().manual_seed(1)) < 0.3).int().cuda()
+    d = prism.embedding_backward(torch.ones(1, width, device="cuda", dtype=BF16).expand(n, width), t, 2, scale=2.0 ** -10)
+    ones = int(t.sum())
+    want = (torch.tensor([n - ones, ones], device="cuda").float() * 2.0 ** -10).to(BF16)
+    assert torch.equal(d, want.view(2, 1).expand(2, width))
+
+
 # ------------------------------------------------------------------------------------------------------- streams and graphs
 
 def _calls(prism, g, dtype):
