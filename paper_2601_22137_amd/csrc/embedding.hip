@@ -32,10 +32,15 @@ template <typename T, bool WHOLE> __device__ inline typename Vec<T>::type load_p
   if constexpr (WHOLE) return *(const typename Vec<T>::type*)(row + c);
   else return load_vector(row, c, width);
 }
-template <typename T, bool WHOLE> __device__ inline void store_piece(T* row, int c, int width, const typename Vec<T>::type& v) {
-  if constexpr (WHOLE) *(typename Vec<T>::type*)(row + c) = v;
+template <typename T, bool WHOLE, bool PAST> __device__ inline void store_piece(T* row, int c, int width, const typename Vec<T>::type& v) {
+  if constexpr (WHOLE && PAST) __builtin_nontemporal_store(v, (typename Vec<T>::type*)(row + c));
+  else if constexpr (WHOLE) *(typename Vec<T>::type*)(row + c) = v;
   else store_vector(row, c, width, v);
 }
+
+// The lookup's result goes past the caches where it fills a quarter of the last one, dout where it and the table fill half of it: 65536 tokens x 768 bf16, 32768 rows, 78 us among others (93 through them).
+// The table's gradient does not: 16384 x 4096 into 131072 rows, with the lookup, 294 us past the caches, 283 through them.
+template <typename T> bool fills(long long rows, int width, int megabytes) { return rows * width * (long long)sizeof(T) > (long long)megabytes << 20; }
 
 struct Lookup {
   const void *table, *tokens;
@@ -45,7 +50,7 @@ struct Lookup {
   float scale;
 };
 
-template <typename T, typename I, bool WHOLE> __global__ void __launch_bounds__(256) embedding_kernel(Lookup p) {
+template <typename T, typename I, bool WHOLE, bool PAST> __global__ void __launch_bounds__(256) embedding_kernel(Lookup p) {
   using V = typename Vec<T>::type;
   constexpr int N = Vec<T>::N, NV = 4;
   const int lane = threadIdx.x & (p.lanes - 1), per = 256 / p.lanes;
@@ -65,7 +70,7 @@ template <typename T, typename I, bool WHOLE> __global__ void __launch_bounds__(
         float o[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) o[e] = there ? (float)v[j][e] * p.scale : 0.0f;
-        store_piece<T, WHOLE>(to, column<T, WHOLE>(first + (j * p.lanes + lane) * N, p.width), p.width, rounded<T>(o));
+        store_piece<T, WHOLE, PAST>(to, column<T, WHOLE>(first + (j * p.lanes + lane) * N, p.width), p.width, rounded<T>(o));
       }
     }
   }
@@ -205,7 +210,7 @@ template <typename T, bool WHOLE> __device__ inline void put(const Sums& p, int 
   float o[Vec<T>::N];
 #pragma unroll
   for (int e = 0; e < Vec<T>::N; ++e) o[e] = sum[e] * p.scale;
-  store_piece<T, WHOLE>((T*)p.dtable + token * p.ts, column<T, WHOLE>(c, p.width), p.width, rounded<T>(o));
+  store_piece<T, WHOLE, false>((T*)p.dtable + token * p.ts, column<T, WHOLE>(c, p.width), p.width, rounded<T>(o));
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -230,7 +235,7 @@ template <typename T, bool WHOLE, bool PAST> __global__ void __launch_bounds__(2
       const bool empty = lane < p.clear && row < p.rows && p.starts[row] == p.starts[row + 1];
       for (unsigned long long left = __ballot(empty); left; left &= left - 1) {
         T* to = (T*)p.dtable + (first + __ffsll((long long)left) - 1) * p.ts;
-        for (int c = lane * N; c < p.width; c += 64 * N) store_piece<T, WHOLE>(to, column<T, WHOLE>(c, p.width), p.width, V{});
+        for (int c = lane * N; c < p.width; c += 64 * N) store_piece<T, WHOLE, false>(to, column<T, WHOLE>(c, p.width), p.width, V{});
       }
     }
     return;
@@ -358,7 +363,8 @@ int tile_of(const prism_embedding_desc& d, int chunks) {
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 template <typename T, typename I> void lookup(const Lookup& p, dim3 grid, hipStream_t s) {
-  hipLaunchKernelGGL((p.width >= Vec<T>::N ? embedding_kernel<T, I, true> : embedding_kernel<T, I, false>), grid, dim3(256), 0, s, p);
+  hipLaunchKernelGGL((p.width < Vec<T>::N ? embedding_kernel<T, I, false, false> : fills<T>(p.count, p.width, 64) ? embedding_kernel<T, I, true, true> : embedding_kernel<T, I, true, false>),
+                     grid, dim3(256), 0, s, p);
 }
 template <typename T> void lookup(const Lookup& p, bool wide, dim3 grid, hipStream_t s) {
   if (wide) lookup<T, int64_t>(p, grid, s);
@@ -366,8 +372,7 @@ template <typename T> void lookup(const Lookup& p, bool wide, dim3 grid, hipStre
 }
 template <typename T> void add_up(const Sums& p, long long tokens, dim3 sums, dim3 joins, hipStream_t s) {
   const bool whole = p.width >= Vec<T>::N;
-  // dout past the caches where it and the table fill half of the last one: 65536 tokens x 768 bf16, 32768 rows, with the lookup 83 us (90 through them)
-  const bool past = (tokens + p.rows) * p.width * (long long)sizeof(T) > (128ll << 20);
+  const bool past = fills<T>(tokens + p.rows, p.width, 128);
   hipLaunchKernelGGL((!whole ? embedding_sums_kernel<T, false, false> : past ? embedding_sums_kernel<T, true, true> : embedding_sums_kernel<T, true, false>), sums, dim3(256), 0, s, p);
   if (joins.x) hipLaunchKernelGGL((whole ? embedding_join_kernel<T, true> : embedding_join_kernel<T, false>), joins, dim3(64 * JOIN_WAVES), 0, s, p);
 }

@@ -54,9 +54,12 @@ template <typename T, int THREADS, int NV, int MODE> struct Row {
         if (at(j) < width && at(j) + N > width) v[j] = __builtin_bit_cast(V, __builtin_bit_cast(unsigned __int128, v[j]) >> ((at(j) + N - width) * (128 / N)));
     }
   }
-  static __device__ void store(T* row, int j, int width, const V& v) {
+  template <bool OVER = false> static __device__ void store(T* row, int j, int width, const V& v) {     // OVER: past the caches in the ..PAST modes
+    if constexpr (MODE == ODD_PAST && OVER) return stream_vector_to(row, at(j), width, v);
     if constexpr (!whole_rows(MODE)) return store_vector(row, at(j), width, v);
-    if (at(j) < width) *(V*)(row + at(j)) = v;
+    if (at(j) >= width) return;
+    if constexpr (MODE == WHOLE_PAST && OVER) __builtin_nontemporal_store(v, (V*)(row + at(j)));
+    else *(V*)(row + at(j)) = v;
   }
 };
 
