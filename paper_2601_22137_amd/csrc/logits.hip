@@ -99,6 +99,7 @@ template <typename T, int THREADS, bool PAST> __device__ inline Sum own_sum(cons
     either<T>(r, [&](auto fused) {
 #pragma unroll
       for (int j = 0; j < K; ++j) {
+        if (first + j * THREADS * N >= p.vocabulary) break;               // (nothing of the row in this piece)
         as_loaded<T>(v[j]);
 #pragma unroll
         for (int e = 0; e < N; ++e) part[e & 3] += exp_of<T, fused.value>(p, r, (float)v[j][e]);
@@ -280,6 +281,7 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   either<T>(own, [&](auto fused) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      if (j * THREADS * N >= p.vocabulary) break;          // (nothing of the row in this piece)
       as_loaded<T>(v[j]);
 #pragma unroll
       for (int e = 0; e < N; ++e) part[e & 3] += exp_of<T, fused.value>(p, own, (float)v[j][e]);
@@ -295,6 +297,7 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   either<T>(r, [&](auto fused) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      if (j * THREADS * N >= p.vocabulary) break;
       as_loaded<T>(v[j]);
       const int width = p.vocabulary - j * THREADS * N;
       const V o = gradient<T, fused.value>(p, r, v[j], at, t - j * THREADS * N, d, factor);
@@ -382,9 +385,12 @@ Logits common(const void* z, const void* tokens, int dt, const prism_logits_desc
   return p;
 }
 
-int threads_of(int vocabulary, int dt) {
+// Threads of a row that is read in pieces, whatever the number of rows, so that a row's results do not depend on what else is in the call.  Sums take four vectors a thread at a time, and fewer threads
+// waste fewer of them (16384 rows of 8000 logits, bf16: 64 threads 44 us, 256 67); the gradients one after the other (256 threads 100 us, 64 111).
+int threads_of(int vocabulary, bool back) {
   const int vectors = (vocabulary + 7) / 8;
-  return vectors <= 512 ? 64 : vectors <= 2048 ? 256 : 512;
+  if (back) return vectors <= 512 ? 64 : vectors <= 2048 ? 256 : 512;
+  return vectors <= 1024 ? 64 : vectors <= 4096 ? 256 : 512;
 }
 
 // Logits that do not fit the card's last cache are read past the caches where they are read once: 4096 x 131072 bf16, log-probabilities alone 165 us (177 through them)
@@ -406,7 +412,8 @@ template <typename T, bool PAST> void (*held_kernel(int vectors, int& threads))(
   if (vectors <= 64 * 8) return threads = 64, vectors <= 64 * 4 ? logits_held_kernel<T, 64, 4, PAST> : logits_held_kernel<T, 64, 8, PAST>;
   if (vectors <= 256 * 8) return threads = 256, vectors <= 256 * 4 ? logits_held_kernel<T, 256, 4, PAST> : logits_held_kernel<T, 256, 8, PAST>;
   if (vectors <= 512 * 8) return threads = 512, logits_held_kernel<T, 512, 8, PAST>;
-  if (vectors <= 1024 * 16) return threads = 1024, vectors <= 1024 * 8 ? logits_held_kernel<T, 1024, 8, PAST> : logits_held_kernel<T, 1024, 16, PAST>;
+  if (vectors <= 512 * 16) return threads = 512, logits_held_kernel<T, 512, 16, PAST>;        // two workgroups a CU: 2684 x 50001 bf16 133 us, with 1024 threads 159
+  if (vectors <= 1024 * 16) return threads = 1024, logits_held_kernel<T, 1024, 16, PAST>;
   return nullptr;
 }
 template <typename T> bool held(const Logits& p, hipStream_t s) {
@@ -419,8 +426,8 @@ template <typename T> bool held(const Logits& p, hipStream_t s) {
 
 void by_type(const Logits& p, int dt, bool back, hipStream_t s) {
   if (!back && p.dz && (dt == PRISM_F32 ? held<float>(p, s) : held<__bf16>(p, s))) return;
-  if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary, dt), back, s);
-  else by_threads<__bf16>(p, threads_of(p.vocabulary, dt), back, s);
+  if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary, back), back, s);
+  else by_threads<__bf16>(p, threads_of(p.vocabulary, back), back, s);
 }
 
 }  // namespace
