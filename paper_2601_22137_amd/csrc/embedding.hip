@@ -8,9 +8,9 @@
 //          tokens: 9.
 //   sums   the sorted tokens are cut into tiles of equal length; a wave adds up the rows of dout of a tile, 64 vectors of 16 bytes wide, eight rows under way, in 32 bits.  A run of equal
 //          tokens that lies in one tile goes straight to the table; what crosses a border is kept as partial sums.  Other waves clear the rows without tokens.  Memory: 65536 x 768
-//          bf16 into 32768 rows 30 us, 161 MB; 16384 x 4096 into 131072 rows 216 us, 1216 MB, most of them zeros (a fill alone runs at 6.8 TB/s).
+//          bf16 into 32768 rows 30 us, 161 MB; 16384 x 4096 into 131072 rows 213 us, 1216 MB, most of them zeros (a fill alone runs at 6.8 TB/s).
 //   join   partial sums of a run in their order, in 64 bits, long runs by eight waves together: 8 to 9 us, a chain of five dependent reads.
-// The lookup: 65536 x 768 from 32768 rows 26 us (154 MB), 16384 x 4096 from 131072 rows 54 us (236 MB, rows at random); a few tokens: 3 us, and the host's call.
+// The lookup: 65536 x 768 from 32768 rows 23 us (147 MB), 16384 x 4096 from 131072 rows 50 us (229 MB, rows at random); a few tokens: 3 us, and the host's call.
 #include "layer.h"
 #include "row_vector.h"
 
