@@ -4,7 +4,7 @@
 //
 // The gradient is a sum over sorted tokens, so that the same call gives the same bits whatever the order in which workgroups run:
 //   sort   a workgroup has a range of the table's rows, about a 256th; it goes through all tokens, counts those of each of its rows and those before its range, keeps its own in LDS and puts
-//          them, 64 at a time, in their places.  Nothing passes between workgroups.  65536 tokens, 32768 rows: 17.6 us, vector units 59 % busy (every workgroup looks at every token); 16384
+//          them, 64 at a time, in their places.  Nothing passes between workgroups.  65536 tokens, 32768 rows: 16.7 us (every workgroup looks at every token, and the one with the commonest has the most to do); 16384
 //          tokens: 9.
 //   sums   the sorted tokens are cut into tiles of equal length; a wave adds up the rows of dout of a tile, 64 vectors of 16 bytes wide, eight rows under way, in 32 bits.  A run of equal
 //          tokens that lies in one tile goes straight to the table; what crosses a border is kept as partial sums.  Other waves clear the rows without tokens.  Memory: 65536 x 768
@@ -89,7 +89,7 @@ template <typename I> __global__ void __launch_bounds__(SORT_THREADS) embedding_
   __shared__ int places[MAX_RANGE * SORT_WAVES];        // [row of the range][wave]: counts, then where the wave's next one goes
   __shared__ int2 lists[SORT_WAVES][LIST];              // the range's tokens among a wave's: (row of the range, index), in their order
   __shared__ int sums[SORT_WAVES];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const unsigned rows = (unsigned)p.rows, first = blockIdx.x * p.range, range = rows - first < p.range ? rows - first : p.range;
   const int slots = range * SORT_WAVES;
   for (int i = threadIdx.x; i < slots; i += SORT_THREADS) places[i] = 0;
@@ -98,15 +98,17 @@ template <typename I> __global__ void __launch_bounds__(SORT_THREADS) embedding_
   const int part = ((p.count + SORT_THREADS - 1) / SORT_THREADS) * 64;
   const int begin = (int)((long long)wave * part < p.count ? wave * part : p.count), end = p.count - begin < part ? p.count : begin + part;
   auto load = [&](int i0, unsigned (&t)[AHEAD]) {
+    if (i0 + 64 * AHEAD <= end) {            // (the same base for all lanes: no arithmetic for addresses)
+      const I* from = (const I*)p.tokens + i0;
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) t[j] = token_at<I>(from, 64 * j + lane);
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       const int i = i0 + 64 * j + lane;
-      t[j] = token_at<I>(p.tokens, i < end ? i : end - 1);
+      t[j] = i < end ? token_at<I>(p.tokens, i) : 0xFFFFFFFFu;
     }
-    if (i0 + 64 * AHEAD <= end) return;
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j)
-      if (i0 + 64 * j + lane >= end) t[j] = 0xFFFFFFFFu;
   };
   int below = 0, listed = 0;                            // of the wave; listed: all of them, also those for which the list has no room
   for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
