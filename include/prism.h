@@ -438,7 +438,7 @@ typedef struct {
   int64_t rows;
   int32_t vocabulary;        /* logits of a row */
   int32_t wide_tokens;
-  double scale;              /* > 0: logits are taken times it (one over the temperature) */
+  double scale;              /* 2^-100 to 2^100: logits are taken times it (one over the temperature) */
   int64_t logits_stride, dlogits_stride;
   /* prism_policy_loss only */
   double clip_low, clip_high; /* the ratio is held between 1 - clip_low and 1 + clip_high */

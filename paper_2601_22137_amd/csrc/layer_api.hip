@@ -108,7 +108,8 @@ int check(const prism_layer_norm_desc* d, int dt) {
 int check(const prism_logits_desc* d, int dt, bool loss) {
   if (!d || !is_type(dt)) return refuse("null description or unknown type");
   if (d->rows < 0 || d->vocabulary < 1) return refuse("negative size, or rows without logits");
-  if (!(d->scale > 0.0) || !std::isnormal((float)d->scale) || !std::isfinite((float)(d->scale * 1.4426950408889634))) return refuse("scale and scale log2(e) have to be positive and in the range of fp32");
+  // (the rest of a rounded factor has to be a normal number too)
+  if (!(d->scale >= std::ldexp(1.0, -100) && d->scale <= std::ldexp(1.0, 100))) return refuse("scale has to be between 2^-100 and 2^100");
   if (bad_stride(d->rows, d->logits_stride, d->dlogits_stride)) return refuse("a stride is negative, or an array ends past 2^60 elements");
   if (loss) {
     if (!(d->clip_low >= 0.0 && d->clip_low <= 1.0) || !(d->clip_high >= 0.0) || !std::isfinite(d->clip_high)) return refuse("clip_low has to be in 0 .. 1, clip_high finite and not negative");

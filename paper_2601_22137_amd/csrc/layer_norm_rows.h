@@ -99,7 +99,7 @@ template <typename T, int THREADS, int NV, int MODE> struct Columns {
 // Rows of `width` entries: the fewest threads that hold one in a few vectors each.  past: the call's `arrays` do not fit the card's last cache (256 MB); 65536 x 768 bf16 with a residual then
 // takes 138 us with its gradients, 160 through the caches, while 8192 x 768 takes 9.2 us (10.9 past them).  More than three vectors a lane cost the gradients a wave of each SIMD: 65536
 // x 1111 bf16 120 us in three, 250 in four.
-struct Shape { int threads, nv, mode; };
+struct Shape { int threads, nv, mode = TINY; };
 inline Shape shape_of(int width, int dt, long long rows, int arrays) {
   const int n = dt == PRISM_F32 ? 4 : 8, vectors = (width + n - 1) / n;
   constexpr Shape whole[] = {{16, 1}, {32, 1}, {32, 3}, {64, 2}, {64, 3}, {256, 1}, {256, 2}, {256, 3}, {1024, 1}, {1024, 2}, {1024, 4}};

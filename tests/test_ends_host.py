@@ -56,7 +56,7 @@ def test_layer_norm_refuses(prism, kw):
     assert L.prism_layer_norm_workspace_bytes(prism.F32, ctypes.byref(d), ctypes.byref(ctypes.c_size_t(0))) == prism.EINVAL
 
 
-@pytest.mark.parametrize("kw", [dict(rows=-1), dict(vocabulary=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=1e-60), dict(scale=3e38), dict(logits_stride=-1),
+@pytest.mark.parametrize("kw", [dict(rows=-1), dict(vocabulary=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=1e-60), dict(scale=1e-31), dict(scale=2e30), dict(scale=3e38), dict(logits_stride=-1),
                                 dict(dlogits_stride=-8)])
 def test_logits_refuse(prism, kw):
     L, d = prism.lib(), _logits(prism, **kw)

@@ -424,6 +424,30 @@ def test_logits_of_the_lowest_value(prism, dtype, v):
     _close(r.dlogits, -ref, bound, "dlogits in one pass")
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1e-6, 300.0, 2.0 ** 60])
+def test_logits_scales_far_from_one(prism, dtype, scale):
+    """Excluded logits stay excluded and probabilities are those of the scaled logits, whatever the scale."""
+    g = torch.Generator().manual_seed(7)
+    z = torch.randn(4, 700, generator=g)
+    z[:, 3::5] = -float("inf")
+    z[1] *= 1.0 / scale if scale < 1e10 else 1.0
+    z[1, 3::5] = -float("inf")
+    z = z.to(dtype).cuda()
+    t = torch.tensor([0, 1, 2, 4], device="cuda")
+    logp, lse = prism.token_logprob(z, t, scale=scale)
+    rlogp, rlse, p = R.logprob(_f64(z), t.tolist(), scale)
+    spread = scale * np.abs(np.where(p > 0, _f64(z), 0.0) - _f64(z).max(1, keepdims=True)) * p
+    # three roundings of each exponent, a thread's sum and the joins; bf16 rounds the factor
+    off = 4 * E * np.where(p > 0, spread, 0.0).sum(1) + 100 * E
+    _close(logp, rlogp, off + 2 * E * np.abs(rlogp), "logp")
+    _close(lse, rlse, off + 2 * E * np.abs(rlse), "lse")
+    d = prism.policy_loss(z, t, scale=scale, weights=torch.ones(4, device="cuda")).dlogits
+    ref = R.logprob_gradient(-np.ones(4), p, t.tolist(), scale)
+    _close(d, ref, _u(dtype) * np.abs(ref) + scale * (4 * E * np.where(p > 0, spread, 0.0) + (off + 10 * E)[:, None] * p + 3 * E * (ref < 0)) + 1e-36, "dlogits")
+    assert not bool(d[:, 3::5].any())
+
+
 def test_offsets_past_32_bits(prism):
     """Rows that lie more than 2^31 elements behind the first."""
     n, width, stride = 40, 264, 1 << 26
