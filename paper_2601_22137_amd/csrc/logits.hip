@@ -357,16 +357,24 @@ __device__ inline double block_sum(double v, double* memory) {
 // One over the number of rows with a token
 __global__ void __launch_bounds__(1024) count_rows_kernel(Logits p) {
   __shared__ double memory[16];
-  double n = 0.0;
-  for (long long row = threadIdx.x; row < p.rows; row += 1024) n += token_of(p, row) >= 0 ? 1.0 : 0.0;
-  n = block_sum(n, memory);
+  int own = 0;
+#pragma unroll 16
+  for (long long row = threadIdx.x; row < p.rows; row += 1024) own += token_of(p, row) >= 0;
+  const double n = block_sum(own, memory);
   if (threadIdx.x == 0) *p.mean = n > 0.0 ? 1.0 / n : 0.0;
 }
 
 __global__ void __launch_bounds__(1024) loss_sum_kernel(Logits p, float* loss) {
   __shared__ double memory[16];
-  double v = 0.0;
-  for (long long row = threadIdx.x; row < p.rows; row += 1024) v += p.losses[row];
+  double v = 0.0, part[8] = {};
+  const long long most = p.rows - p.rows % 8192;
+  for (long long row = threadIdx.x; row < most; row += 8192) {          // eight reads on their way at a time
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[i] += p.losses[row + 1024 * i];
+  }
+  for (long long row = most + threadIdx.x; row < p.rows; row += 1024) v += p.losses[row];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v += part[i];
   v = block_sum(v, memory);
   if (threadIdx.x == 0) *loss = (float)v;
 }
