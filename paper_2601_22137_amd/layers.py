@@ -1,9 +1,11 @@
 """The layer operators for autograd, and the attention half of a transformer layer made of them: the part of a model whose 2-D weights
 optim.muon_orthogonalize updates; and the operators at the ends of a model: embedding, norm of the residual stream, log-probabilities and losses.
 
-Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.  Second derivatives are an error (those of dropout are computed).
+Every step of the operators, gradients included, runs in the HIP kernels; the projections are PyTorch products.  Second derivatives are an error (those of dropout are computed), and so are
+tangents of forward mode.
 """
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import prism
@@ -138,11 +140,16 @@ def _fixed(t, name):
         raise prism.PrismError("%s: there is no gradient for it" % name)
 
 
+def _followed(*tensors):
+    """Whether autograd has to see a call: gradients are on, or an argument has a tangent (no_grad leaves forward mode on), which the functions here refuse."""
+    return torch.is_grad_enabled() or (forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors))
+
+
 def norm_rope(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, start=0, norm=True, interleaved=False, scale=1.0, eps=1e-6):
     """prism.qk_norm_rope of queries and keys (or of one of them) with gradients for them and the weights."""
     _fixed(inv_freq, "inv_freq")
     options = dict(start=start, norm=norm, interleaved=interleaved, scale=scale, eps=eps)
-    if not torch.is_grad_enabled():       # tokens one by one: the host's time counts
+    if not _followed(q, k, q_weight, k_weight, inv_freq):       # tokens one by one: the host's time counts
         return prism.qk_norm_rope(q, k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, positions=positions, **options)
     return _NormRope.apply(q, k, q_weight, k_weight, inv_freq, positions, options)
 
@@ -161,14 +168,14 @@ def dropout(x, p, seed, offset=0, residual=None):
 def embedding(tokens, table, scale=1.0):
     """prism.embedding with a gradient for the table [rows, width]."""
     tokens = tokens.contiguous()
-    if not torch.is_grad_enabled():
+    if not _followed(table):
         return prism.embedding(tokens, table, scale=scale)
     return _Embedding.apply(tokens, table, scale)
 
 
 def layer_norm(x, weight=None, bias=None, residual=None, center=True, eps=1e-5):
     """The norm of the rows of x, or, with a residual, (the norm of their sum, the sum): prism.layer_norm with gradients for x, the residual, weight and bias."""
-    if not torch.is_grad_enabled():
+    if not _followed(x, residual, weight, bias):
         y, total, _ = prism.layer_norm(x, weight, bias, residual=residual, center=center, eps=eps)
         return y if residual is None else (y, total)
     return _LayerNorm.apply(x, residual, weight, bias, center, eps)

@@ -31,3 +31,23 @@ def test_log_probabilities_may_be_written_to_before_the_backward_pass(prism):
     logp.detach().mul_(0.5)
     loss.backward()
     assert z.grad.shape == z.shape
+
+
+def test_tangents_are_not_lost(prism):
+    """no_grad does not turn forward mode off: an argument with a tangent, for which the operators have no derivative, is an error there too."""
+    from paper_2601_22137_amd import layers
+    import torch.autograd.forward_ad as forward
+    x, w, tokens = torch.randn(3, 8), torch.ones(8), torch.zeros(3, dtype=torch.int64)
+    heads, freq = torch.randn(1, 3, 2, 8), torch.ones(4)
+    norm_rope = lambda q=heads, k=heads, qw=w, kw=w, f=freq: layers.norm_rope(q, k, qw, kw, inv_freq=f)   # noqa: E731
+    calls = [(layers.embedding, (tokens, x), 1)] + [(lambda *a: layers.layer_norm(*a), (x, w, w, x), i) for i in range(4)] + [(norm_rope, (heads, heads, w, w, freq), i) for i in range(5)]
+    with forward.dual_level():
+        for call, args, i in calls:
+            dual = list(args)
+            dual[i] = forward.make_dual(args[i], torch.ones_like(args[i]))
+            with torch.no_grad():
+                call(*args)
+                with pytest.raises((NotImplementedError, layers.prism.PrismError), match="jvp|inv_freq"):
+                    call(*dual)
+            with torch.inference_mode():                 # where forward mode is off
+                call(*dual)
