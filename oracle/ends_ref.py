@@ -101,3 +101,21 @@ def policy_rows(logp, there, advantages=None, old=None, ref=None, weights=None, 
             dd[i] += kl * np.exp(f)
         l[i], d[i], dd[i] = w * l[i], w * d[i], abs(w) * dd[i]
     return l, d, dd
+
+
+def logprob_apart(z, tokens, scale):
+    """(logp, 1 - p of the token, p of all) with the token's own term apart from the others', so that a token next to certain keeps its digits; 0 where the token is not in the vocabulary.  Rows
+    have a finite logit at the token."""
+    n, v = z.shape
+    logp, rest, p = np.zeros(n), np.zeros(n), np.zeros((n, v))
+    for i, t in enumerate(tokens):
+        if not 0 <= t < v:
+            continue
+        a = scale * z[i]
+        e = np.exp(a - a[t])                               # odds against the token, one by one
+        e[t] = 0.0
+        odds = e.sum()
+        logp[i], rest[i] = -np.log1p(odds), odds / (1.0 + odds)
+        e[t] = 1.0
+        p[i] = e / (1.0 + odds)
+    return logp, rest, p

@@ -1,12 +1,14 @@
 // What is computed from rows of logits and one token of each: its log-probability, losses of it, and the logits' gradients.
 //
 //   logp = s z_t - lse, lse = log sum_j exp(s z_j);   dz_j = s d ([j = t] - exp(s z_j - lse)), d = the derivative of the loss by logp
+//   with o = sum over j other than t of exp(s (z_j - z_t)):   logp = -log(1 + o), 1 - p_t = o / (1 + o), dz_t = s d (1 - p_t)
 //   loss = sum w l,  l = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(f) - f - 1),  r = exp(logp - old), f = ref - logp;  without old l = -A logp + ...
 //   dl / dlogp = -(r A where r A <= clip(r) A, else 0) + kl (1 - exp(f))
 //
 // A row is one workgroup's (or one wave's, to 4096 logits of bf16).  Its exponentials are taken in base 2 relative to a running maximum m, exp2(c (z - m)), c = s log2 e, every thread with its own, joined
-// at the end: the difference first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  Sums are in 32 bits a thread, what follows from the whole
-// row in 64: a ratio next to where it is cut off decides about a row's gradient.
+// at the end: the difference first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  The sum is over the others than the token, and in 32 bits to its
+// end, joins too: as a token next to certain has 1 - p_t from it, not what is left of 1, its errors are relative to 1 - p_t and to logp.  What follows from it is in 64 bits: a ratio next to where
+// it is cut off decides about a row's gradient.
 //
 // Loss and gradient in one pass hold the row in registers, up to 16384 vectors of 16 bytes, so that it is read once and written once: 8192 x 32768 bf16 172 us (1013 MB, 5.9 TB/s, vector units 72 % busy),
 // 2048 x 131072 203 us (5.0 TB/s: the registers of a CU hold one such row, and nothing reads while it is computed).  Read twice, the second time from the caches: 249 and 266.  Log-probabilities
@@ -31,6 +33,8 @@ struct Logits {
   double low, high, kl, exact_scale;
   bool wide;
 };
+
+constexpr double LN2 = 0.69314718055994530942;
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -79,8 +83,23 @@ struct Sum {
   }
 };
 
-// The sum over a row that is read in pieces of K vectors a thread, all on their way before the first is used
-template <typename T, int THREADS, bool PAST> __device__ inline Sum own_sum(const Logits& p, const T* z) {
+// Entry `at` of a vector, if it has one.  By words: entries of 16 bits, one by one, take twice the instructions.
+template <typename T> __device__ inline void set_entry(typename Vec<T>::type& v, int at, float x) {
+  typedef unsigned words __attribute__((ext_vector_type(4)));
+  words w = __builtin_bit_cast(words, v);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = i == at ? __builtin_bit_cast(unsigned, x) : w[i];
+  } else {
+    const unsigned stays = at & 1 ? 0x0000FFFFu : 0xFFFF0000u, put = __builtin_bit_cast(unsigned short, (T)x) * 0x10001u & ~stays;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = i == at >> 1 ? (w[i] & stays) | put : w[i];
+  }
+  v = __builtin_bit_cast(typename Vec<T>::type, w);
+}
+
+// The sum over a row without its token t.  The row is read in pieces of K vectors a thread, all on their way before the first is used.
+template <typename T, int THREADS, bool PAST> __device__ inline Sum own_sum(const Logits& p, const T* z, int t) {
   constexpr int N = Vec<T>::N, K = 4;
   using V = typename Vec<T>::type;
   Sum a;
@@ -88,6 +107,11 @@ template <typename T, int THREADS, bool PAST> __device__ inline Sum own_sum(cons
     V v[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) v[j] = load_vector<T, PAST>(z + first + j * THREADS * N, (int)threadIdx.x * N, p.vocabulary - first - j * THREADS * N, -INFINITY);
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int place = t - first - j * THREADS * N;                      // the same in all threads: one piece has it
+      if ((unsigned)place < (unsigned)(THREADS * N)) set_entry<T>(v[j], place - (int)threadIdx.x * N, -INFINITY);
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < K; ++j)
@@ -123,8 +147,6 @@ template <typename T, int THREADS> __device__ inline Sum whole_row(const Logits&
   return b;
 }
 
-constexpr double LN2 = 0.69314718055994530942;
-
 __device__ inline int token_of(const Logits& p, long long row) {
   const long long t = p.wide ? ((const long long*)p.tokens)[row] : (long long)((const int*)p.tokens)[row];
   return t >= 0 && t < p.vocabulary ? (int)t : -1;
@@ -136,7 +158,7 @@ struct Given {
   float weight, advantage, old, ref;
 };
 __device__ inline Given given_for(const Logits& p, long long row) {
-  Given g = {token_of(p, row), 0.0f, 1.0f, 0.0f, 0.0f};
+  Given g = {__builtin_amdgcn_readfirstlane(token_of(p, row)), 0.0f, 1.0f, 0.0f, 0.0f};
   if (p.weights) g.weight = p.weights[row];
   if (p.advantages) g.advantage = p.advantages[row];
   if (p.old) g.old = p.old[row];
@@ -144,10 +166,43 @@ __device__ inline Given given_for(const Logits& p, long long row) {
   return g;
 }
 
-// What one thread computes of a row: its results, and the derivative of the loss by logp.  z: the logit of the token
+// exp2(c (x - y)), x <= y, good to what the instruction is, 1 ulp in 32 bits, however far they are apart: with what the roundings of the difference, of the factor and of their product left over
+__device__ inline float exp_of_difference(const Logits& p, float x, float y) {
+  const float d = x - y, back = d - x, rest = (x - (d - back)) - (y + back), k = d * p.c;
+  return k < -150.0f ? 0.0f : exp2_of(k) * fmaf(fmaf(d, p.c, -k) + fmaf(d, p.c_rest, rest * p.c), (float)LN2, 1.0f);
+}
+
+// The sum over a row's other logits beside its token's exponential e = exp(-|s (m - z)|), which is as good as that sum.  z: the logit of the token
+struct Others {
+  float e;
+  bool above;                   // one of them is, m > z: everything relative to m then, to z otherwise
+  __device__ Others(const Logits& p, const Sum& a, float z) : above(a.m > z) { e = above ? exp_of_difference(p, z, a.m) : exp_of_difference(p, a.m, z); }
+  // all of them, less 1
+  __device__ float rest(const Sum& a) const { return above ? (a.s - 1.0f) + e : a.s * e; }
+  // 1 - p_t
+  __device__ float share(const Sum& a) const { return (above ? a.s : a.s * e) * __builtin_amdgcn_rcpf(1.0f + rest(a)); }
+  // logp = -max(0, s (m - z)) - this, log(1 + y): next to 0 the series, off by y^3 / 4 = 2e-13 of it (the library's log1p takes a dozen registers more)
+  __device__ double log_of_all(const Sum& a) const {
+    const float y = rest(a);
+    return y < 1e-4f ? (double)(y * (1.0f - y * (0.5f - y * (1.0f / 3.0f)))) : log(1.0 + (double)y);
+  }
+};
+
+// What one thread computes of a row: its results, and the gradient at the token, s d (1 - p_t)
 __device__ inline float finish_row(const Logits& p, long long row, const Given& g, int count, const Sum& a, float z) {
-  const double logs = log((double)a.s), lse = a.m == -INFINITY ? -INFINITY : a.m * p.exact_scale + logs;
-  const double logp = z == -INFINITY ? -INFINITY : ((double)z - a.m) * p.exact_scale - logs;
+  double logp, lse;
+  float share;
+  if (a.s == 0.0f) {            // no others
+    logp = z == -INFINITY ? -INFINITY : 0.0;
+    lse = z * p.exact_scale;
+    share = z == -INFINITY ? 1.0f : 0.0f;
+  } else {
+    const Others o(p, a, z);
+    share = o.share(a);
+    const double l = o.log_of_all(a);
+    logp = 0.0 - (o.above ? ((double)a.m - z) * p.exact_scale + l : l);
+    lse = (o.above ? a.m : z) * p.exact_scale + l;
+  }
   if (p.logp) p.logp[row] = (float)logp;
   if (p.lse) p.lse[row] = (float)lse;
   if (!p.losses) return 0.0f;
@@ -177,7 +232,7 @@ __device__ inline float finish_row(const Logits& p, long long row, const Given& 
   }
   p.losses[row] = l;
   if (p.dlogp) p.dlogp[row] = (float)d;
-  return (float)d;
+  return (float)d * p.scale * share;
 }
 
 // Rows with a token, by the whole workgroup
@@ -201,22 +256,18 @@ template <typename T> __device__ inline void clear_row(const Logits& p, long lon
   for (int at = threadIdx.x * Vec<T>::N; at < p.vocabulary; at += threads * Vec<T>::N) store_vector(dz, at, p.vocabulary, typename Vec<T>::type{});
 }
 
-// A vector of the gradient: [j = t] d - exp2(c (z - m)) factor; factor has the reference's rest in it
+// A vector of the gradient, the token's entry aside: -exp2(c (z - m)) factor; factor has the reference's rest in it
 template <typename T, bool FUSED>
-__device__ inline typename Vec<T>::type gradient(const Logits& p, const Reference& r, const typename Vec<T>::type& v, int at, int t, float d, float factor) {
+__device__ inline typename Vec<T>::type gradient(const Logits& p, const Reference& r, const typename Vec<T>::type& v, float factor) {
   constexpr int N = Vec<T>::N;
   float g[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) g[e] = exp_of<T, FUSED>(p, r, (float)v[e]) * -factor;
-  if ((unsigned)(t - at) < (unsigned)N) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) g[e] += at + e == t ? d : 0.0f;
-  }
   return rounded<T>(g);
 }
 
 template <typename T, int THREADS, bool GRAD, bool PAST>
-__global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) logits_kernel(Logits p) {
   constexpr int N = Vec<T>::N;
   __shared__ float2 memory[THREADS / 64];
   __shared__ float result;
@@ -231,17 +282,28 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(Logits p) {
     }
     const T* z = (const T*)p.z + row * p.zs;
     const float zt = (float)z[t];
-    const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, PAST>(p, z), memory);
+    const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, PAST>(p, z, t), memory);
     if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
     if constexpr (GRAD) {
       __syncthreads();
       const Reference r(p, a.reference(), sizeof(T) == 2);
-      const float d = result * p.scale, factor = a.s > 0.0f ? d / a.s * r.rest : 0.0f;
+      const float own = result, factor = a.s > 0.0f ? own / a.s * r.rest : 0.0f;
       T* dz = (T*)p.dz + row * p.ds;
       either<T>(r, [&](auto fused) {
-#pragma unroll 4
-        for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
-          store_vector(dz, at, p.vocabulary, gradient<T, fused.value>(p, r, load_vector(z, at, p.vocabulary, -INFINITY), at, t, d, factor));
+        for (int first = 0; first < p.vocabulary; first += 4 * THREADS * N) {
+          typename Vec<T>::type v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = load_vector(z + first + j * THREADS * N, (int)threadIdx.x * N, p.vocabulary - first - j * THREADS * N, -INFINITY);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int width = p.vocabulary - first - j * THREADS * N, place = t - first - j * THREADS * N;
+            if (width <= 0) break;
+            as_loaded<T>(v[j]);
+            typename Vec<T>::type o = gradient<T, fused.value>(p, r, v[j], factor);
+            if ((unsigned)place < (unsigned)(THREADS * N)) set_entry<T>(o, place - (int)threadIdx.x * N, own);
+            store_vector(dz + first + j * THREADS * N, (int)threadIdx.x * N, width, o);
+          }
+        }
       });
       __syncthreads();
     }
@@ -272,6 +334,11 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   const int count = count_rows<THREADS>(p);         // (while the row is under way)
   float top = -INFINITY, part[4] = {};
 #pragma unroll
+  for (int j = 0; j < NV; ++j) {                    // the sum is over the others than the token
+    const int place = t - j * THREADS * N;
+    if ((unsigned)place < (unsigned)(THREADS * N)) set_entry<T>(v[j], place - at, -INFINITY);
+  }
+#pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int e = 0; e < N; ++e) top = fmaxf(top, (float)v[j][e]);
@@ -292,15 +359,16 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
   __syncthreads();
   const Reference r(p, a.reference(), sizeof(T) == 2);
-  const float d = result * p.scale, factor = a.s > 0.0f ? d / a.s * r.rest : 0.0f;
+  const float token = result, factor = a.s > 0.0f ? token / a.s * r.rest : 0.0f;
   T* dz = (T*)p.dz + row * p.ds;
   either<T>(r, [&](auto fused) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if (j * THREADS * N >= p.vocabulary) break;
       as_loaded<T>(v[j]);
-      const int width = p.vocabulary - j * THREADS * N;
-      const V o = gradient<T, fused.value>(p, r, v[j], at, t - j * THREADS * N, d, factor);
+      const int width = p.vocabulary - j * THREADS * N, place = t - j * THREADS * N;
+      V o = gradient<T, fused.value>(p, r, v[j], factor);
+      if ((unsigned)place < (unsigned)(THREADS * N)) set_entry<T>(o, place - at, token);
       if constexpr (PAST) stream_vector_to(dz + j * THREADS * N, at, width, o);
       else store_vector(dz + j * THREADS * N, at, width, o);
     }
@@ -311,11 +379,14 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
 constexpr float MOST_LSE = 64.0f;
 
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) logprob_backward_kernel(Logits p) {
-  constexpr int N = Vec<T>::N;
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(6))) logprob_backward_kernel(Logits p) {
+  constexpr int N = Vec<T>::N, K = 4;
+  using V = typename Vec<T>::type;
   __shared__ float2 memory[THREADS / 64];
+  __shared__ float sums[THREADS / 32];
+  int turn = 0;
   for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
-    const int t = token_of(p, row);
+    const int t = __builtin_amdgcn_readfirstlane(token_of(p, row));
     if (t < 0) {
       clear_row<T>(p, row, THREADS);
       continue;
@@ -323,23 +394,57 @@ __global__ void __launch_bounds__(THREADS) logprob_backward_kernel(Logits p) {
     const T* z = (const T*)p.z + row * p.zs;
     T* dz = (T*)p.dz + row * p.ds;
     const float d = p.dlogp[row] * p.scale, lse = p.lse[row];
-    float m, factor;
-    if (fabsf(lse) <= MOST_LSE) {        // the reference is lse / s, rounded; the factor makes up for its rounding
+    const bool given = fabsf(lse) <= MOST_LSE;
+    float m, factor, token;
+    if (given) {                         // the reference is lse / s, rounded; the factor makes up for its rounding
       const double exact = (double)lse / p.exact_scale;
       m = (float)exact;
       factor = d * exp2_of((float)((m - exact) * p.c));
-    } else {                             // lse itself is rounded by too much: its sum once more
-      const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, false>(p, z), memory);
+    } else {                             // lse itself is rounded by too much: the sum once more
+      const float zt = (float)z[t];      // (before the barriers, and dlogits may be the logits)
+      const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, false>(p, z, t), memory);
       m = a.reference();
-      factor = a.s > 0.0f ? d / a.s : 0.0f;
+      token = a.s > 0.0f ? d * Others(p, a, zt).share(a) : zt == -INFINITY ? d : 0.0f;
+      factor = a.s > 0.0f ? token / a.s : 0.0f;
     }
     const Reference r(p, m, sizeof(T) == 2);
     factor *= r.rest;
+    float part[4] = {}, zt = 0.0f;       // of the others' exponentials; the token's logit, in the thread that has it
     either<T>(r, [&](auto fused) {
-#pragma unroll 4
-      for (int at = threadIdx.x * N; at < p.vocabulary; at += THREADS * N)
-        store_vector(dz, at, p.vocabulary, gradient<T, fused.value>(p, r, load_vector(z, at, p.vocabulary, -INFINITY), at, t, d, factor));
+      for (int first = 0; first < p.vocabulary; first += K * THREADS * N) {
+        V v[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) v[j] = load_vector(z + first + j * THREADS * N, (int)threadIdx.x * N, p.vocabulary - first - j * THREADS * N, -INFINITY);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          const int width = p.vocabulary - first - j * THREADS * N, place = t - first - j * THREADS * N;
+          if (width <= 0) break;
+          as_loaded<T>(v[j]);
+          if ((unsigned)place < (unsigned)(THREADS * N)) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) zt = e == place - (int)threadIdx.x * N ? (float)v[j][e] : zt;
+            set_entry<T>(v[j], place - (int)threadIdx.x * N, -INFINITY);
+          }
+          float g[N];
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            g[e] = exp_of<T, fused.value>(p, r, (float)v[j][e]);
+            part[e & 3] += g[e];
+            g[e] *= -factor;
+          }
+          store_vector(dz + first + j * THREADS * N, (int)threadIdx.x * N, width, rounded<T>(g));
+        }
+      }
     });
+    // the token's by the thread that had it: d times the others' share of all, in which the rounding of lse is no more
+    const float others = given ? row_sum<THREADS>((part[0] + part[1]) + (part[2] + part[3]), sums, turn++) : 0.0f;
+    if (t / N % THREADS == (int)threadIdx.x) {
+      if (given) {
+        either<T>(r, [&](auto fused) { token = exp_of<T, fused.value>(p, r, zt); });
+        token = d * (others / (others + token));
+      }
+      dz[t] = (T)token;
+    }
   }
 }
 

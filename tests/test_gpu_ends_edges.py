@@ -1,0 +1,104 @@
+"""Operators at the ends of a model where their numbers are hardest: tokens next to certain.
+
+E = 2^-24 is the relative error of a rounding to fp32, U that of one to the type of the arrays."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ends_ref as R
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+E = 2.0 ** -24
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def prism():
+    from paper_2601_22137_amd import prism as P
+    P.lib()
+    return P
+
+
+def _u(dtype):
+    return 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+
+
+def _f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _within(got, ref, bound, what):
+    got = _f64(got)
+    assert got.shape == ref.shape and np.all(np.isfinite(got)), what
+    off = np.abs(got - ref) / np.maximum(bound, 1e-300)
+    assert off.max(initial=0.0) <= 1.0, (what, float(off.max()), np.unravel_index(off.argmax(), off.shape))
+
+
+# ------------------------------------------------------------------------------------------------- tokens next to certain
+
+def _likely(rows, v, dtype, scale):
+    """Rows whose token is 8 to 24 nats above the sum of the others; the first token, the last, one next to the last whole vector, some in the middle."""
+    g = torch.Generator().manual_seed(rows + v)
+    z = (2.0 * torch.randn(rows, v, generator=g)).to(dtype).double()
+    t = torch.randint(0, v, (rows,), generator=g)
+    t[0], t[1], t[2] = 0, v - 1, max(v - 9, 0)
+    at = torch.arange(rows)
+    z[at, t] = -INF
+    z[at, t] = (torch.logsumexp(scale * z, 1) + torch.linspace(8.0, 24.0, rows, dtype=torch.float64)) / scale
+    return z.to(dtype).cuda(), t.cuda()
+
+
+def _off_others(z, tokens, scale, v):
+    """(what the sum of a row's other exponentials may be off by, relative; the distances of the logits from the others' largest; that).
+
+    An exponential is off by its exponent's roundings (difference, factor, product: 3 E of it) and the instruction's, 3 E.  A thread adds up to v / 64 or v / (4 * 512) of them in vectors of
+    four, 8 E each with what it raises its reference by; 16 joins of 5 E."""
+    a = scale * z
+    a[np.arange(len(a)), tokens] = -INF
+    top = a.max(1, keepdims=True)
+    far = np.where(np.isfinite(a), top - np.where(np.isfinite(a), a, 0.0), 0.0)
+    w = np.where(np.isfinite(a), np.exp(-far), 0.0)
+    vectors = max(v / (64 * 4) if v <= 8192 else v / (256 * 4) if v <= 32768 else v / (512 * 4), 1.0)
+    return E * (3 * (w * far).sum(1) / w.sum(1) + 8 * (vectors + 1) + 83), far, top[:, 0]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+@pytest.mark.parametrize("rows,v", [(12, 2), (40, 64), (23, 1000), (9, 5000), (8, 32768), (7, 50001), (5, 131080)])
+def test_tokens_next_to_certain(prism, dtype, scale, rows, v):
+    """logp, 1 - p and the token's gradient keep their relative precision, whatever is left of 1: they follow from the sum of the others."""
+    z, t = _likely(rows, v, dtype, scale)
+    at, tokens = np.arange(rows), t.cpu().numpy()
+    logp_ref, rest, p = R.logprob_apart(_f64(z), tokens.tolist(), scale)
+    off, far, top = _off_others(_f64(z), tokens, scale, v)
+    # the sum, the token's exponential beside it (3 E), the result
+    off_logp = (off + 5 * E) * np.abs(logp_ref)
+    lse_ref = scale * _f64(z)[at, tokens] - logp_ref
+    logp, lse = prism.token_logprob(z, t, scale=scale)
+    _within(logp, logp_ref, off_logp, "logp")
+    assert bool((logp < 0).all())
+    _within(lse, lse_ref, off_logp + E * np.abs(lse_ref), "lse")
+
+    def gradient(d):
+        g = R.logprob_gradient(d, p, tokens.tolist(), scale)
+        g[at, tokens] = scale * d * rest
+        return g
+    # in one pass with the loss: 3 E of an exponent; the sum, and 1 - p, which is in error by the sum's error; ten roundings of factors and the result's
+    d = torch.linspace(0.5, 1.5, rows).cuda()
+    r = prism.policy_loss(z, t, weights=d, scale=scale)
+    ref = gradient(-_f64(d))
+    relative = 3 * E * far + (2 * off + 10 * E)[:, None] + _u(dtype)
+    relative[at, tokens] = off + 10 * E + _u(dtype)
+    _within(r.logp, logp_ref, off_logp, "logp of the loss")
+    _within(r.loss.view(1), np.array([-(_f64(d) * logp_ref).sum()]), (_f64(d) * off_logp).sum() + E * (_f64(d) * np.abs(logp_ref)).sum(), "loss")
+    _within(r.dlogits, ref, relative * np.abs(ref) + 1e-37, "dlogits of the loss")
+    # from lse, which is rounded: all of a row by the same factor; distances from it rather than from the others' largest.  The token's is the others' share, added up like their sum and without that factor.
+    ref = gradient(_f64(d))
+    further = 3 * E * np.abs(lse_ref - top)
+    relative = 3 * E * far + (2 * off + further + E * np.abs(lse_ref) + 10 * E)[:, None] + _u(dtype)
+    relative[at, tokens] = off + further + 10 * E + _u(dtype)
+    _within(prism.token_logprob_backward(d, z, t, lse, scale=scale), ref, relative * np.abs(ref) + 1e-37, "dlogits")
+    place = z.clone()
+    assert torch.equal(prism.token_logprob_backward(d, z, t, lse, scale=scale), prism.token_logprob_backward(d, place, t, lse, scale=scale, out=place))
