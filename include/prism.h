@@ -452,8 +452,8 @@ typedef struct {
 } prism_logits_desc;
 
 /* logp[row] = scale * logits[row][token] - lse[row], lse = the logarithm of the sum of exp(scale * logits[row]), fp32 (either may be NULL).  A row whose token is not in 0 .. vocabulary - 1
- * (padding) is not read: 0 in both.  Logits may be -inf (excluded: probability 0; logp -inf if it is the token's), but neither +inf nor NaN; scale times them has to stay
- * in the range of fp32.  logp, and the gradients at the token, follow from the sum over the other logits: a token next to certain keeps its digits (logp is never above 0). */
+ * (padding) is not read: 0 in both.  Logits may be -inf (excluded: probability 0; logp -inf if it is the token's), +inf and NaN
+ * give NaN in all of their row; scale times them has to stay in the range of fp32.  logp, and the gradients at the token, follow from the sum over the other logits: a token next to certain keeps its digits (logp is never above 0). */
 int prism_token_logprob(const void* logits, const void* tokens, float* logp, float* lse, prism_dtype dt, const prism_logits_desc* desc, void* stream);
 /* dlogits = scale * dlogp[row] * ([j is the token] - exp(scale * logits[row][j] - lse[row])), rounded once; zeros in rows without a token (whose dlogp is not read).  lse as the
  * forward call gave it.  dlogits may be logits with the same stride. */

@@ -188,14 +188,17 @@ struct Others {
   }
 };
 
+__device__ inline float share_of_one(float z) { return z == -INFINITY ? 1.0f : z - z; }         // no others: 0, and NaN stays
+__device__ inline float share_of(const Logits& p, const Sum& a, float z) { return a.s == 0.0f ? share_of_one(z) : Others(p, a, z).share(a); }
+
 // What one thread computes of a row: its results, and the gradient at the token, s d (1 - p_t)
 __device__ inline float finish_row(const Logits& p, long long row, const Given& g, int count, const Sum& a, float z) {
   double logp, lse;
   float share;
   if (a.s == 0.0f) {            // no others
-    logp = z == -INFINITY ? -INFINITY : 0.0;
+    share = share_of_one(z);
+    logp = z == -INFINITY ? -INFINITY : share;
     lse = z * p.exact_scale;
-    share = z == -INFINITY ? 1.0f : 0.0f;
   } else {
     const Others o(p, a, z);
     share = o.share(a);
@@ -212,7 +215,7 @@ __device__ inline float finish_row(const Logits& p, long long row, const Given& 
     const double A = g.advantage;
     if (p.old) {
       const double r = exp(logp - g.old), low = 1.0 - p.low, high = 1.0 + p.high, held = (r < low ? low : r > high ? high : r) * A, free = r * A;
-      if (free <= held) {
+      if (free <= held || r != r || A != A) {
         l = -free;
         d = -free;
       } else {
@@ -234,6 +237,14 @@ __device__ inline float finish_row(const Logits& p, long long row, const Given& 
   if (p.dlogp) p.dlogp[row] = (float)d;
   return (float)d * p.scale * share;
 }
+
+// The token's logit; +inf is no number here, as it is among the others (inf less inf)
+template <typename T> __device__ inline float logit_of(const T* z, int t) {
+  const float x = (float)z[t];
+  return x < INFINITY ? x : NAN;
+}
+// What the exponentials of the others are multiplied by; no others: 0, and NaN as ever where the token's gradient is
+__device__ inline float factor_of(const Sum& a, float token) { return a.s == 0.0f ? 0.0f * token : token / a.s; }
 
 // Rows with a token, by the whole workgroup
 template <int THREADS> __device__ inline int count_rows(const Logits& p) {
@@ -281,13 +292,13 @@ __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4)
       continue;
     }
     const T* z = (const T*)p.z + row * p.zs;
-    const float zt = (float)z[t];
+    const float zt = logit_of(z, t);
     const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, PAST>(p, z, t), memory);
     if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
     if constexpr (GRAD) {
       __syncthreads();
       const Reference r(p, a.reference(), sizeof(T) == 2);
-      const float own = result, factor = a.s > 0.0f ? own / a.s * r.rest : 0.0f;
+      const float own = result, factor = factor_of(a, own) * r.rest;
       T* dz = (T*)p.dz + row * p.ds;
       either<T>(r, [&](auto fused) {
         for (int first = 0; first < p.vocabulary; first += 4 * THREADS * N) {
@@ -326,7 +337,7 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
     return;
   }
   const T* z = (const T*)p.z + row * p.zs;
-  const float zt = (float)z[t];
+  const float zt = logit_of(z, t);
   const int at = (int)threadIdx.x * N;       // in each of NV pieces of the row, whose beginnings all lanes share: one offset takes fewer registers than NV
   V v[NV];
 #pragma unroll
@@ -359,7 +370,7 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   if (threadIdx.x == 0) result = finish_row(p, row, g, count, a, zt);
   __syncthreads();
   const Reference r(p, a.reference(), sizeof(T) == 2);
-  const float token = result, factor = a.s > 0.0f ? token / a.s * r.rest : 0.0f;
+  const float token = result, factor = factor_of(a, token) * r.rest;
   T* dz = (T*)p.dz + row * p.ds;
   either<T>(r, [&](auto fused) {
 #pragma unroll
@@ -401,11 +412,11 @@ __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(6)
       m = (float)exact;
       factor = d * exp2_of((float)((m - exact) * p.c));
     } else {                             // lse itself is rounded by too much: the sum once more
-      const float zt = (float)z[t];      // (before the barriers, and dlogits may be the logits)
+      const float zt = logit_of(z, t);   // (before the barriers, and dlogits may be the logits)
       const Sum a = whole_row<T, THREADS>(p, own_sum<T, THREADS, false>(p, z, t), memory);
       m = a.reference();
-      token = a.s > 0.0f ? d * Others(p, a, zt).share(a) : zt == -INFINITY ? d : 0.0f;
-      factor = a.s > 0.0f ? token / a.s : 0.0f;
+      token = d * share_of(p, a, zt);
+      factor = factor_of(a, token);
     }
     const Reference r(p, m, sizeof(T) == 2);
     factor *= r.rest;

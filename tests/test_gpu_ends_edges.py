@@ -1,4 +1,4 @@
-"""Operators at the ends of a model where their numbers are hardest: tokens next to certain.
+"""Operators at the ends of a model where their numbers are hardest: tokens next to certain, and logits that are no numbers.
 
 E = 2^-24 is the relative error of a rounding to fp32, U that of one to the type of the arrays."""
 import numpy as np
@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 BF16, F32 = torch.bfloat16, torch.float32
 E = 2.0 ** -24
-INF = float("inf")
+INF, NAN = float("inf"), float("nan")
 
 
 @pytest.fixture(scope="module")
@@ -102,3 +102,45 @@ def test_tokens_next_to_certain(prism, dtype, scale, rows, v):
     _within(prism.token_logprob_backward(d, z, t, lse, scale=scale), ref, relative * np.abs(ref) + 1e-37, "dlogits")
     place = z.clone()
     assert torch.equal(prism.token_logprob_backward(d, z, t, lse, scale=scale), prism.token_logprob_backward(d, place, t, lse, scale=scale, out=place))
+
+
+# --------------------------------------------------------------------------------------------------- what is no number
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("v", [2, 40, 5000, 65544, 131080])
+def test_rows_with_logits_that_are_no_numbers(prism, dtype, v):
+    """A NaN or +inf among a row's logits is NaN in all that the row has, its whole gradient among it, and in no other row."""
+    g = torch.Generator().manual_seed(v)
+    z, t = torch.randn(8, v, generator=g).to(dtype).cuda(), torch.randint(0, v, (8,), generator=g)
+    clean = z.clone()
+    other = (t + 1) % v
+    z[1, other[1]], z[2, other[2]], z[3, t[3]], z[4, t[4]] = NAN, INF, NAN, INF
+    z[6] = -INF
+    z[6, t[6]] = NAN
+    t[7], z[7] = -1, NAN
+    t, bad, good = t.cuda(), [1, 2, 3, 4, 6], [0, 5]
+    logp, lse = prism.token_logprob(z, t)
+    want = prism.token_logprob(clean, t)
+    d = prism.token_logprob_backward(torch.ones(8, device="cuda"), z, t, lse)
+    assert bool(logp[bad].isnan().all()) and bool(lse[bad].isnan().all()) and bool(d[bad].isnan().all())
+    assert torch.equal(logp[good], want[0][good]) and torch.equal(lse[good], want[1][good]) and logp[7] == 0 and lse[7] == 0
+    assert torch.equal(d[good], prism.token_logprob_backward(torch.ones(8, device="cuda"), clean, t, lse)[good]) and not bool(d[7].any())
+    given = dict(advantages=torch.linspace(-1, 1, 8).cuda(), old_logp=want[0] - 0.1, ref_logp=want[0] + 0.1, kl=0.1)
+    for kw in ({}, given, dict(given, kl=0.0)):
+        r, c = prism.policy_loss(z, t, **kw), prism.policy_loss(clean, t, **kw)
+        assert bool(r.loss.isnan()) and bool(r.dlogits[bad].isnan().all()) and torch.equal(r.dlogits[good], c.dlogits[good]) and not bool(r.dlogits[7].any())
+        assert bool(r.dlogp[bad].isnan().all()) if kw else torch.equal(r.dlogp, c.dlogp)         # without a ratio it does not depend on logp
+        assert torch.equal(r.dlogp[good], c.dlogp[good]) and bool(r.logp[bad].isnan().all())
+
+
+def test_ratios_that_are_no_numbers(prism):
+    """An advantage or an old log-probability that is no number is one in the gradient; an infinite ratio without an advantage adds nothing."""
+    z, t = torch.randn(4, 30, device="cuda"), torch.arange(4, device="cuda")
+    logp, _ = prism.token_logprob(z, t)
+    old, a = logp.clone(), torch.ones(4, device="cuda")
+    old[1], a[2], old[3], a[3] = NAN, NAN, -INF, 0.0
+    r = prism.policy_loss(z, t, advantages=a, old_logp=old, weights=torch.ones(4, device="cuda"))
+    assert r.dlogp.isnan().tolist() == [False, True, True, False] and r.dlogits.isnan().all(1).tolist() == [False, True, True, False]
+    assert r.dlogp[3] == 0 and not bool(r.dlogits[3].any())
+    r = prism.policy_loss(z[3:], t[3:], advantages=a[3:], old_logp=old[3:])
+    assert r.loss == 0
