@@ -456,7 +456,7 @@ typedef struct {
  * give NaN in all of their row; scale times them has to stay in the range of fp32.  logp, and the gradients at the token, follow from the sum over the other logits: a token next to certain keeps its digits (logp is never above 0). */
 int prism_token_logprob(const void* logits, const void* tokens, float* logp, float* lse, prism_dtype dt, const prism_logits_desc* desc, void* stream);
 /* dlogits = scale * dlogp[row] * ([j is the token] - exp(scale * logits[row][j] - lse[row])), rounded once; zeros in rows without a token (whose dlogp is not read).  lse as the
- * forward call gave it.  dlogits may be logits with the same stride. */
+ * forward call gave it (rows of up to 16384 vectors of 16 bytes have their sum taken once more, so that its rounding is not in the probabilities).  dlogits may be logits with the same stride. */
 int prism_token_logprob_backward(const float* dlogp, const void* logits, const void* tokens, const float* lse, void* dlogits, prism_dtype dt,
                                  const prism_logits_desc* desc, void* stream);
 /* loss (fp32, one) = the sum over rows with a token of weight * l, in a fixed order,

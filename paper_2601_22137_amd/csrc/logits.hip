@@ -24,7 +24,8 @@ namespace {
 struct Logits {
   const void *z, *tokens;
   void* dz;
-  float *logp, *lse, *dlogp;             // results (backward: lse and dlogp are given)
+  float *logp, *lse, *dlogp;             // results
+  const float *dlogp_given, *lse_given;  // backward
   const float *advantages, *old, *ref, *weights;
   double *losses, *mean;                 // weighted losses of the rows; one over the number of rows with a token (null: every workgroup counts them itself)
   long long rows, zs, ds;
@@ -155,11 +156,12 @@ __device__ inline int token_of(const Logits& p, long long row) {
 // What is given for a row, read ahead
 struct Given {
   int token;
-  float weight, advantage, old, ref;
+  float weight, advantage, old, ref;     // backward: weight is the derivative by logp
 };
 __device__ inline Given given_for(const Logits& p, long long row) {
   Given g = {__builtin_amdgcn_readfirstlane(token_of(p, row)), 0.0f, 1.0f, 0.0f, 0.0f};
   if (p.weights) g.weight = p.weights[row];
+  if (p.dlogp_given) g.weight = p.dlogp_given[row];
   if (p.advantages) g.advantage = p.advantages[row];
   if (p.old) g.old = p.old[row];
   if (p.kl != 0.0) g.ref = p.ref[row];
@@ -193,6 +195,7 @@ __device__ inline float share_of(const Logits& p, const Sum& a, float z) { retur
 
 // What one thread computes of a row: its results, and the gradient at the token, s d (1 - p_t)
 __device__ inline float finish_row(const Logits& p, long long row, const Given& g, int count, const Sum& a, float z) {
+  if (p.dlogp_given) return g.weight * p.scale * share_of(p, a, z);
   double logp, lse;
   float share;
   if (a.s == 0.0f) {            // no others
@@ -321,7 +324,7 @@ __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4)
   }
 }
 
-// The same with the row in registers, NV vectors a thread: loss and gradient read it once
+// The same with the row in registers, NV vectors a thread: loss and gradient, or the gradient alone, read it once
 template <typename T, int THREADS, int NV, bool PAST>
 __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   constexpr int N = Vec<T>::N;
@@ -386,8 +389,9 @@ __global__ void __launch_bounds__(THREADS) logits_held_kernel(Logits p) {
   });
 }
 
-// lse up to which the gradient takes it as it was rounded: probabilities are off by 2^-24 |lse|, 4e-6 here
-constexpr float MOST_LSE = 64.0f;
+// The gradient of rows that registers do not hold is taken from lse, up to this one as it was rounded: probabilities are off by 2^-24 |lse|, 2^-20 here and 2^-19 in bf16, whose own
+// rounding is 2^-8.  A row beyond is summed once more (1000 x 131072 fp32: 312 us, 228 without).
+template <typename T> constexpr float MOST_LSE = sizeof(T) == 4 ? 32.0f : 64.0f;
 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(6))) logprob_backward_kernel(Logits p) {
@@ -404,8 +408,8 @@ __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(6)
     }
     const T* z = (const T*)p.z + row * p.zs;
     T* dz = (T*)p.dz + row * p.ds;
-    const float d = p.dlogp[row] * p.scale, lse = p.lse[row];
-    const bool given = fabsf(lse) <= MOST_LSE;
+    const float d = p.dlogp_given[row] * p.scale, lse = p.lse_given[row];
+    const bool given = fabsf(lse) <= MOST_LSE<T>;
     float m, factor, token;
     if (given) {                         // the reference is lse / s, rounded; the factor makes up for its rounding
       const double exact = (double)lse / p.exact_scale;
@@ -549,7 +553,7 @@ template <typename T> bool held(const Logits& p, hipStream_t s) {
 }
 
 void by_type(const Logits& p, int dt, bool back, hipStream_t s) {
-  if (!back && p.dz && (dt == PRISM_F32 ? held<float>(p, s) : held<__bf16>(p, s))) return;
+  if (p.dz && (dt == PRISM_F32 ? held<float>(p, s) : held<__bf16>(p, s))) return;
   if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary, back), back, s);
   else by_threads<__bf16>(p, threads_of(p.vocabulary, back), back, s);
 }
@@ -567,7 +571,7 @@ int launch_logprob(const void* z, const void* tokens, float* logp, float* lse, i
 int launch_logprob_backward(const float* dlogp, const void* z, const void* tokens, const float* lse, void* dz, int dt, const prism_logits_desc& d, hipStream_t s) {
   ProfScope prof(PK_LOGPROB_BACKWARD, s);
   Logits p = common(z, tokens, dt, d);
-  p.dlogp = (float*)dlogp; p.lse = (float*)lse; p.dz = dz;
+  p.dlogp_given = dlogp; p.lse_given = lse; p.dz = dz;
   by_type(p, dt, true, s);
   return PRISM_OK;
 }

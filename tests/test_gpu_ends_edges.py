@@ -1,4 +1,4 @@
-"""Operators at the ends of a model where their numbers are hardest: tokens next to certain, and logits that are no numbers.
+"""Operators at the ends of a model where their numbers are hardest: tokens next to certain, logits that are no numbers, large logarithms of sums.
 
 E = 2^-24 is the relative error of a rounding to fp32, U that of one to the type of the arrays."""
 import numpy as np
@@ -144,3 +144,24 @@ def test_ratios_that_are_no_numbers(prism):
     assert r.dlogp[3] == 0 and not bool(r.dlogits[3].any())
     r = prism.policy_loss(z[3:], t[3:], advantages=a[3:], old_logp=old[3:])
     assert r.loss == 0
+
+
+# ------------------------------------------------------------------------------------------------ large logarithms of sums
+
+@pytest.mark.parametrize("v", [3, 300, 5000, 40000, 65541])
+def test_probabilities_of_rows_with_a_large_lse(prism, v):
+    """fp32: lse is rounded by up to 2^-24 |lse|, 32 E here, which the probabilities do not take over.  Three logits close together, the others excluded: an exponent's roundings are 3 E of 0.25, in the probability and
+    in the sum; two sums, two instructions of 2 E, the reciprocal's 2 E and six roundings of products each side."""
+    g = torch.Generator().manual_seed(3)
+    rows = 500
+    z = torch.empty(rows, 3).uniform_(40.0, 62.0, generator=g)[:, :1] + 0.25 * torch.rand(rows, 3, generator=g)
+    z[::2] -= 100.0
+    t = torch.randint(0, 3, (rows,), generator=g)
+    places = torch.arange(3) * (v - 1) // 2
+    z, t = torch.full((rows, v), -INF, device="cuda").index_copy_(1, places.cuda(), z.cuda()), places[t].cuda()
+    _, lse = prism.token_logprob(z, t)
+    _, rest, p = R.logprob_apart(_f64(z), t.tolist(), 1.0)
+    d = torch.rand(rows, generator=g).cuda()
+    ref = R.logprob_gradient(_f64(d), p, t.tolist(), 1.0)
+    ref[np.arange(rows), t.cpu().numpy()] = _f64(d) * rest
+    _within(prism.token_logprob_backward(d, z, t, lse), ref, (2 * 3 * 0.25 + 2 + 4 + 2 + 12) * E * np.abs(ref), "dlogits")
