@@ -1,4 +1,5 @@
-"""Operators at the ends of a model where their numbers are hardest: tokens next to certain, logits that are no numbers, large logarithms of sums.
+"""Operators at the ends of a model where their numbers are hardest: tokens next to certain, logits that are no numbers, large logarithms of sums, a ratio on its border; and the
+kernels that only long odd rows, rows at odd entries or large arrays of fp32 reach.
 
 E = 2^-24 is the relative error of a rounding to fp32, U that of one to the type of the arrays."""
 import numpy as np
@@ -165,3 +166,111 @@ def test_probabilities_of_rows_with_a_large_lse(prism, v):
     ref = R.logprob_gradient(_f64(d), p, t.tolist(), 1.0)
     ref[np.arange(rows), t.cpu().numpy()] = _f64(d) * rest
     _within(prism.token_logprob_backward(d, z, t, lse), ref, (2 * 3 * 0.25 + 2 + 4 + 2 + 12) * E * np.abs(ref), "dlogits")
+
+
+# --------------------------------------------------------------------------------------------------- a ratio on its border
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("v", [1, 300, 5000, 140000])
+def test_a_ratio_on_its_border_has_the_gradient_of_the_ratio(prism, dtype, v):
+    """Tokens without another logit: logp is 0, the ratio 1 and nothing is lost to rounding; held between 1 and 1.  And where there are others the gradient reaches them."""
+    z = torch.full((4, v), -INF, dtype=dtype, device="cuda")
+    t = torch.tensor([0, v // 2, v - 1, 0], device="cuda")
+    z[torch.arange(4), t] = torch.tensor([0.0, 3.0, -7.0, 1.5], dtype=dtype, device="cuda")
+    a, w = torch.tensor([1.0, -1.0, 2.0, -0.5], device="cuda"), torch.ones(4, device="cuda")
+    r = prism.policy_loss(z, t, advantages=a, old_logp=torch.zeros(4, device="cuda"), weights=w, clip=(0.0, 0.0))
+    assert torch.equal(r.logp, torch.zeros(4, device="cuda")) and torch.equal(r.dlogp, -a) and r.loss == -a.sum() and not bool(r.dlogits.any())
+    if v > 1:
+        z[torch.arange(4), (t + 1) % v] = z[torch.arange(4), t]
+        logp, _ = prism.token_logprob(z, t)                  # -log 2, rounded: the ratio is off by 2^-24 at most
+        r = prism.policy_loss(z, t, advantages=a, old_logp=logp, weights=w, clip=(0.25, 0.25))
+        assert bool(((r.dlogp + a).abs() <= 4 * E * a.abs()).all()) and bool(((r.dlogits[torch.arange(4), t].float() + a / 2).abs() <= (_u(dtype) + 8 * E) * a.abs()).all())
+
+
+# ------------------------------------------------------------------------- rows of the norm at odd entries, and long odd ones
+
+def _at_odd_entries(t):
+    whole = torch.full((t.shape[0], t.shape[1] + 5), NAN, dtype=t.dtype, device="cuda")
+    whole[:, 3:3 + t.shape[1]] = t
+    view = whole[:, 3:3 + t.shape[1]]
+    assert not view.is_contiguous() or t.shape[0] == 1
+    return view
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,width", [(1, 1), (3, 2), (5, 8), (257, 64), (70, 100), (11, 129), (9, 513), (20, 768), (2, 1111), (3, 2050), (3, 4096), (2, 5001), (2, 7001), (2, 8200), (2, 16383)])
+def test_norm_of_rows_at_odd_entries(prism, dtype, rows, width):
+    """The same bits as those of rows next to each other, with NaN around each row."""
+    g = torch.Generator(device="cuda").manual_seed(rows + width)
+    make = lambda: torch.randn(rows, width, generator=g, device="cuda").to(dtype)   # noqa: E731
+    x, r, dy, dt, w = make(), make(), make(), make(), torch.rand(width, generator=g, device="cuda")
+    for res in (None, r):
+        y, total, stats = prism.layer_norm(x, w, residual=res)
+        got = prism.layer_norm(_at_odd_entries(x), w, residual=None if res is None else _at_odd_entries(res))
+        assert torch.equal(got[0], y) and torch.equal(got[1], total) and torch.equal(got[2], stats)
+        want = prism.layer_norm_backward(dy, total, stats, w, dtotal=None if res is None else dt)
+        got = prism.layer_norm_backward(_at_odd_entries(dy), _at_odd_entries(total), stats, w, dtotal=None if res is None else _at_odd_entries(dt))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# 1024 threads a row with part of a vector at its end: over 3 * 256 vectors
+@pytest.mark.parametrize("dtype,width", [(F32, 3079), (F32, 8193), (F32, 16383), (BF16, 6147), (BF16, 9001), (BF16, 16383)])
+@pytest.mark.parametrize("center,residual,affine", [(True, False, True), (True, True, True), (False, True, True), (False, False, False)])
+@pytest.mark.parametrize("rows", [2, 600])
+def test_norm_of_long_odd_rows(prism, dtype, width, center, residual, affine, rows):
+    """Against the oracle, with the bounds of the other widths."""
+    import test_gpu_ends
+    test_gpu_ends.test_layer_norm_and_gradients(prism, dtype, center, residual, affine, "plain" if rows > 2 else "odd", rows, width)
+
+
+# ------------------------------------------------------------------------------------------- large arrays of fp32
+
+def _parts(rows, size):
+    return [slice(a, a + size) for a in (0, rows // 2, rows - size)]
+
+
+@pytest.mark.parametrize("dtype,v", [(F32, 200), (F32, 2000), (F32, 4000), (F32, 8000), (F32, 16384), (F32, 32768), (F32, 65536), (F32, 66001), (BF16, 2000), (BF16, 4000), (BF16, 8000), (BF16, 16384)])
+def test_logits_larger_than_the_caches(prism, dtype, v):
+    """Kernels that read past the caches, of every number of threads: rows are the same bits as in calls of a part of them."""
+    g = torch.Generator(device="cuda").manual_seed(v)
+    rows = (300 << 20) // (v * (4 if dtype == F32 else 2))
+    z, t = torch.randn(rows, v, generator=g, device="cuda").to(dtype), torch.randint(-1, v, (rows,), generator=g, device="cuda")
+    w, old = torch.rand(rows, generator=g, device="cuda"), torch.full((rows,), -12.0, device="cuda")
+    logp, lse = prism.token_logprob(z, t)
+    r = prism.policy_loss(z, t, old_logp=old, weights=w)
+    for part in _parts(rows, 70):
+        b = prism.policy_loss(z[part], t[part], old_logp=old[part], weights=w[part])
+        assert torch.equal(r.dlogits[part], b.dlogits) and torch.equal(r.logp[part], b.logp)
+        c = prism.token_logprob(z[part], t[part])
+        assert torch.equal(logp[part], c[0]) and torch.equal(lse[part], c[1])
+
+
+@pytest.mark.parametrize("width", [100, 101, 768, 771, 4096, 4099, 8192, 16384, 16383])
+def test_norm_of_fp32_larger_than_the_caches(prism, width):
+    g = torch.Generator(device="cuda").manual_seed(width)
+    rows = (100 << 20) // (4 * width)
+    make = lambda: torch.randn(rows, width, generator=g, device="cuda")   # noqa: E731
+    x, res, weight = make(), make(), torch.rand(width, generator=g, device="cuda")
+    y, total, stats = prism.layer_norm(x, weight, residual=res)
+    dx, dw, db = prism.layer_norm_backward(y, total, stats, weight, dtotal=res)
+    for part in _parts(rows, 300):
+        b = prism.layer_norm(x[part], weight, residual=res[part])
+        assert all(torch.equal(p, q) for p, q in zip(b, (y[part], total[part], stats[part])))
+        assert torch.equal(dx[part], prism.layer_norm_backward(y[part], total[part], stats[part], weight, dtotal=res[part])[0])
+    n = (total.double() - stats[:, :1].double()) * stats[:, 1:].double()
+    for got, terms in ((dw, y.double() * n), (db, y.double())):
+        # 256 workgroups at least, and so rows / 256 terms a thread at most; n is off by two roundings, and parts are joined
+        assert bool(((got.double() - terms.sum(0)).abs() <= (rows // 256 + 40) * E * terms.abs().sum(0)).all())
+
+
+def test_embedding_of_fp32_larger_than_the_caches(prism):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    n, rows, width = 40000, 12000, 1000
+    dout, table, t = torch.randn(n, width, generator=g, device="cuda"), torch.randn(rows, width, generator=g, device="cuda"), torch.randint(-1, rows, (n,), generator=g, device="cuda")
+    out = prism.embedding(t, table, scale=0.5)
+    assert torch.equal(out, torch.where((t >= 0).unsqueeze(1), table[t.clamp(min=0)] * 0.5, torch.zeros((), device="cuda")))
+    d = prism.embedding_backward(dout, t, rows)
+    whole = torch.zeros(rows, width, device="cuda", dtype=torch.float64).index_add_(0, t.clamp(min=0), torch.where((t >= 0).unsqueeze(1), dout.double(), 0.0))
+    size = torch.zeros(rows, width, device="cuda", dtype=torch.float64).index_add_(0, t.clamp(min=0), torch.where((t >= 0).unsqueeze(1), dout.abs().double(), 0.0))
+    # 64 terms one after the other at most, parts rounded, joined in 64 bits, rounded
+    assert bool(((d.double() - whole).abs() <= 67 * E * size).all())
