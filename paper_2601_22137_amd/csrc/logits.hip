@@ -174,20 +174,35 @@ __device__ inline float exp_of_difference(const Logits& p, float x, float y) {
   return k < -150.0f ? 0.0f : exp2_of(k) * fmaf(fmaf(d, p.c, -k) + fmaf(d, p.c_rest, rest * p.c), (float)LN2, 1.0f);
 }
 
+// log(1 + y), y from -2^-20, NaN for NaN: 1 + y = f 2^k, f next to 1, and log f = 2 artanh((f - 1) / (f + 1)), its series cut off where it is 4e-14 of it; f - 1 is y where k is 0, so that small ones
+// keep their digits.  (The library's log and log1p are good to a unit of 64 bits, with three times the instructions and, log1p, a dozen registers more, for a sum in 32 bits.)
+__device__ inline double log_of_one_and(double y) {
+  double f = __builtin_amdgcn_frexp_mant(1.0 + y);
+  int k = __builtin_amdgcn_frexp_exp(1.0 + y);
+  if (f < 0.70710678118654752440) {
+    f *= 2.0;
+    --k;
+  }
+  double r = __builtin_amdgcn_rcp(f + 1.0);
+  r = fma(fma(-(f + 1.0), r, 1.0), r, r);
+  const double x = (k == 0 ? y : f - 1.0) * r, q = x * x;
+  double series = 2.0 / 15;
+#pragma unroll
+  for (int i = 13; i > 1; i -= 2) series = fma(series, q, 2.0 / i);
+  return fma((double)k, LN2, fma(series * q, x, 2.0 * x));
+}
+
 // The sum over a row's other logits beside its token's exponential e = exp(-|s (m - z)|), which is as good as that sum.  z: the logit of the token
 struct Others {
   float e;
   bool above;                   // one of them is, m > z: everything relative to m then, to z otherwise
-  __device__ Others(const Logits& p, const Sum& a, float z) : above(a.m > z) { e = above ? exp_of_difference(p, z, a.m) : exp_of_difference(p, a.m, z); }
+  __device__ Others(const Logits& p, const Sum& a, float z) : above(a.m > z) { e = exp_of_difference(p, above ? z : a.m, above ? a.m : z); }
   // all of them, less 1
   __device__ float rest(const Sum& a) const { return above ? (a.s - 1.0f) + e : a.s * e; }
   // 1 - p_t
   __device__ float share(const Sum& a) const { return (above ? a.s : a.s * e) * __builtin_amdgcn_rcpf(1.0f + rest(a)); }
-  // logp = -max(0, s (m - z)) - this, log(1 + y): next to 0 the series, off by y^3 / 4 = 2e-13 of it (the library's log1p takes a dozen registers more)
-  __device__ double log_of_all(const Sum& a) const {
-    const float y = rest(a);
-    return y < 1e-4f ? (double)(y * (1.0f - y * (0.5f - y * (1.0f / 3.0f)))) : log(1.0 + (double)y);
-  }
+  // logp = -max(0, s (m - z)) - this
+  __device__ double log_of_all(const Sum& a) const { return log_of_one_and(rest(a)); }
 };
 
 __device__ inline float share_of_one(float z) { return z == -INFINITY ? 1.0f : z - z; }         // no others: 0, and NaN stays
