@@ -554,6 +554,7 @@ template <typename T> void by_threads(const Logits& p, int threads, bool back, h
 template <typename T, bool PAST> void (*held_kernel(int vectors, int& threads))(Logits) {
   if (vectors <= 64 * 8) return threads = 64, vectors <= 64 * 4 ? logits_held_kernel<T, 64, 4, PAST> : logits_held_kernel<T, 64, 8, PAST>;
   if (vectors <= 256 * 8) return threads = 256, vectors <= 256 * 4 ? logits_held_kernel<T, 256, 4, PAST> : logits_held_kernel<T, 256, 8, PAST>;
+  if (vectors <= 512 * 5) return threads = 512, logits_held_kernel<T, 512, 5, PAST>;         // (three pieces of eight would hold nothing: 8192 x 20000 bf16 120 us, 124 in eight)
   if (vectors <= 512 * 8) return threads = 512, logits_held_kernel<T, 512, 8, PAST>;
   if (vectors <= 512 * 16) return threads = 512, logits_held_kernel<T, 512, 16, PAST>;        // two workgroups a CU: 2684 x 50001 bf16 133 us, with 1024 threads 159
   if (vectors <= 1024 * 16) return threads = 1024, logits_held_kernel<T, 1024, 16, PAST>;
