@@ -6,13 +6,13 @@
 //   dl / dlogp = -(r A where r A <= clip(r) A, else 0) + kl (1 - exp(f))
 //
 // A row is one workgroup's (or one wave's, to 4096 logits of bf16).  Its exponentials are taken in base 2 relative to a running maximum m, exp2(c (z - m)), c = s log2 e, every thread with its own, joined
-// at the end: the difference first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  The sum is over the others than the token, and in 32 bits to its
-// end, joins too: as a token next to certain has 1 - p_t from it, not what is left of 1, its errors are relative to 1 - p_t and to logp.  What follows from it is in 64 bits: a ratio next to where
-// it is cut off decides about a row's gradient.
+// at the end: the difference first, so that logits of the type's lowest value (masks) neither overflow nor differ from one another.  The sum is over the others than the token, in 32 bits to its end,
+// joins too: o has its errors, and so 1 - p_t and logp have them relative to themselves, however close to certain the token is.  The loss follows from logp in 64 bits: a ratio next to where it is
+// cut off decides about a row's gradient.
 //
-// Loss and gradient in one pass hold the row in registers, up to 16384 vectors of 16 bytes, so that it is read once and written once: 8192 x 32768 bf16 172 us (1013 MB, 5.9 TB/s, vector units 72 % busy),
-// 2048 x 131072 203 us (5.0 TB/s: the registers of a CU hold one such row, and nothing reads while it is computed).  Read twice, the second time from the caches: 249 and 266.  Log-probabilities
-// alone, 4096 x 131072: 167 us, 6.4 TB/s.  Two transcendental instructions a logit, four cycles each, are half of what the vector units do.
+// Loss and gradient in one pass hold the row in registers, up to 16384 vectors of 16 bytes, so that it is read once and written once: 8192 x 32768 bf16 172 us (1013 MB, 5.9 TB/s, vector units 73 % busy),
+// 2048 x 131072 204 us (5.0 TB/s: the registers of a CU hold one such row, and nothing reads while it is computed).  Read twice, the second time from the caches: 249 and 266.  Log-probabilities
+// alone, 4096 x 131072: 165 us, 6.5 TB/s.  The gradient of given derivatives, in the same way: 8192 x 32768 201 us, 4096 x 32000 fp32 181.  Two transcendental instructions a logit, four cycles each, are half of what the vector units do.
 #include <cmath>
 
 #include "layer.h"
@@ -39,7 +39,8 @@ constexpr double LN2 = 0.69314718055994530942;
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// c (z - m): fp32 with the rest of c, whose rounding would show there (of a difference of 20: 4e-7 of the exponential)
+// c (z - m): fp32 with the rest of c, whose rounding would show there (of a difference of 20: 4e-7 of the exponential).  bf16 leaves it out, an instruction in nine: its logits are rounded by 2^-8 of
+// themselves, and logp and lse take 2^-24 of the mean distance from the largest, 3e-7 of 5.
 template <typename T> __device__ inline float power(const Logits& p, float z, float m) {
   const float d = z - m;
   if constexpr (sizeof(T) == 4) return fmaf(d, p.c, d * p.c_rest);
@@ -528,11 +529,10 @@ Logits common(const void* z, const void* tokens, int dt, const prism_logits_desc
   return p;
 }
 
-// Threads of a row that is read in pieces, whatever the number of rows, so that a row's results do not depend on what else is in the call.  Sums take four vectors a thread at a time, and fewer threads
-// waste fewer of them (16384 rows of 8000 logits, bf16: 64 threads 44 us, 256 67); the gradients one after the other (256 threads 100 us, 64 111).
-int threads_of(int vocabulary, bool back) {
+// Threads of a row that is read in pieces, whatever the number of rows, so that a row's results do not depend on what else is in the call.  Four vectors a thread are under way at a time, and fewer
+// threads waste fewer of them (log-probabilities of 16384 rows of 8000 logits, bf16: 64 threads 44 us, 256 67).
+int threads_of(int vocabulary) {
   const int vectors = (vocabulary + 7) / 8;
-  if (back) return vectors <= 512 ? 64 : vectors <= 2048 ? 256 : 512;
   return vectors <= 1024 ? 64 : vectors <= 4096 ? 256 : 512;
 }
 
@@ -570,8 +570,8 @@ template <typename T> bool held(const Logits& p, hipStream_t s) {
 
 void by_type(const Logits& p, int dt, bool back, hipStream_t s) {
   if (p.dz && (dt == PRISM_F32 ? held<float>(p, s) : held<__bf16>(p, s))) return;
-  if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary, back), back, s);
-  else by_threads<__bf16>(p, threads_of(p.vocabulary, back), back, s);
+  if (dt == PRISM_F32) by_threads<float>(p, threads_of(p.vocabulary), back, s);
+  else by_threads<__bf16>(p, threads_of(p.vocabulary), back, s);
 }
 
 }  // namespace

@@ -263,6 +263,25 @@ def test_norm_of_fp32_larger_than_the_caches(prism, width):
         assert bool(((got.double() - terms.sum(0)).abs() <= (rows // 256 + 40) * E * terms.abs().sum(0)).all())
 
 
+def test_gradient_of_log_probabilities_of_many_rows(prism):
+    """More rows than one launch has workgroups for: from lse, or their sums once more, like those of a call of fewer, to the rounding of lse and some of each exponential."""
+    rows = (1 << 20) + 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z, t = torch.randn(rows, 5, generator=g, device="cuda"), torch.randint(-1, 5, (rows,), generator=g, device="cuda")
+    z[::3] += 80.0
+    z[1::7] -= 40.0
+    z[torch.arange(rows, device="cuda"), t.clamp(min=0)] += 12.0 * torch.rand(rows, generator=g, device="cuda")
+    d = torch.rand(rows, generator=g, device="cuda") + 0.5
+    _, lse = prism.token_logprob(z, t)
+    got = prism.token_logprob_backward(d, z, t, lse)
+    half = rows // 2
+    want = torch.cat([prism.token_logprob_backward(d[part], z[part], t[part], lse[part]) for part in (slice(0, half), slice(half, rows))])
+    # exponents of 20 at most: 3 E of that on either side, 20 E of factors and sums, and 32 E of lse
+    assert bool(((got - want).abs() <= (2 * 3 * 20 + 2 * 20 + 32) * E * want.abs()).all())
+    assert not bool(got[t < 0].any())
+    assert torch.equal(got, prism.token_logprob_backward(d, z, t, lse, out=z))
+
+
 def test_embedding_of_fp32_larger_than_the_caches(prism):
     g = torch.Generator(device="cuda").manual_seed(1)
     n, rows, width = 40000, 12000, 1000
